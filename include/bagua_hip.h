@@ -410,6 +410,101 @@ int bagua_bucket_flatten_batched_run(const void* const* plans, const size_t* T, 
                                      void* stream);
 
 /*
+ * The step that follows a round where the parameters are not one fp32 bucket: an AdamW update of any number of separate
+ * tensors in one launch (bias correction, decoupled weight decay, gradients and parameters in 32 or 16 bits, moments in 32 or
+ * in 8 bits), and in front of it the global norm of their gradients with the factor that clips it.  Both read a table of the
+ * tensors that bagua_tensor_plan writes into the caller's workspace; the plan SYNCHRONISES `stream` (a set-up call, as
+ * bagua_flatten_plan), the two calls only launch and can be recorded into a HIP graph.
+ *
+ * bagua_tensor_plan: a tensor is contiguous, may be empty, and needs the alignment of its element type only.
+ *   numel          host[T], elements; T >= 1
+ *   grad           host[T] of device pointers, read only; grad_type BAGUA_F32, BAGUA_BF16 or BAGUA_F16
+ *   param          host[T], in-out, or NULL (a plan for the norm alone: everything below is NULL, state_bits 0)
+ *   param_type     BAGUA_F32, or BAGUA_BF16 (no fp32 copy anywhere; grad_type must then be BAGUA_F32 or BAGUA_BF16)
+ *   state_bits     32: m and v are fp32[numel];  8: E4M3 codes u8[numel] of m and of sqrt(v), with one fp32 scale for every
+ *                  256 elements of a tensor, counted from its first one, in m_scale and v_scale, fp32[ceil(numel / 256)];
+ *                  value = code * scale.  All zero = the state before the first step.
+ *   copy           host[T] of device pointers, copy_type[numel], written: the parameters rounded to nearest for the next
+ *                  forward pass; copy_type BAGUA_BF16 or BAGUA_F16; NULL: none.  Only with fp32 parameters.
+ *   decay          host[T] of factors on the step's weight decay (0 for tensors that are not decayed); NULL: 1 for all
+ *   workspace      device, >= bagua_tensor_plan_bytes(numel, T) bytes, 16-byte aligned; belongs to the plan from then on
+ *   plan           host, written; the calls take it.  Its fields are not for the caller.
+ * Pointers of empty tensors may be NULL.  Aliasing rule over all tensors of the plan, and the workspace.
+ *
+ * bagua_grad_norm:  out[0] = N = grad_scale * sqrt(sum of g^2 over all tensors),  out[1] = grad_scale * min(1, max_norm / (N + 1e-6)).
+ *   Summed in 64 bits in an order that depends on the sizes alone.  grad_scale: what the gradients have to be multiplied with
+ *   (1 / loss scale; 1: nothing).  max_norm: INFINITY for no clipping.  N not finite: out[1] = 0.
+ *   out device fp32[2], written.  Calls on one plan must not overlap in time (it holds the partial sums).
+ *
+ * bagua_adamw_step:  step t >= 1, all operations in fp32 and rounded one by one, host factors formed in 64 bits:
+ *   g = grad;  if clip: g = g * clip[1];
+ *   m = beta1*m + (1-beta1)*g;   v = beta2*v + (1-beta2)*(g*g);   r = sqrt(v);
+ *   u = m / (r * fl(1/sqrt(1-beta2^t)) + eps);   p = p - (u * fl(lr/(1-beta1^t)) + p * fl(decay_i * fl(lr*weight_decay)))
+ *   clip     device fp32[2] as bagua_grad_norm leaves it, or NULL.  clip[0] not finite: the step changes nothing.
+ *   8 bits:  v = r*r of the stored root.  scale = fl(max |x| of the block * fl(1/448)), 0 below 2^-126; y = x * fl(1/scale).
+ *            m: y to the nearest E4M3 (ties to even).  r: stochastically, code = floor(E4M3 position of y + random / 2^20), not
+ *            below 1 where r > 0 and not above 448.  (A step changes r by up to (1-beta2)/2 of itself, far less than half the
+ *            distance of two codes; rounded to nearest, r would stay where it is for ever.)
+ *   BF16 p:  stochastically, p = high half of (bits of p + random of 16 bits).
+ *   random:  h(i) = mix(i/4 * 0x9E3779B9 + mix(tensor * 0x9E3779B9 + seed)) for element i of a tensor, turned left by 8 * (i mod 4),
+ *            of which r takes the upper 20 bits; p the upper 16 of mix(h + 0x9E3779B9) turned in the same way;
+ *            mix(x): x ^= x>>16, x *= 0x6A09E667, x ^= x>>15, x *= 0xBB67AE85, x ^= x>>16.   `seed`: another one each step.
+ */
+enum { BAGUA_F32 = 0, BAGUA_BF16 = 1, BAGUA_F16 = 2 };
+typedef struct {
+    void* workspace;
+    uint64_t tiles;
+    uint32_t tensors;
+    int32_t grad_type, param_type, copy_type, state_bits;
+} bagua_tensor_plan_t;
+size_t bagua_tensor_plan_bytes(const size_t* numel, size_t T);
+int bagua_tensor_plan(const size_t* numel, size_t T, const void* const* grad, int grad_type, void* const* param, int param_type,
+                      void* const* m, void* const* v, int state_bits, float* const* m_scale, float* const* v_scale,
+                      void* const* copy, int copy_type, const float* decay, void* workspace, size_t workspace_bytes,
+                      bagua_tensor_plan_t* plan, void* stream);
+int bagua_grad_norm(const bagua_tensor_plan_t* plan, double grad_scale, double max_norm, float* out, void* stream);
+int bagua_adamw_step(const bagua_tensor_plan_t* plan, uint64_t step, double lr, double beta1, double beta2, double eps,
+                     double weight_decay, const float* clip, uint32_t seed, void* stream);
+
+/*
+ * The balance loss of a mixture of experts: the training loss whose statistics are sums over the tokens of ALL data-parallel
+ * workers.  For token t of a worker, logits x_t over E experts and `top_k` chosen experts:
+ *   p_t = softmax(x_t);   S_e = sum of p_te over all tokens;   C_e = number of choices of expert e;   N = number of tokens;
+ *   loss = alpha * E * sum_e (C_e / (top_k*N)) * (S_e / N);   weight_e = d loss / d S_e = alpha * E * C_e / (top_k*N*N);
+ *   d loss / d x_te = p_te * (weight_e - sum_j weight_j p_tj)              (the counts have no gradient).
+ * N = 0: loss 0, weights 0.  Perfect balance of full rows gives loss = alpha.
+ *
+ * bagua_balance_stats: forward over k workers' tokens in one launch.
+ *   dtype     BAGUA_F32, BAGUA_BF16 or BAGUA_F16: of the logits
+ *   logits    host[k] of device [tokens[i]][experts], rows `ld` >= experts elements apart; the alignment of an element suffices
+ *   tokens    host[k], any may be 0 (its pointers may then be NULL)
+ *   ids       host[k] of device [tokens[i]][top_k] chosen experts, int32 (id_bytes 4) or int64 (8), rows `ids_ld` >= top_k apart;
+ *             an id outside [0, experts) is a choice that was dropped: it counts for no expert
+ *   mask      host[k] of device u8[tokens[i]], 0 = padding: the token counts nowhere, its logits and ids are not looked at; NULL: none
+ *   counts    device int32[experts + 1], written: C_e, and N behind them
+ *   prob      device fp32[experts], written: S_e
+ *   loss, weight   device fp32[1], fp32[experts], written; NULL together where other GPUs' sums are still to be added
+ *   workspace device, >= bagua_balance_workspace_bytes(experts) bytes, 16-byte aligned.  Its first 64 bytes must be 0 before the
+ *             first call; every call leaves them so.  Calls on one workspace must not overlap in time.
+ *   limits    1 <= k <= BAGUA_MAX_WORKERS, experts <= BAGUA_MAX_EXPERTS, top_k <= experts, all choices together below 2^31
+ * bagua_balance_loss: loss and weights from counts and prob that were added up over GPUs.
+ * bagua_balance_grad: backward; dlogits[i] (rows ld_out apart) = *upstream * d loss / d x, 0 for padding.  upstream: device
+ *   fp32[1], NULL = 1.
+ * A row of logits that is -infinity throughout has probabilities 0 and gradient 0; NaN and +infinity in a row that counts make that
+ * row's probabilities NaN.  Sums over tokens are formed in fp32 within a workgroup and in 64 bits across them, in a fixed order.
+ */
+#define BAGUA_MAX_EXPERTS 2048
+size_t bagua_balance_workspace_bytes(int experts);
+int bagua_balance_stats(int dtype, const void* const* logits, size_t ld, const size_t* tokens, int k, int experts, const void* const* ids,
+                        int id_bytes, size_t ids_ld, int top_k, const uint8_t* const* mask, int32_t* counts, float* prob, double alpha,
+                        float* loss, float* weight, void* workspace, size_t workspace_bytes, void* stream);
+int bagua_balance_loss(const int32_t* counts, const float* prob, int experts, int top_k, double alpha, float* loss, float* weight,
+                       void* stream);
+int bagua_balance_grad(int dtype, const void* const* logits, size_t ld, const size_t* tokens, int k, int experts,
+                       const uint8_t* const* mask, const float* weight, const float* upstream, void* const* dlogits, size_t ld_out,
+                       void* stream);
+
+/*
  * Measurement utilities used by the benchmark to state what the memory system of the GPU at hand delivers for
  * plain access patterns (the ceilings printed next to the roofline fractions); no arithmetic of the method.
  * bagua_probe_read: a read-only reduction, tile_sums[t] = sum of x[4096 t .. 4096 t + 4095] (device fp32[ceil(n/4096)]).

@@ -29,6 +29,8 @@ CODEC_SIGN1 = 1
 AVG_FP = 0
 AVG_LP_MINMAX_U8 = 1
 MAX_WORKERS = 32
+MAX_EXPERTS = 2048
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # BAGUA_F32, BAGUA_BF16, BAGUA_F16
 
 EXPORTS = (
     "bagua_status_string", "bagua_flatten_workspace_bytes", "bagua_flatten_plan", "bagua_bucket_flatten_run",
@@ -41,6 +43,8 @@ EXPORTS = (
     "bagua_batch_workspace_bytes", "bagua_compress_minmax_u8_batched", "bagua_sign_compress_ef_batched",
     "bagua_decompress_reduce_recompress_batched", "bagua_bucket_flatten_batched_run", "bagua_probe_read",
     "bagua_probe_streams", "bagua_flatten_sign_compress_ef", "bagua_decompress_unflatten", "bagua_reduce_compress_sign_ef", "bagua_decompress_sgd_step_topk", "bagua_decompress_adam_step_topk",
+    "bagua_tensor_plan_bytes", "bagua_tensor_plan", "bagua_grad_norm", "bagua_adamw_step",
+    "bagua_balance_workspace_bytes", "bagua_balance_stats", "bagua_balance_loss", "bagua_balance_grad",
 )
 
 
@@ -98,10 +102,19 @@ def _load():
     lib.bagua_sign_compress_ef_batched.argtypes = [vp, vp, vp, sz, sz, vp, vp, vp, sz, vp]
     lib.bagua_decompress_reduce_recompress_batched.argtypes = [i32, vp, vp, i32, vp, vp, sz, sz, vp, vp, vp, vp, sz, vp]
     lib.bagua_bucket_flatten_batched_run.argtypes = [vp, vp, vp, vp, sz, vp, sz, vp]
+    cd = ctypes.c_double
+    lib.bagua_tensor_plan_bytes.argtypes = [vp, sz]
+    lib.bagua_tensor_plan.argtypes = [vp, sz, vp, i32, vp, i32, vp, vp, i32, vp, vp, vp, i32, vp, vp, sz, vp, vp]
+    lib.bagua_grad_norm.argtypes = [vp, cd, cd, vp, vp]
+    lib.bagua_adamw_step.argtypes = [vp, ctypes.c_uint64, cd, cd, cd, cd, cd, vp, ctypes.c_uint32, vp]
+    lib.bagua_balance_workspace_bytes.argtypes = [i32]
+    lib.bagua_balance_stats.argtypes = [i32, vp, sz, vp, i32, i32, vp, i32, sz, i32, vp, vp, vp, cd, vp, vp, vp, sz, vp]
+    lib.bagua_balance_loss.argtypes = [vp, vp, i32, i32, cd, vp, vp, vp]
+    lib.bagua_balance_grad.argtypes = [i32, vp, sz, vp, i32, i32, vp, vp, vp, vp, sz, vp]
     for name in EXPORTS[2:]:
-        if name != "bagua_batch_workspace_bytes":
-            getattr(lib, name).restype = i32
-    lib.bagua_batch_workspace_bytes.restype = sz
+        getattr(lib, name).restype = i32
+    for name in ("bagua_batch_workspace_bytes", "bagua_tensor_plan_bytes", "bagua_balance_workspace_bytes"):
+        getattr(lib, name).restype = sz
     return lib
 
 
@@ -571,6 +584,163 @@ def bagua_bucket_flatten_batched_run(plans, Ts, buckets, workspace, stream=None,
     ba = (ctypes.c_void_p * B)(*[_ptr(b, torch.float32) for b in buckets])
     return _run(prepare, "bagua_bucket_flatten_batched_run", _lib.bagua_bucket_flatten_batched_run,
                 (pa, _sizes(Ts), ba, _sizes([b.numel() for b in buckets]), B, wp, wb), (plans, buckets, workspace), stream)
+
+
+# ---------------------------------------------------------------------------------------------- many tensors
+class _PlanStruct(ctypes.Structure):
+    _fields_ = [("workspace", ctypes.c_void_p), ("tiles", ctypes.c_uint64), ("tensors", ctypes.c_uint32),
+                ("grad_type", ctypes.c_int32), ("param_type", ctypes.c_int32), ("copy_type", ctypes.c_int32), ("state_bits", ctypes.c_int32)]
+
+
+class TensorPlan:
+    """What bagua_tensor_plan has laid out: the table of the tensors in the workspace.  Holds the tensors: their addresses are
+    in the table, so a tensor that is replaced by another one needs a new plan."""
+
+    def __init__(self, struct, keep):
+        self._struct, self._at, self._keep = struct, ctypes.addressof(struct), keep
+
+
+def _type_of(tensors, what, allowed):
+    """The one type of a list of tensors."""
+    dtype = tensors[0].dtype
+    if dtype not in allowed:
+        raise ValueError("%s must be one of %s, got %s" % (what, ", ".join(str(d) for d in allowed), dtype))
+    return dtype
+
+
+def _tensors(tensors, dtype, numels):
+    """Addresses of contiguous tensors that hold at least those numbers of elements."""
+    at = (ctypes.c_void_p * len(tensors))()
+    for i, (t, n) in enumerate(zip(tensors, numels)):
+        at[i] = _ptr(t, dtype, n * t.element_size()) if n else None
+    return at
+
+
+def bagua_tensor_plan_bytes(numels):
+    """Bytes of workspace that a plan over tensors of these sizes needs."""
+    return int(_lib.bagua_tensor_plan_bytes(_sizes(numels), len(numels)))
+
+
+def bagua_tensor_plan(grads, workspace, params=None, m=None, v=None, m_scales=None, v_scales=None, copies=None, decay=None, stream=None):
+    """Table of T tensors for bagua_grad_norm (grads alone suffice) and bagua_adamw_step.  Lists of T contiguous GPU tensors:
+    grads fp32, bf16 or fp16; params fp32 or bf16; m, v fp32, or float8_e4m3fn with m_scales, v_scales (fp32, one value for 256
+    elements); copies bf16 or fp16; decay: T factors on the weight decay.  Synchronises the stream."""
+    T = len(grads)
+    if T == 0:
+        raise ValueError("a plan needs at least one tensor")
+    if (params is None) != (m is None) or (params is None) != (v is None):
+        raise ValueError("params, m and v go together")
+    _same_len(T, params=params, m=m, v=v, m_scales=m_scales, v_scales=v_scales, copies=copies, decay=decay)
+    ns = [g.numel() for g in grads]
+    gt = _type_of(grads, "gradients", (torch.float32, torch.bfloat16, torch.float16))
+    pt = mt = ct = None
+    if params is not None:
+        pt = _type_of(params, "parameters", (torch.float32, torch.bfloat16))
+        mt = _type_of(m, "moments", (torch.float32, torch.float8_e4m3fn))
+        for p, n in zip(params, ns):
+            if p.numel() != n:
+                raise ValueError("a parameter of %d elements has a gradient of %d" % (p.numel(), n))
+    if copies is not None:
+        ct = _type_of(copies, "copies", (torch.bfloat16, torch.float16))
+    blocks = [(n + 255) // 256 for n in ns]
+    array = lambda ts, dtype, sizes: None if ts is None else _tensors(ts, dtype, sizes)  # noqa: E731
+    plan = _PlanStruct()
+    wp, wb = _ws(workspace)
+    _check("bagua_tensor_plan", _lib.bagua_tensor_plan(
+        _sizes(ns), T, _tensors(grads, gt, ns), _TYPES[gt], array(params, pt, ns), _TYPES.get(pt, 0), array(m, mt, ns), array(v, mt, ns),
+        0 if mt is None else 32 if mt is torch.float32 else 8, array(m_scales, torch.float32, blocks), array(v_scales, torch.float32, blocks),
+        array(copies, ct, ns), _TYPES.get(ct, 0), None if decay is None else (ctypes.c_float * T)(*[float(d) for d in decay]), wp, wb,
+        ctypes.addressof(plan), _stream(stream)))
+    return TensorPlan(plan, (list(grads), params, m, v, m_scales, v_scales, copies, workspace))
+
+
+def bagua_grad_norm(plan, out, max_norm=float("inf"), grad_scale=1.0, stream=None):
+    """out[0] = norm of all gradients (times grad_scale), out[1] = the factor that clips them (with grad_scale in it)."""
+    _check("bagua_grad_norm", _lib.bagua_grad_norm(plan._at, grad_scale, max_norm, _ptr(out, torch.float32, 8), _stream(stream)))
+
+
+def bagua_adamw_step(plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, clip=None, seed=0, stream=None):
+    """Step number `step` (from 1 on) of all tensors of the plan.  clip: what bagua_grad_norm has left; where the norm is not
+    finite nothing changes.  seed: a number of 32 bits, another one each step, for what is rounded stochastically."""
+    _check("bagua_adamw_step", _lib.bagua_adamw_step(plan._at, step, lr, beta1, beta2, eps, weight_decay, _ptr(clip, torch.float32, 8), seed,
+                                                     _stream(stream)))
+
+
+# ---------------------------------------------------------------------------------------------- balance loss
+def _matrices(tensors, dtypes, columns, rows=None):
+    """Type, common row stride and addresses of a list of 2-D GPU tensors whose rows are contiguous."""
+    dtype, ld = tensors[0].dtype, None
+    if dtype not in dtypes:
+        raise ValueError("expected one of %s, got %s" % (", ".join(str(d) for d in dtypes), dtype))
+    at = (ctypes.c_void_p * len(tensors))()
+    for i, t in enumerate(tensors):
+        if not t.is_cuda or t.dim() != 2 or t.shape[1] != columns or t.dtype is not dtype or (rows is not None and t.shape[0] != rows[i]):
+            raise ValueError("expected GPU tensors of %s rows and %d columns of %s" % ("the tokens'" if rows else "any", columns, dtype))
+        if t.shape[0] > 0 and columns > 1 and t.stride(1) != 1:
+            raise ValueError("the elements of a row must lie next to each other")
+        if t.shape[0] > 1:
+            if t.stride(0) < columns or (ld is not None and t.stride(0) != ld):
+                raise ValueError("the rows of all workers' tensors must lie equally far apart, and not overlap")
+            ld = t.stride(0)
+        at[i] = t.data_ptr() if t.shape[0] else None
+    return dtype, columns if ld is None else ld, at
+
+
+def _mask_array(mask, rows):
+    if mask is None:
+        return None
+    at = (ctypes.c_void_p * len(mask))()
+    for i, (t, n) in enumerate(zip(mask, rows)):
+        if t.dtype not in (torch.bool, torch.uint8):
+            raise ValueError("a mask must be bool or uint8, got %s" % t.dtype)
+        at[i] = _ptr(t, None, n) if n else None
+    return at
+
+
+def bagua_balance_workspace_bytes(experts):
+    """Bytes of workspace of bagua_balance_stats; it must be zero before the first call."""
+    return int(_lib.bagua_balance_workspace_bytes(experts))
+
+
+def bagua_balance_stats(logits, ids, mask, counts, prob, workspace, alpha=0.01, loss=None, weight=None, stream=None):
+    """Statistics of the k workers' tokens, and the loss with its derivative by the probability sums.  logits: k tensors [tokens,
+    experts]; ids: k tensors [tokens, top_k], int32 or int64; mask: k tensors [tokens] (0 = padding) or None."""
+    k = len(logits)
+    _same_len(k, ids=ids, mask=mask)
+    if k == 0 or logits[0].dim() != 2 or ids[0].dim() != 2:
+        raise ValueError("expected 2-D tensors of at least one worker")
+    rows = [x.shape[0] for x in logits]
+    experts, top = logits[0].shape[1], ids[0].shape[1]
+    dtype, ld, la = _matrices(logits, tuple(_TYPES), experts)
+    it, ids_ld, ia = _matrices(ids, (torch.int32, torch.int64), top, rows)
+    wp, wb = _ws(workspace)
+    _check("bagua_balance_stats", _lib.bagua_balance_stats(
+        _TYPES[dtype], la, ld, _sizes(rows), k, experts, ia, 4 if it is torch.int32 else 8, ids_ld, top, _mask_array(mask, rows),
+        _ptr(counts, torch.int32, 4 * (experts + 1)), _ptr(prob, torch.float32, 4 * experts), alpha, _ptr(loss, torch.float32, 4),
+        _ptr(weight, torch.float32, 4 * experts), wp, wb, _stream(stream)))
+
+
+def bagua_balance_loss(counts, prob, top_k, alpha, loss, weight, stream=None):
+    """Loss and weights from counts (experts + 1 of them) and prob that were added up over GPUs."""
+    experts = prob.numel()
+    _check("bagua_balance_loss", _lib.bagua_balance_loss(
+        _ptr(counts, torch.int32, 4 * (experts + 1)), _ptr(prob, torch.float32), experts, top_k, alpha, _ptr(loss, torch.float32, 4),
+        _ptr(weight, torch.float32, 4 * experts), _stream(stream)))
+
+
+def bagua_balance_grad(logits, mask, weight, upstream, dlogits, stream=None):
+    """Gradient of the balance loss by the k workers' logits; upstream: the gradient that arrives at the loss (fp32[1]) or None."""
+    k = len(logits)
+    _same_len(k, mask=mask, dlogits=dlogits)
+    if k == 0 or logits[0].dim() != 2:
+        raise ValueError("expected 2-D tensors of at least one worker")
+    rows = [x.shape[0] for x in logits]
+    experts = logits[0].shape[1]
+    dtype, ld, la = _matrices(logits, tuple(_TYPES), experts)
+    _, ld_out, oa = _matrices(dlogits, (dtype,), experts, rows)
+    _check("bagua_balance_grad", _lib.bagua_balance_grad(
+        _TYPES[dtype], la, ld, _sizes(rows), k, experts, _mask_array(mask, rows), _ptr(weight, torch.float32, 4 * experts),
+        _ptr(upstream, torch.float32, 4), oa, ld_out, _stream(stream)))
 
 
 # ---------------------------------------------------------------------------------------------- probes

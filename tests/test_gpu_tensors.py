@@ -1,0 +1,441 @@
+"""Global gradient norm and AdamW over many tensors: against the formulas in 64 bits with bounds from counting roundings, and bit for
+bit against the same operations in NumPy's fp32 (one rounding each), codes and stochastic rounding included."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24                                    # half a unit in the last place of fp32
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+F8 = torch.float8_e4m3fn
+# sizes of one plan: empty ones, single elements, around a block and a tile, several tiles
+LISTS = [[1], [0], [255, 256, 257], [0, 3, 1023, 1024, 1025, 0, 4099, 2], [70001], [5] * 300 + [12345]]
+HYPER = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.1)
+
+
+@pytest.fixture(scope="module")
+def bg():
+    import paper_2107_01499_amd as b
+    assert torch.cuda.is_available()
+    return b
+
+
+def placed(arrays, dtype, offset):
+    """Tensors on the GPU that begin `offset` elements behind an aligned address, each in a storage with a guard behind it."""
+    out = []
+    for a in arrays:
+        store = torch.full((a.size + offset + 64,), 7.0, device="cuda").to(dtype)
+        t = store[offset:offset + a.size]
+        t.copy_(torch.from_numpy(a).cuda())
+        t.guard = store
+        out.append(t)
+    return out
+
+
+def guards_intact(tensors, offset):
+    for t in tensors:
+        edge = torch.cat([t.guard[:offset].float(), t.guard[offset + t.numel():].float()])
+        assert bool((edge == 7.0).all())
+
+
+def blocks(n):
+    return (n + 255) // 256
+
+
+def plan_of(bg, ns, *args, **kw):
+    return bg.bagua_tensor_plan(*args[:1], torch.empty(bg.bagua_tensor_plan_bytes(ns), dtype=torch.uint8, device="cuda"), **kw)
+
+
+# ------------------------------------------------------------------------------------------------ norm
+@pytest.mark.parametrize("offset", [0, 1, 3])
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("ns", LISTS, ids=lambda ns: "%d tensors of %d" % (len(ns), sum(ns)))
+def test_norm(bg, ns, dtype, offset):
+    r = np.random.default_rng(sum(ns) + offset)
+    gs = placed([r.standard_normal(n).astype(np.float32) * np.float32(10.0 ** r.uniform(-3, 1)) for n in ns], TYPES[dtype], offset)
+    plan, out = plan_of(bg, ns, gs), torch.full((2,), 9.0, device="cuda")
+    want = math.sqrt(math.fsum(float(x) ** 2 for g in gs for x in g.double().cpu().numpy()))
+    for max_norm, scale in ((1.0, 1.0), (math.inf, 0.125), (1e9, 2.0), (0.0, 1.0)):
+        bg.bagua_grad_norm(plan, out, max_norm, scale)
+        n, c = out.cpu().tolist()
+        full = scale * want
+        assert abs(n - full) <= 2 * U * full
+        factor = scale * min(1.0, max_norm / (full + 1e-6))
+        assert abs(c - factor) <= 2 * U * factor
+        bits = out.clone()
+        bg.bagua_grad_norm(plan, out, max_norm, scale)
+        assert torch.equal(out, bits)
+
+
+def test_norm_of_extremes(bg):
+    out = torch.zeros(2, device="cuda")
+    for values, want in (([1e30] * 3 + [-3e38], 3e38 * math.sqrt(1 + 3 * (1e30 / 3e38) ** 2)), ([1e-30, 1e-44], 1e-30), ([0.0] * 5, 0.0)):
+        g = torch.tensor(values, device="cuda")
+        bg.bagua_grad_norm(plan_of(bg, [g.numel()], [g]), out, 1.0)
+        assert abs(float(out[0]) - want) <= 2 * U * want
+        assert abs(float(out[1]) - min(1.0, 1.0 / (want + 1e-6))) <= 2 * U
+    for bad in (math.inf, -math.inf, math.nan):
+        g = [torch.ones(5000, device="cuda") for _ in range(3)]
+        g[1][4321] = bad
+        bg.bagua_grad_norm(plan_of(bg, [5000] * 3, g), out, 1.0)
+        assert not math.isfinite(float(out[0])) and float(out[1]) == 0.0
+
+
+def test_norm_of_more_tiles_than_a_launch_has_waves(bg):
+    n = 9 * 1024 * 8192 + 5
+    g = torch.empty(n, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    out = torch.zeros(2, device="cuda")
+    bg.bagua_grad_norm(plan_of(bg, [n], [g]), out)
+    want = math.sqrt(float(g.double().square().sum()))
+    assert abs(float(out[0]) - want) <= 2 * U * want and float(out[1]) == 1.0
+
+
+# ------------------------------------------------------------------------------------------------ AdamW in NumPy
+GOLDEN, ROOT2, ROOT3 = np.uint32(0x9E3779B9), np.uint32(0x6A09E667), np.uint32(0xBB67AE85)
+VALUES = np.array([c * 2.0 ** -9 if c < 8 else (8 + c % 8) * 2.0 ** (c // 8 - 10) for c in range(127)])      # E4M3's magnitudes, by code
+
+
+def mix(x):
+    x = (x ^ (x >> np.uint32(16))) * ROOT2
+    x = (x ^ (x >> np.uint32(15))) * ROOT3
+    return x ^ (x >> np.uint32(16))
+
+
+def turned(h, i):
+    by = (8 * (i % 4)).astype(np.uint64)
+    h = h.astype(np.uint64)
+    return ((h << by | h >> (np.uint64(32) - by)) & np.uint64(0xFFFFFFFF)).astype(np.uint32)
+
+
+def hashes(n, tensor, seed):
+    i = np.arange(n, dtype=np.uint32)
+    with np.errstate(over="ignore"):
+        base = mix(np.array([tensor], dtype=np.uint32) * GOLDEN + np.uint32(seed))
+        h = mix((i // np.uint32(4)) * GOLDEN + base)
+        return turned(h, i), turned(mix(h + GOLDEN), i)
+
+
+def scales(x):
+    pad = np.zeros(blocks(x.size) * 256, np.float32)
+    pad[:x.size] = np.abs(x)
+    s = (pad.reshape(-1, 256).max(1) * np.float32(1.0 / 448.0)).astype(np.float32)
+    s = np.where(s >= np.float32(2.0 ** -126), s, np.float32(0))
+    with np.errstate(divide="ignore"):
+        return s, np.where(s > 0, np.float32(1.0) / s, np.float32(0)).astype(np.float32)
+
+
+def nearest_code(y):
+    a = np.abs(y.astype(np.float64))
+    hi = np.searchsorted(VALUES, a).clip(0, 126)
+    lo = (hi - 1).clip(0)
+    up = (VALUES[hi] - a < a - VALUES[lo]) | ((VALUES[hi] - a == a - VALUES[lo]) & (hi % 2 == 0))
+    return (np.where(up, hi, lo) + np.where(np.signbit(y), 128, 0)).astype(np.uint8)
+
+
+def decode(codes, scale):
+    c = codes.astype(np.int64)
+    return (np.where(c >= 128, -1.0, 1.0) * VALUES[c % 128]).astype(np.float32) * np.repeat(scale, 256)[:c.size]
+
+
+def step_in_fp32(p, g, m, v, t, clip, decay, lr, beta1, beta2, eps, weight_decay):
+    """m, v: fp32 moments (v itself).  One rounding per operation."""
+    f = np.float32
+    if clip is not None:
+        g = g * f(clip)
+    m = m * f(beta1) + g * f(1.0 - beta1)
+    v = v * f(beta2) + (g * g) * f(1.0 - beta2)
+    r = np.sqrt(v)
+    u = m / (r * f(1.0 / math.sqrt(1.0 - beta2 ** t)) + f(eps))
+    return p - (u * f(lr / (1.0 - beta1 ** t)) + p * (f(decay) * f(lr * weight_decay))), m, v, r
+
+
+def step_in_64(p, g, m, v, t, clip, decay, lr, beta1, beta2, eps, weight_decay):
+    """The step and how far fp32 may be off: every rounding moves its result by at most U of itself."""
+    p, g, m, v = (x.astype(np.float64) for x in (p, g, m, v))
+    g = g * (1.0 if clip is None else float(clip))
+    a, b = beta1 * m, (1 - beta1) * g
+    m2, dm = a + b, 4 * U * (np.abs(a) + np.abs(b))               # factor, product (and the clipped gradient), sum
+    v2 = beta2 * v + (1 - beta2) * g * g
+    dv = 6 * U * v2 + 2.0 ** -148                                  # factor, clipped gradient twice, square, product, sum; below the smallest numbers
+    den = np.sqrt(v2 / (1 - beta2 ** t)) + eps
+    u = (m2 / (1 - beta1 ** t)) / den
+    dr = np.sqrt(v2 + dv) - np.sqrt(np.maximum(v2 - dv, 0)) + U * np.sqrt(v2)
+    du = (np.abs(u) * (dr / math.sqrt(1 - beta2 ** t) + 5 * U * den) + dm / (1 - beta1 ** t)) / (den - dr / math.sqrt(1 - beta2 ** t)).clip(eps)
+    p2 = p - lr * (u + weight_decay * decay * p)
+    dp = lr * (du + 4 * U * np.abs(u)) + 5 * U * lr * weight_decay * np.abs(decay * p) + U * (np.abs(p2) + lr * np.abs(u + weight_decay * decay * p))
+    return p2, m2, v2, 1.1 * dp, 1.1 * dm, 1.1 * dv
+
+
+def bf16(x):
+    """An fp32 array rounded to nearest bf16, as fp32."""
+    return torch.from_numpy(np.ascontiguousarray(x)).to(torch.bfloat16).float().numpy()
+
+
+FORMS = [("f32", "f32", None), ("bf16", "f32", None), ("f16", "f32", None), ("f32", "f32", "bf16"), ("bf16", "f32", "bf16"), ("f16", "f32", "f16"),
+         ("bf16", "f32", "f16"), ("f32", "f32", "f16"), ("f16", "f32", "bf16"), ("bf16", "bf16", None), ("f32", "bf16", None)]
+
+
+@pytest.mark.parametrize("ns,offset", [(LISTS[0], 1), (LISTS[1], 0), (LISTS[2], 0), (LISTS[3], 1), (LISTS[3], 3), (LISTS[4], 0), (LISTS[5], 1)],
+                         ids=lambda x: str(x) if isinstance(x, int) else "%d tensors of %d" % (len(x), sum(x)))
+@pytest.mark.parametrize("grad,param,copy", FORMS)
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw(bg, ns, offset, grad, param, copy, bits):
+    print("adamw bits=%d %s %s %s %d tensors of %d offset %d" % (bits, grad, param, copy, len(ns), sum(ns), offset), flush=True)
+    r = np.random.default_rng(sum(ns) * 3 + bits)
+    decay = [0.0 if i % 3 == 1 else 1.0 if i % 3 else 0.5 for i in range(len(ns))]
+    P = [(r.standard_normal(n) * 0.02).astype(np.float32) for n in ns]
+    if param == "bf16":
+        P = [bf16(p) for p in P]
+    gp, gg = placed(P, TYPES[param], offset), placed([np.zeros(n, np.float32) for n in ns], TYPES[grad], offset)
+    state = torch.float32 if bits == 32 else F8
+    gm, gv = (placed([np.zeros(n, np.float32) for n in ns], state, offset) for _ in range(2))
+    more = {}
+    if bits == 8:
+        gms, gvs = (placed([np.zeros(blocks(n), np.float32) for n in ns], torch.float32, offset) for _ in range(2))
+        more.update(m_scales=gms, v_scales=gvs)
+    if copy:
+        gc = placed(P, TYPES[copy], offset)
+        more.update(copies=gc)
+    plan = plan_of(bg, ns, gg, params=gp, m=gm, v=gv, decay=decay, **more)
+    M, V = [np.zeros(n, np.float32) for n in ns], [np.zeros(n, np.float32) for n in ns]
+    for t in (1, 2, 3):
+        clip = None if t == 2 else 0.37 * t
+        dclip = None if clip is None else torch.tensor([5.0, clip], device="cuda")
+        for g in gg:
+            # gradients over many orders of magnitude, exact zeros among them
+            x = (r.standard_t(2, g.numel()) * 10.0 ** r.uniform(-6, -2, g.numel())).astype(np.float32)
+            x[::7] = 0.0
+            g.copy_(torch.from_numpy(x).cuda())
+        seed = 4000000000 + t
+        bg.bagua_adamw_step(plan, t, clip=dclip, seed=seed, **HYPER)
+        for i, n in enumerate(ns):
+            if n == 0:
+                continue
+            g = gg[i].float().cpu().numpy()
+            before = P[i], M[i], V[i]
+            p, m, v, root = step_in_fp32(P[i], g, M[i], V[i], t, None if clip is None else np.float32(clip), decay[i], **HYPER)
+            p64, m64, v64, dp, dm, dv = step_in_64(*before[:1], g, *before[1:], t, None if clip is None else np.float32(clip), decay[i], **HYPER)
+            h, h2 = hashes(n, i, seed)
+            if bits == 32:
+                got_m, got_v = gm[i].cpu().numpy(), gv[i].cpu().numpy()
+                assert np.all(np.abs(got_m - m64) <= dm) and np.all(np.abs(got_v - v64) <= dv)
+                assert np.array_equal(got_m.view(np.uint32), m.view(np.uint32)) and np.array_equal(got_v.view(np.uint32), v.view(np.uint32))
+                M[i], V[i] = m, v
+            else:
+                s, inv = scales(m)
+                codes = nearest_code(m * np.repeat(inv, 256)[:n])
+                got = gm[i].view(torch.uint8).cpu().numpy()
+                assert np.array_equal(gms[i].cpu().numpy(), s) and np.array_equal(got & 127, codes & 127)
+                assert np.array_equal((got >= 128)[codes % 128 != 0], (codes >= 128)[codes % 128 != 0])
+                # the stored value is one of the two next to the exact one, the nearer one at that
+                M[i] = decode(got, s)
+                y = np.abs(m64) / np.repeat(np.where(s > 0, s, np.inf), 256)[:n]
+                near = np.abs(VALUES[:, None] - y[None, :4096]).min(0)
+                assert np.all(np.abs(VALUES[got[:4096] & 127] - y[:4096]) <= near + 8 * U * 448)
+                s, inv = scales(root)
+                y = root * np.repeat(inv, 256)[:n]
+                c = ((y * np.float32(2.0 ** -120)).view(np.uint32) + (h >> np.uint32(12))) >> np.uint32(20)
+                c = np.where(root > 0, c.clip(1, 126), 0).astype(np.uint8)
+                got = gv[i].view(torch.uint8).cpu().numpy()
+                assert np.array_equal(gvs[i].cpu().numpy(), s) and np.array_equal(got, c)
+                low = np.searchsorted(VALUES, y.astype(np.float64) * (1 - 4 * U), side="right") - 1
+                assert np.all((got >= low) & (got <= np.maximum(low + 1, 1)) | (got == 126))
+                V[i] = decode(got, s) ** 2
+            got_p = gp[i].float().cpu().numpy()
+            if param == "bf16":
+                want = ((p.view(np.uint32).astype(np.uint64) + (h2 >> np.uint32(16))) >> np.uint64(16)).astype(np.uint32) << np.uint32(16)
+                assert np.array_equal(got_p.view(np.uint32), want)
+                assert np.all(np.abs(got_p - p64) <= dp + np.maximum(np.abs(p64), 2.0 ** -126) * 2.0 ** -7)
+            else:
+                assert np.all(np.abs(got_p - p64) <= dp)
+                assert np.array_equal(got_p.view(np.uint32), p.view(np.uint32))
+            if copy:
+                assert torch.equal(gc[i], gp[i].to(TYPES[copy]))
+            P[i] = got_p
+    for ts in (gp, gg, gm, gv) + ((gms, gvs) if bits == 8 else ()) + ((gc,) if copy else ()):
+        guards_intact(ts, offset)
+
+
+def test_many_steps_follow_torch(bg):
+    """The same fifty steps as torch's own AdamW in 64 bits."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    ps = [torch.randn(n, device="cuda", generator=g) * 0.1 for n in (1000, 257, 3)]
+    ref = [p.double().clone().requires_grad_() for p in ps]
+    opt = torch.optim.AdamW([dict(params=ref[:1], weight_decay=0.1), dict(params=ref[1:], weight_decay=0.0)], lr=1e-2, betas=(0.9, 0.999), eps=1e-8, foreach=False)
+    gs, ms, vs = ([torch.zeros_like(p) for p in ps] for _ in range(3))
+    plan = plan_of(bg, [p.numel() for p in ps], gs, params=ps, m=ms, v=vs, decay=[1, 0, 0])
+    for t in range(1, 51):
+        for x, p in zip(gs, ref):
+            x.copy_(torch.randn(x.shape, device="cuda", generator=g))
+            p.grad = x.double()
+        opt.step()
+        bg.bagua_adamw_step(plan, t, 1e-2, weight_decay=0.1)
+    for p, q in zip(ps, ref):
+        # each step adds at most 1.1 * lr * 12 U and an U of |p|
+        assert float((p.double() - q.detach()).abs().max()) <= 50 * (1.1 * 1e-2 * 20 * U * 4 + 2 * U)
+
+
+def test_stochastic_rounding_is_unbiased(bg):
+    """The mean over many seeds of what is stored is the value that was rounded."""
+    n, seeds = 256, 4096
+    x = torch.linspace(0.3, 1.0, n, device="cuda")
+    total, root = torch.zeros(n, device="cuda", dtype=torch.float64), None
+    p_total = torch.zeros(n, device="cuda", dtype=torch.float64)
+    ws = torch.empty(bg.bagua_tensor_plan_bytes([n]), dtype=torch.uint8, device="cuda")
+    p0 = torch.linspace(1.0, 2.0, n, device="cuda").to(torch.bfloat16)
+    p, m, v = p0.clone(), torch.zeros(n, device="cuda").to(F8), torch.zeros(n, device="cuda").to(F8)
+    ms, vs = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    plan = bg.bagua_tensor_plan([x], ws, params=[p], m=[m], v=[v], m_scales=[ms], v_scales=[vs])
+    for s in range(seeds):
+        p.copy_(p0)
+        for z in (m, v):
+            z.view(torch.uint8).zero_()
+        ms.zero_()
+        vs.zero_()
+        bg.bagua_adamw_step(plan, 1, 1e-3, 0.9, 0.999, 1e-8, 0.0, seed=s)
+        total += v.double() * vs.double()
+        p_total += p.double()
+    root = x.double() * math.sqrt(0.001)
+    # a value between two codes is off by a step at most, which is an eighth of it: six standard deviations of the mean
+    assert float(((total / seeds - root).abs() / root).max()) <= 6 * (0.125 / 2) / math.sqrt(seeds) + 1e-6
+    want = p0.double() - 1e-3          # the first step moves every parameter by lr
+    assert float((p_total / seeds - want).abs().max()) <= 6 * (2.0 ** -7 / 2) / math.sqrt(seeds) + 2.0 ** -22
+
+
+def test_a_norm_that_is_not_finite_changes_nothing(bg):
+    for bits in (32, 8):
+        n = 3000
+        p, g = torch.ones(n, device="cuda"), torch.ones(n, device="cuda")
+        m, v = (torch.ones(n, device="cuda").to(torch.float32 if bits == 32 else F8) for _ in range(2))
+        more = {} if bits == 32 else dict(m_scales=[torch.ones(12, device="cuda")], v_scales=[torch.ones(12, device="cuda")])
+        plan = plan_of(bg, [n], [g], params=[p], m=[m], v=[v], **more)
+        clip = torch.zeros(2, device="cuda")
+        before = [t.clone() for t in (p, m, v)] + [t.clone() for ts in more.values() for t in ts]
+        for bad in (math.inf, math.nan):
+            g[1234] = bad
+            bg.bagua_grad_norm(plan, clip, 1.0)
+            bg.bagua_adamw_step(plan, 1, 1e-2, clip=clip)
+            for a, b in zip(before, [p, m, v] + [t for ts in more.values() for t in ts]):
+                assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+        g[1234] = 1.0
+        bg.bagua_grad_norm(plan, clip, 1.0)
+        bg.bagua_adamw_step(plan, 1, 1e-2, clip=clip)
+        assert not torch.equal(before[0], p)
+
+
+def test_tiny_and_huge_blocks_in_8_bits(bg):
+    """Blocks whose first moment is below what a scale can hold are stored as 0; a root above zero never becomes zero."""
+    n = 1024
+    g = torch.zeros(n, device="cuda")
+    g[:256] = 1e-38
+    g[256:512] = 3e18
+    g[512] = 1.0
+    g[513:768] = 1e-12
+    p, m, v = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda").to(F8), torch.zeros(n, device="cuda").to(F8)
+    ms, vs = torch.zeros(4, device="cuda"), torch.zeros(4, device="cuda")
+    bg.bagua_adamw_step(plan_of(bg, [n], [g], params=[p], m=[m], v=[v], m_scales=[ms], v_scales=[vs]), 1, 1e-3, seed=1)
+    assert float(ms[0]) == 0.0 and int(m.view(torch.uint8)[:256].max()) == 0
+    assert bool((m.view(torch.uint8)[256:512] == 126).all()) and math.isfinite(float(vs[1]))
+    assert int(v.view(torch.uint8)[513:768].min()) == 1 and int(v.view(torch.uint8)[512]) == 126
+    assert int(v.view(torch.uint8)[768:].max()) == 0 and float(vs[3]) == 0.0 and bool((p[768:] == 0).all())
+    assert bool(torch.isfinite(p).all())
+
+
+def test_beyond_32_bits(bg):
+    """One tensor of more than 2^32 elements: what is updated at its end, and the norm."""
+    n = (1 << 32) + 777
+    p = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda").view(F8) for _ in range(2))
+    ms, vs = torch.zeros(blocks(n), device="cuda"), torch.zeros(blocks(n), device="cuda")
+    spots = [0, 1 << 31, (1 << 32) - 1, 1 << 32, n - 1]
+    for i, s in enumerate(spots):
+        g[s] = 2.0 ** i
+    plan = plan_of(bg, [n], [g], params=[p], m=[m], v=[v], m_scales=[ms], v_scales=[vs])
+    out = torch.zeros(2, device="cuda")
+    bg.bagua_grad_norm(plan, out)
+    assert abs(float(out[0]) - math.sqrt(sum(4.0 ** i for i in range(5)))) <= 4 * U * 20
+    bg.bagua_adamw_step(plan, 1, 0.5, 0.9, 0.999, 0.0, 0.0, seed=3)   # eps 0: 0 / 0 where there is no gradient
+    for i, s in enumerate(spots):
+        assert abs(float(p[s]) + 0.5) <= 2.0 ** -8 and float(m[s].float()) == 448.0 and float(v[s].float()) == 448.0
+        assert abs(float(ms[s // 256]) - 0.1 * 2.0 ** i / 448) <= 8 * U * 2.0 ** i / 448
+    assert int((m.view(torch.uint8) != 0).sum()) == 5
+
+
+def test_streams_and_graphs(bg):
+    """On a stream of its own, and recorded: every replay is another step on the same state, as the eager calls make it."""
+    ns = [3000, 1, 70000]
+    def fresh():
+        r = torch.Generator(device="cuda").manual_seed(9)
+        ps, gs = ([torch.randn(n, device="cuda", generator=r) for n in ns] for _ in range(2))
+        ms, vs = ([torch.zeros_like(p) for p in ps] for _ in range(2))
+        return ps, ms, vs, torch.zeros(2, device="cuda"), plan_of(bg, ns, gs, params=ps, m=ms, v=vs), gs
+    a, b = fresh(), fresh()
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        bg.bagua_grad_norm(b[4], b[3], 1.0)
+        bg.bagua_adamw_step(b[4], 7, 1e-2, weight_decay=0.1, clip=b[3], seed=5)
+    for _ in range(4):
+        bg.bagua_grad_norm(a[4], a[3], 1.0)
+        bg.bagua_adamw_step(a[4], 7, 1e-2, weight_decay=0.1, clip=a[3], seed=5)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(a[0] + a[1] + a[2] + [a[3]], b[0] + b[1] + b[2] + [b[3]]):
+            assert torch.equal(x, y)
+        for x, y in zip(a[5], b[5]):
+            x.mul_(1.5)
+            y.mul_(1.5)
+    bg.bagua_adamw_step(a[4], 8, 1e-2, stream=s)
+    s.synchronize()
+    bg.bagua_adamw_step(b[4], 8, 1e-2)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(a[0], b[0]))
+
+
+def test_refusals(bg):
+    n = 100
+    f = lambda dtype=torch.float32, n=n: torch.zeros(n, device="cuda").to(dtype)  # noqa: E731
+    ws = torch.empty(bg.bagua_tensor_plan_bytes([n]), dtype=torch.uint8, device="cuda")
+    ok = dict(params=[f()], m=[f()], v=[f()])
+    for what, grads, more in (
+            ("at least one", [], {}), ("go together", [f()], dict(params=[f()])), ("gradients must be", [f(torch.float64)], {}),
+            ("parameters must be", [f()], dict(ok, params=[f(torch.float16)])), ("moments must be", [f()], dict(ok, m=[f(torch.bfloat16)])),
+            ("expected dtype", [f()], dict(ok, v=[f(torch.bfloat16)])), ("copies must be", [f()], dict(ok, copies=[f()])),
+            ("one per worker", [f()], dict(ok, m=[f(), f()])), ("has a gradient of", [f()], dict(ok, params=[f(n=99)])),
+            ("too small", [f()], dict(ok, m=[f(n=99)])), ("contiguous GPU tensor", [torch.zeros(n)], {}),
+            ("contiguous GPU tensor", [torch.zeros(2 * n, device="cuda")[::2]], {})):
+        with pytest.raises(ValueError, match=what):
+            bg.bagua_tensor_plan(grads, ws, **more)
+    for grads, more, status in (
+            ([f()], dict(params=[f()], m=[f(F8)], v=[f(F8)]), "INVALID"),                                   # no scales
+            ([f()], dict(ok, m_scales=[f()], v_scales=[f()]), "INVALID"),                                   # scales without codes
+            ([f(torch.float16)], dict(ok, params=[f(torch.bfloat16)]), "INVALID"),
+            ([f()], dict(ok, params=[f(torch.bfloat16)], copies=[f(torch.bfloat16)]), "INVALID"),
+            ([f()], dict(ok, decay=[math.nan]), "INVALID")):
+        with pytest.raises(bg.BaguaError, match=status):
+            bg.bagua_tensor_plan(grads, ws, **more)
+    x = f()
+    with pytest.raises(bg.BaguaError, match="INVALID"):
+        bg.bagua_tensor_plan([x], ws, params=[x], m=[f()], v=[f()])                                         # in-out over read
+    with pytest.raises(bg.BaguaError, match="INVALID"):
+        bg.bagua_tensor_plan([f()], ws[:64], **ok)
+    plan = bg.bagua_tensor_plan([f()], ws)
+    with pytest.raises(bg.BaguaError, match="INVALID"):
+        bg.bagua_adamw_step(plan, 1, 1e-3)                                                                  # a plan for the norm alone
+    with pytest.raises(ValueError, match="too small"):
+        bg.bagua_grad_norm(plan, f(n=1))
+    for kw in (dict(max_norm=math.nan), dict(max_norm=-1.0), dict(grad_scale=math.inf)):
+        with pytest.raises(bg.BaguaError, match="INVALID"):
+            bg.bagua_grad_norm(plan, f(n=2), **kw)
+    plan = bg.bagua_tensor_plan([f()], ws, **ok)
+    for bad in (dict(step=0), dict(lr=math.inf), dict(beta1=1.0), dict(beta2=-0.1), dict(eps=-1e-8), dict(weight_decay=math.nan)):
+        with pytest.raises(bg.BaguaError, match="INVALID"):
+            bg.bagua_adamw_step(plan, **dict(dict(step=1, lr=1e-3), **bad))
+    torch.cuda.synchronize()
+    assert bool((ok["params"][0] == 0).all())
