@@ -656,12 +656,16 @@ def bagua_tensor_plan(grads, workspace, params=None, m=None, v=None, m_scales=No
 
 def bagua_grad_norm(plan, out, max_norm=float("inf"), grad_scale=1.0, stream=None):
     """out[0] = norm of all gradients (times grad_scale), out[1] = the factor that clips them (with grad_scale in it)."""
+    if _native.grad_norm(plan._at, out, max_norm, grad_scale, stream):
+        return
     _check("bagua_grad_norm", _lib.bagua_grad_norm(plan._at, grad_scale, max_norm, _ptr(out, torch.float32, 8), _stream(stream)))
 
 
 def bagua_adamw_step(plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, clip=None, seed=0, stream=None):
     """Step number `step` (from 1 on) of all tensors of the plan.  clip: what bagua_grad_norm has left; where the norm is not
     finite nothing changes.  seed: a number of 32 bits, another one each step, for what is rounded stochastically."""
+    if _native.adamw_step(plan._at, step, lr, beta1, beta2, eps, weight_decay, clip, seed, stream):
+        return
     _check("bagua_adamw_step", _lib.bagua_adamw_step(plan._at, step, lr, beta1, beta2, eps, weight_decay, _ptr(clip, torch.float32, 8), seed,
                                                      _stream(stream)))
 
@@ -705,6 +709,8 @@ def bagua_balance_workspace_bytes(experts):
 def bagua_balance_stats(logits, ids, mask, counts, prob, workspace, alpha=0.01, loss=None, weight=None, stream=None):
     """Statistics of the k workers' tokens, and the loss with its derivative by the probability sums.  logits: k tensors [tokens,
     experts]; ids: k tensors [tokens, top_k], int32 or int64; mask: k tensors [tokens] (0 = padding) or None."""
+    if _native.balance_stats(logits, ids, mask, counts, prob, workspace, alpha, loss, weight, stream):
+        return
     k = len(logits)
     _same_len(k, ids=ids, mask=mask)
     if k == 0 or logits[0].dim() != 2 or ids[0].dim() != 2:
@@ -730,6 +736,8 @@ def bagua_balance_loss(counts, prob, top_k, alpha, loss, weight, stream=None):
 
 def bagua_balance_grad(logits, mask, weight, upstream, dlogits, stream=None):
     """Gradient of the balance loss by the k workers' logits; upstream: the gradient that arrives at the loss (fp32[1]) or None."""
+    if _native.balance_grad(logits, mask, weight, upstream, dlogits, stream):
+        return
     k = len(logits)
     _same_len(k, mask=mask, dlogits=dlogits)
     if k == 0 or logits[0].dim() != 2:

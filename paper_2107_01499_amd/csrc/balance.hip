@@ -6,15 +6,16 @@
 // store the same bits.
 #include <cmath>
 
+#include "batch.hpp"
 #include "elements.hpp"
 
 #pragma clang fp contract(off)
 
 namespace bagua {
 
-constexpr int kBalanceWaves = 16;            // of a workgroup of the forward pass
 constexpr unsigned kBalanceGroups = kCus;    // most workgroups of the forward pass: the last one adds up their sums
 constexpr int kGradWaves = 4;
+constexpr uint32_t kGradMostWaves = 65536;   // of a launch of the backward pass
 
 struct Workers {
     const void* logits[BAGUA_MAX_WORKERS];
@@ -51,6 +52,26 @@ __device__ __forceinline__ float lanes_reduce(float v, const F& op)
     if (L >= 64) {
         const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
         v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    return v;
+}
+
+constexpr int kRor1 = 0x121, kRor2 = 0x122, kRor4 = 0x124, kRor8 = 0x128;   // lane l reads l + 1, ... of its row of 16, around its end
+// The sum over the lanes that hold the same elements of different rows: l, l + L, l + 2 L, ...
+template <int L>
+__device__ __forceinline__ float rows_sum(float v)
+{
+    if (L <= 8) v = v + dpp<kRor8>(v);
+    if (L <= 4) v = v + dpp<kRor4>(v);
+    if (L <= 2) v = v + dpp<kRor2>(v);
+    if (L <= 1) v = v + dpp<kRor1>(v);
+    if (L <= 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (L <= 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
     }
     return v;
 }
@@ -119,22 +140,57 @@ struct Row {
     }
 };
 
-// The token of a lane's row in unit `unit` (wave-uniform): of worker w, its index there, and whether it is one that counts.
-struct Token {
-    uint32_t w, t;
-    bool exists, counts;
+// The workers' table with worker i in lane i: which worker has a unit is one comparison and a count of bits, and what belongs to it
+// is read from its lane.  (From the arguments that is a chain of scalar loads, a new one for every worker that is passed over.)
+struct LaneTable {
+    uint32_t first_unit, tokens;
+    uint64_t logits, other, mask;
+    __device__ __forceinline__ explicit LaneTable(const Workers& ws)
+    {
+        const uint32_t i = threadIdx.x & (BAGUA_MAX_WORKERS - 1);
+        first_unit = ws.first_unit[i];
+        tokens = ws.tokens[i];
+        logits = reinterpret_cast<uintptr_t>(ws.logits[i]);
+        other = reinterpret_cast<uintptr_t>(ws.ids[i]);
+        mask = reinterpret_cast<uintptr_t>(ws.mask[i]);
+    }
+    static __device__ __forceinline__ uint32_t of(uint32_t v, uint32_t w) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), static_cast<int>(w))); }
+    static __device__ __forceinline__ uint64_t of(uint64_t v, uint32_t w)
+    {
+        return static_cast<uint64_t>(of(static_cast<uint32_t>(v >> 32), w)) << 32 | of(static_cast<uint32_t>(v), w);
+    }
+    // The last worker whose units begin at `unit` or before it (of workers without tokens, which begin there too, the one behind them).
+    __device__ __forceinline__ uint32_t worker(uint32_t unit) const
+    {
+        return static_cast<uint32_t>(__popc(static_cast<uint32_t>(__ballot(first_unit <= unit)))) - 1u;
+    }
+};
+static_assert(BAGUA_MAX_WORKERS == 32, "a worker for each lane of half a wave");
+
+// A unit's rows: of one worker, from token t0 on.
+struct Unit {
+    uint64_t logits, other;
+    const uint8_t* flag;       // of the lane's own row; where there is no mask, or no such row, some other address that can be read
+    uint32_t t0, t, rows;      // t: the token of the lane's own row;  rows: that exist (one at least)
+    bool exists, masked;
 };
 template <int ROWS, int L>
-__device__ __forceinline__ Token token_of(const Workers& ws, uint32_t unit, uint32_t units)
+__device__ __forceinline__ Unit unit_of(const LaneTable& table, uint32_t unit, uint32_t units)
 {
-    Token k{0, 0, unit < units, false};
-    if (!k.exists) return k;
-    while (ws.first_unit[k.w + 1] <= unit) ++k.w;     // first_unit[k] = units
-    k.t = (unit - ws.first_unit[k.w]) * ROWS + (threadIdx.x & 63) / L;
-    k.exists = k.t < ws.tokens[k.w];
-    const uint8_t* mask = ws.mask[k.w];
-    k.counts = k.exists && (!mask || mask[k.t] != 0);
-    return k;
+    const bool there = unit < units;
+    unit = there ? unit : units - 1;
+    const uint32_t w = table.worker(unit), row = (threadIdx.x & 63) / L;
+    Unit u;
+    u.t0 = (unit - LaneTable::of(table.first_unit, w)) * ROWS;
+    u.rows = min(static_cast<uint32_t>(ROWS), LaneTable::of(table.tokens, w) - u.t0);
+    u.logits = LaneTable::of(table.logits, w);
+    u.other = LaneTable::of(table.other, w);
+    u.t = u.t0 + min(row, u.rows - 1);
+    u.exists = there && row < u.rows;
+    const uint64_t mask = LaneTable::of(table.mask, w);
+    u.masked = mask != 0;
+    u.flag = mask ? table_ptr<const uint8_t>(mask) + u.t : table_ptr<const uint8_t>(u.logits);
+    return u;
 }
 
 struct BalanceOut {
@@ -165,20 +221,30 @@ __device__ __forceinline__ void balance_loss(const BalanceOut& o, int32_t tokens
     o.loss[0] = static_cast<float>(sum);
 }
 
-// The forward pass.  Dynamic LDS: float sums[experts], then uint32 counters[(experts + 1) << lg]: 2^lg copies of each, one of which a
-// lane adds to, so that popular experts are not waited for.  Workspace: counter (64 bytes), then every workgroup's sums and counts.
-template <int TYPE, int VEC, int L, int NV, int UNROLL>
-__global__ void __launch_bounds__(kWave * kBalanceWaves)
+constexpr int kSumFloats = 8192;   // of LDS for the waves' sums
+// Rows of `experts` sums that fit there, of as many waves at a time.
+__host__ __device__ constexpr int sum_rows(int waves, int experts)
+{
+    int rows = waves;
+    while (rows > 1 && rows * experts > kSumFloats) rows /= 2;
+    return rows;
+}
+
+// The forward pass.  Dynamic LDS: float sums[sum_rows][experts], then uint32 counters[(experts + 1) << lg]: 2^lg copies of each, one of
+// which a lane adds to, so that popular experts are not waited for.  Workspace: counter (64 bytes), then every workgroup's sums and counts.
+template <int TYPE, int VEC, int L, int NV, int UNROLL, int WAVES>
+__global__ void __launch_bounds__(kWave * WAVES)
 k_balance_stats(Workers ws, size_t ld, size_t ids_ld, int id_bytes, uint32_t units, uint32_t per_k, int lg, uint32_t* workspace, BalanceOut o)
 {
     typedef Row<TYPE, VEC, L, NV> R;
+    constexpr int kThreads = kWave * WAVES;
     extern __shared__ float sums[];
-    __shared__ double part[kBalanceWaves];
+    __shared__ double part[WAVES];
     __shared__ bool last;
-    const int experts = o.experts, lane = threadIdx.x & 63, wave = wave_index();
-    uint32_t* counters = reinterpret_cast<uint32_t*>(sums + experts);
-    for (int i = threadIdx.x; i < (experts + 1) << lg; i += kWave * kBalanceWaves) counters[i] = 0;
-    for (int i = threadIdx.x; i < experts; i += kWave * kBalanceWaves) sums[i] = 0.0f;
+    const int experts = o.experts, lane = threadIdx.x & 63, wave = wave_index(), rows_of_sums = sum_rows(WAVES, experts);
+    uint32_t* counters = reinterpret_cast<uint32_t*>(sums + rows_of_sums * experts);
+    const LaneTable table(ws);
+    for (int i = threadIdx.x; i < (experts + 1) << lg; i += kThreads) counters[i] = 0;
     __syncthreads();
 
     float own[NV][VEC], acc[NV][VEC];
@@ -187,119 +253,152 @@ k_balance_stats(Workers ws, size_t ld, size_t ids_ld, int id_bytes, uint32_t uni
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) acc[j][i] = 0.0f;
-    const uint32_t waves = gridDim.x * kBalanceWaves;
+    const uint32_t waves = gridDim.x * WAVES, top = static_cast<uint32_t>(o.top_k);
     uint32_t tokens = 0;
-    for (uint32_t unit = blockIdx.x * kBalanceWaves + wave; unit < units; unit += UNROLL * waves) {
-        Token k[UNROLL];
+    for (uint32_t unit = blockIdx.x * WAVES + wave; unit < units; unit += UNROLL * waves) {
+        // All loads of the units are in flight together, and none stands behind a test: the rows' flags and the first 64 choices, then
+        // the rows.
+        Unit k[UNROLL];
         R row[UNROLL];
+        uint8_t flag[UNROLL];
+        uint64_t id[UNROLL];
+        bool counts[UNROLL];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) k[u] = token_of<R::kRows, L>(ws, unit + u * waves, units);
+        for (int u = 0; u < UNROLL; ++u) k[u] = unit_of<R::kRows, L>(table, unit + u * waves, units);
+        auto choice = [&](const Unit& n, uint32_t i) {      // choice i of the unit, of its row i / top; beyond the last one: the last
+            i = min(i, n.rows * top - 1);
+            const uint32_t r = per_k ? __umulhi(i, per_k) : i;
+            const size_t at = (n.t0 + r) * ids_ld + (i - r * top);
+            return id_bytes == 8 ? table_ptr<const uint64_t>(n.other)[at]
+                                 : static_cast<uint64_t>(static_cast<int64_t>(table_ptr<const int32_t>(n.other)[at]));
+        };
+        auto count = [&](uint64_t who, uint64_t rows, uint32_t i) {     // rows: bit L * r is set where row r counts
+            const uint32_t r = per_k ? __umulhi(i, per_k) : i;
+            if (who < static_cast<uint64_t>(experts) && r < R::kRows && (rows >> ((r * L) & 63) & 1))
+                atomicAdd(counters + (static_cast<uint32_t>(who) << lg) + (lane & ((1 << lg) - 1)), 1u);
+        };
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u)
-            row[u].load(static_cast<const typename R::one*>(ws.logits[k[u].w]) + k[u].t * ld, experts, k[u].counts);
+        for (int u = 0; u < UNROLL; ++u) flag[u] = *k[u].flag;
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) id[u] = choice(k[u], static_cast<uint32_t>(lane));
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) counts[u] = k[u].exists && (!k[u].masked || flag[u] != 0);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) row[u].load(table_ptr<const typename R::one>(k[u].logits) + k[u].t * ld, experts, counts[u]);
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
+            const uint64_t counting = __ballot(counts[u]);
+            tokens += __popcll(counting) / L;
+            count(id[u], counting, static_cast<uint32_t>(lane));
+            for (uint32_t i = kWave + lane; i < k[u].rows * top; i += kWave) count(choice(k[u], i), counting, i);
             float e[NV][VEC];
             float inverse = row[u].exponentials(own, e);
-            inverse = k[u].counts ? inverse : 0.0f;         // (rows that do not count were read as zeros)
-            tokens += __popcll(__ballot(k[u].counts && lane % L == 0));
+            inverse = counts[u] ? inverse : 0.0f;         // (rows that do not count were read as zeros)
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) acc[j][i] = __builtin_fmaf(e[j][i], inverse, acc[j][i]);
         }
     }
-
-    // the choices: one per thread, worker after worker
-    for (uint32_t w = 0; w < ws.k; ++w) {
-        const uint32_t choices = ws.tokens[w] * static_cast<uint32_t>(o.top_k);
-        for (uint32_t i = blockIdx.x * (kWave * kBalanceWaves) + threadIdx.x; i < choices; i += gridDim.x * (kWave * kBalanceWaves)) {
-            uint32_t t = per_k ? __umulhi(i, per_k) : i;       // i / top_k, or one more (below 2^31)
-            if (t * static_cast<uint32_t>(o.top_k) > i) --t;
-            if (ws.mask[w] && ws.mask[w][t] == 0) continue;
-            const size_t at = t * ids_ld + (i - t * static_cast<uint32_t>(o.top_k));
-            const int64_t id = id_bytes == 8 ? static_cast<const int64_t*>(ws.ids[w])[at] : static_cast<const int32_t*>(ws.ids[w])[at];
-            if (static_cast<uint64_t>(id) < static_cast<uint64_t>(experts))
-                atomicAdd(counters + (static_cast<uint32_t>(id) << lg) + (lane & ((1 << lg) - 1)), 1u);
-        }
-    }
     if (lane == 0 && tokens) atomicAdd(counters + (experts << lg), tokens);
 
-    // rows of one wave, then the waves one after another
+    // the rows of a wave, then the waves: as many as there is room for side by side, the others on top of them
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-#pragma unroll
-            for (int s = L; s < kWave; s <<= 1) acc[j][i] += __shfl_xor(acc[j][i], s);
-        }
-    for (int w = 0; w < kBalanceWaves; ++w) {
-        if (w == wave && lane < L) {
+        for (int i = 0; i < VEC; ++i) acc[j][i] = rows_sum<L>(acc[j][i]);
+    float* mine = sums + wave % rows_of_sums * experts;
+    for (int first = 0; first < WAVES; first += rows_of_sums) {
+        if (wave >= first && wave < first + rows_of_sums && lane < L) {
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int i = 0; i < VEC; ++i)
-                    if (own[j][i] != 0.0f) sums[R::at(j, experts) + i] += acc[j][i];
+                    if (own[j][i] != 0.0f) mine[R::at(j, experts) + i] = first == 0 ? acc[j][i] : mine[R::at(j, experts) + i] + acc[j][i];
         }
         __syncthreads();
     }
-    float* prob = reinterpret_cast<float*>(workspace + 16);
-    uint32_t* count = workspace + 16 + gridDim.x * experts;
-    auto sum_of = [&](int e) {
+    auto wave_sums = [&](int e) {
+        float s = sums[e];
+#pragma unroll 4
+        for (int r = 1; r < rows_of_sums; ++r) s += sums[r * experts + e];
+        return s;
+    };
+    auto copies = [&](int e) {
         uint32_t c = 0;
+#pragma unroll 8
         for (int r = 0; r < 1 << lg; ++r) c += counters[(e << lg) + r];
         return c;
     };
-    for (int e = threadIdx.x; e <= experts; e += kWave * kBalanceWaves) {
-        if (e < experts) __hip_atomic_store(prob + blockIdx.x * experts + e, sums[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(count + blockIdx.x * (experts + 1) + e, sum_of(e), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    auto finish = [&](auto&& count, auto&& prob) {       // by what the whole workgroup sees
+        for (int e = threadIdx.x; e <= experts; e += kThreads) {
+            o.counts[e] = static_cast<int32_t>(count(e));
+            if (e < experts) o.prob[e] = prob(e);
+        }
+        if (o.loss)
+            balance_loss<kThreads>(o, static_cast<int32_t>(count(experts)), [&](int e) { return static_cast<double>(count(e)); },
+                                   [&](int e) { return static_cast<double>(prob(e)); }, part);
+    };
+    if (gridDim.x == 1) {
+        finish(copies, wave_sums);
+        return;
     }
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0)
-        last = __hip_atomic_fetch_add(workspace, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
+
+    // [group][expert] of a sum and a count, and every group's tokens behind them
+    uint64_t* pairs = reinterpret_cast<uint64_t*>(workspace + 16);
+    uint32_t* group_tokens = reinterpret_cast<uint32_t*>(pairs + static_cast<size_t>(gridDim.x) * experts);
+    for (int e = threadIdx.x; e < experts; e += kThreads)
+        publish(pairs + blockIdx.x * experts + e, static_cast<uint64_t>(copies(e)) << 32 | __float_as_uint(wave_sums(e)));
+    if (threadIdx.x == 0) publish(group_tokens + blockIdx.x, copies(experts));
+    if (!last_to_arrive(workspace, &last)) return;
 
     // The groups' sums, by as many threads per expert as there are, in a fixed order.
-    __shared__ double slice_sum[kWave * kBalanceWaves];
-    __shared__ uint32_t slice_count[kWave * kBalanceWaves];
+    __shared__ double slice_sum[kThreads];
+    __shared__ uint32_t slice_count[kThreads];
+    uint32_t all = threadIdx.x < gridDim.x ? group_tokens[threadIdx.x] : 0;     // (no more groups than threads)
+    static_assert(kThreads >= kBalanceGroups, "a thread for every group");
     int width = 1;                                          // threads of a slice, a power of two
-    while (width < experts + 1 && width < kWave * kBalanceWaves) width *= 2;
-    const int slices = kWave * kBalanceWaves / width, slice = threadIdx.x / width;
-    for (int e0 = 0; e0 <= experts; e0 += width) {
+    while (width < experts && width < kThreads) width *= 2;
+    const uint32_t slices = kThreads / width, slice = threadIdx.x / width;
+    for (int e0 = 0; e0 < experts; e0 += width) {
         const int e = e0 + threadIdx.x % width;
         double s = 0.0;
         uint32_t c = 0;
-        if (e <= experts) {
-#pragma unroll 8
-            for (uint32_t g = slice; g < gridDim.x; g += slices) {
-                if (e < experts) s += __hip_atomic_load(prob + g * experts + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                c += __hip_atomic_load(count + g * (experts + 1) + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint64_t* from = pairs + min(e, experts - 1);
+        // sixteen at a time and without a test before a load, or each would be waited for
+        for (uint32_t g = slice; g < gridDim.x; g += 16 * slices) {
+            uint64_t pair[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) pair[i] = from[static_cast<size_t>(min(g + i * slices, gridDim.x - 1)) * experts];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                if (g + i * slices >= gridDim.x) pair[i] = 0;
+                s += __uint_as_float(static_cast<uint32_t>(pair[i]));
+                c += static_cast<uint32_t>(pair[i] >> 32);
             }
         }
         slice_sum[threadIdx.x] = s;
         slice_count[threadIdx.x] = c;
         __syncthreads();
-        if (slice == 0 && e <= experts) {
-            for (int i = 1; i < slices; ++i) {
+        if (slice == 0 && e < experts) {
+#pragma unroll 8
+            for (uint32_t i = 1; i < slices; ++i) {
                 s += slice_sum[i * width + threadIdx.x];
                 c += slice_count[i * width + threadIdx.x];
             }
-            o.counts[e] = static_cast<int32_t>(c);
-            if (e < experts) {
-                o.prob[e] = static_cast<float>(s);
-                sums[e] = static_cast<float>(s);
-            }
+            sums[e] = static_cast<float>(s);
             counters[e] = c;
         }
         __syncthreads();
     }
+    if (threadIdx.x == 0) counters[experts] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) all += __shfl_xor(all, s);
+    if (lane == 0 && all) atomicAdd(counters + experts, all);
+    __syncthreads();
     if (threadIdx.x == 0) __hip_atomic_store(workspace, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next call
-    if (o.loss)
-        balance_loss<kWave * kBalanceWaves>(o, static_cast<int32_t>(counters[experts]), [&](int e) { return static_cast<double>(counters[e]); },
-                                            [&](int e) { return static_cast<double>(sums[e]); }, part);
+    finish([&](int e) { return counters[e]; }, [&](int e) { return sums[e]; });
 }
 
 __global__ void __launch_bounds__(256)
@@ -312,11 +411,12 @@ k_balance_loss(const int32_t* __restrict__ counts, const float* __restrict__ pro
 
 // The backward pass: the probabilities are formed again from the logits, which are read anyway.
 template <int TYPE, int VEC, int L, int NV, int UNROLL>
-__global__ void __launch_bounds__(kWave * kGradWaves)
+__global__ void __launch_bounds__(kWave * kGradWaves, NV == 1 ? 8 : 1)
 k_balance_grad(Workers ws, size_t ld, size_t ld_out, uint32_t units, int experts, const float* __restrict__ weight, const float* __restrict__ upstream)
 {
     typedef Row<TYPE, VEC, L, NV> R;
     typedef typename R::one one;
+    const LaneTable table(ws);
     const uint32_t waves = gridDim.x * kGradWaves;
     const float up = upstream ? upstream[0] : 1.0f;
     float own[NV][VEC], g[NV][VEC];
@@ -326,12 +426,18 @@ k_balance_grad(Workers ws, size_t ld, size_t ld_out, uint32_t units, int experts
 #pragma unroll
         for (int i = 0; i < VEC; ++i) g[j][i] = weight[R::at(j, experts) + i];
     for (uint32_t unit = blockIdx.x * kGradWaves + wave_index(); unit < units; unit += UNROLL * waves) {
-        Token k[UNROLL];
+        Unit k[UNROLL];
         R row[UNROLL];
+        uint8_t flag[UNROLL];
+        bool counts[UNROLL];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) k[u] = token_of<R::kRows, L>(ws, unit + u * waves, units);
+        for (int u = 0; u < UNROLL; ++u) k[u] = unit_of<R::kRows, L>(table, unit + u * waves, units);
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) row[u].load(static_cast<const one*>(ws.logits[k[u].w]) + k[u].t * ld, experts, k[u].counts);
+        for (int u = 0; u < UNROLL; ++u) flag[u] = *k[u].flag;
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) counts[u] = k[u].exists && (!k[u].masked || flag[u] != 0);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) row[u].load(table_ptr<const one>(k[u].logits) + k[u].t * ld, experts, counts[u]);
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             float e[NV][VEC], dot = 0.0f;
@@ -340,24 +446,24 @@ k_balance_grad(Workers ws, size_t ld, size_t ld_out, uint32_t units, int experts
             for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) dot = __builtin_fmaf(e[j][i], g[j][i] * own[j][i], dot);
-            dot = lanes_reduce<L>(dot, OpAddF()) * inverse;
-            const float scale = inverse * up;
-            one* out = static_cast<one*>(const_cast<void*>(ws.ids[k[u].w])) + k[u].t * ld_out;
+            // (rows that do not count were read as zeros)
+            const float scale = counts[u] ? inverse * up : 0.0f, shift = -(lanes_reduce<L>(dot, OpAddF()) * inverse) * scale;
+            one* out = table_ptr<one>(k[u].other) + k[u].t * ld_out;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 typename R::raw q;
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) q[i] = Elem<TYPE>::narrow(k[u].counts ? (e[j][i] * scale) * (g[j][i] - dot) : 0.0f);
+                for (int i = 0; i < VEC; ++i) q[i] = Elem<TYPE>::narrow(e[j][i] * __builtin_fmaf(g[j][i], scale, shift));
                 if (k[u].exists) __builtin_nontemporal_store(q, reinterpret_cast<typename R::raw*>(out + R::at(j, experts)));
             }
         }
     }
 }
 
-// Calls f with the layout of a row of `experts` elements: {VEC, L, NV, rows of a wave that are in flight together}.
-template <int VEC_, int L_, int NV_, int UNROLL_>
+// Calls f with the layout of a row of `experts` elements: VEC, L, NV, and units that a wave has in flight together.
+template <int VEC_, int L_, int NV_, int UNROLL_, int WAVES_ = 16>
 struct Layout {
-    static constexpr int VEC = VEC_, L = L_, NV = NV_, UNROLL = UNROLL_;
+    static constexpr int VEC = VEC_, L = L_, NV = NV_, UNROLL = UNROLL_, WAVES = WAVES_, GRAD_UNROLL = NV_ == 1 ? 2 : 1;   // WAVES: of a workgroup of the forward pass
 };
 template <typename F>
 inline void with_layout(int experts, const F& f)
@@ -375,7 +481,7 @@ inline void with_layout(int experts, const F& f)
     else if (experts <= 256) f(Layout<8, 32, 1, 4>());
     else if (experts <= 512) f(Layout<8, 64, 1, 4>());
     else if (experts <= 1024) f(Layout<8, 64, 2, 2>());
-    else f(Layout<8, 64, 4, 1>());
+    else f(Layout<8, 64, 4, 1, 8>());
 }
 template <typename F>
 inline void with_type(int dtype, const F& f)
@@ -422,7 +528,7 @@ using namespace bagua;
 extern "C" size_t bagua_balance_workspace_bytes(int experts)
 {
     if (experts < 1 || experts > BAGUA_MAX_EXPERTS) return 0;
-    return (64 + kBalanceGroups * (2 * static_cast<size_t>(experts) + 1) * sizeof(uint32_t) + 15) & ~static_cast<size_t>(15);
+    return 64 + kBalanceGroups * (2 * static_cast<size_t>(experts) + 1) * sizeof(uint32_t);
 }
 
 extern "C" int bagua_balance_stats(int dtype, const void* const* logits, size_t ld, const size_t* tokens, int k, int experts,
@@ -462,9 +568,8 @@ extern "C" int bagua_balance_stats(int dtype, const void* const* logits, size_t 
     if (!aligned16(workspace) || !aligned4(counts) || !aligned4(prob) || !aligned4(loss) || !aligned4(weight)) return BAGUA_ERR_ALIGNMENT;
     const BalanceOut out{counts, prob, loss, weight, alpha, experts, top_k};
     const uint32_t per_k = top_k == 1 ? 0 : static_cast<uint32_t>((0x100000000ull + static_cast<uint64_t>(top_k) - 1) / static_cast<uint64_t>(top_k));
-    int lg = 5;                                             // copies of a counter: what fits 16 KiB
+    int lg = 3;                                             // copies of a counter: what fits 16 KiB, eight at most
     while (lg > 0 && ((e + 1) << lg) > 4096) --lg;
-    const size_t lds = (e + ((e + 1) << lg)) * sizeof(float);
     int status = BAGUA_OK;
     with_layout(experts, [&](auto layout) {
         typedef decltype(layout) Lay;
@@ -473,10 +578,10 @@ extern "C" int bagua_balance_stats(int dtype, const void* const* logits, size_t 
             return;
         }
         const uint32_t units = ws.first_unit[BAGUA_MAX_WORKERS];
-        const size_t work = std::max<size_t>((units + kBalanceWaves - 1) / kBalanceWaves, (choices + 8 * kWave * kBalanceWaves - 1) / (8 * kWave * kBalanceWaves));
-        const dim3 grid(static_cast<unsigned>(std::min<size_t>(std::max<size_t>(work, 1), kBalanceGroups))), block(kWave * kBalanceWaves);
+        const dim3 grid(std::min<uint32_t>(std::max<uint32_t>((units + Lay::WAVES - 1) / Lay::WAVES, 1), kBalanceGroups)), block(kWave * Lay::WAVES);
+        const size_t lds = (static_cast<size_t>(sum_rows(Lay::WAVES, experts)) * e + ((e + 1) << lg)) * sizeof(float);
         with_type(dtype, [&](auto type) {
-            launch_kernel(k_balance_stats<decltype(type)::value, Lay::VEC, Lay::L, Lay::NV, Lay::UNROLL>, grid, block, lds, static_cast<hipStream_t>(stream),
+            launch_kernel(k_balance_stats<decltype(type)::value, Lay::VEC, Lay::L, Lay::NV, Lay::UNROLL, Lay::WAVES>, grid, block, lds, static_cast<hipStream_t>(stream),
                           ws, ld, ids_ld, id_bytes, units, per_k, lg, static_cast<uint32_t*>(workspace), out);
         });
         status = launch_status();
@@ -535,9 +640,10 @@ extern "C" int bagua_balance_grad(int dtype, const void* const* logits, size_t l
         }
         const uint32_t units = ws.first_unit[BAGUA_MAX_WORKERS];
         if (units == 0) return;
-        const dim3 grid(std::min<uint32_t>((units + kGradWaves - 1) / kGradWaves, kCus * 8)), block(kWave * kGradWaves);
+        const uint32_t waves = std::min<uint32_t>((units + Lay::GRAD_UNROLL - 1) / Lay::GRAD_UNROLL, kGradMostWaves);
+        const dim3 grid((waves + kGradWaves - 1) / kGradWaves), block(kWave * kGradWaves);
         with_type(dtype, [&](auto type) {
-            launch_kernel(k_balance_grad<decltype(type)::value, Lay::VEC, Lay::L, Lay::NV, Lay::UNROLL>, grid, block, 0, static_cast<hipStream_t>(stream), ws, ld,
+            launch_kernel(k_balance_grad<decltype(type)::value, Lay::VEC, Lay::L, Lay::NV, Lay::GRAD_UNROLL>, grid, block, 0, static_cast<hipStream_t>(stream), ws, ld,
                           ld_out, units, experts, weight, upstream);
         });
         status = launch_status();

@@ -29,9 +29,15 @@ namespace {
     X(bagua_decompress_adam_step) X(bagua_compress_topk_ef) X(bagua_decompress_reduce_recompress_topk) X(bagua_decompress_topk) \
     X(bagua_decompress_sgd_step_topk) X(bagua_decompress_adam_step_topk)
 
+// Those of the calls on a plan and of the balance loss; their functions here go by the second part of the name.
+#define BAGUA_NATIVE_STEPS(X) X(grad_norm) X(adamw_step) X(balance_stats) X(balance_grad)
+
 // The entry points, as binding.py's library has them: the address of each, so that both paths call one and the same library.
 #define X(name) decltype(&name) f_##name = nullptr;
 BAGUA_NATIVE(X)
+#undef X
+#define X(name) decltype(&bagua_##name) f_bagua_##name = nullptr;
+BAGUA_NATIVE_STEPS(X)
 #undef X
 PyObject* g_error = nullptr;        // binding.BaguaError
 PyObject* g_raw_stream = nullptr;   // device index -> raw handle of its current stream
@@ -93,13 +99,14 @@ struct Args {
         ok = ok && v < 256;
         return static_cast<int>(v);
     }
-    float real(int i)
+    double number(int i)
     {
-        if (!ok || !(PyFloat_CheckExact(a[i]) || PyLong_CheckExact(a[i]))) { ok = false; return 0.0f; }
+        if (!ok || !(PyFloat_CheckExact(a[i]) || PyLong_CheckExact(a[i]))) { ok = false; return 0.0; }
         const double v = PyFloat_AsDouble(a[i]);
         if (PyErr_Occurred()) PyErr_Clear(), ok = false;
-        return static_cast<float>(v);
+        return v;
     }
+    float real(int i) { return static_cast<float>(number(i)); }
     bool flag(int i)
     {
         ok = ok && PyBool_Check(a[i]);
@@ -135,6 +142,54 @@ struct Args {
             ok = v >= 0 && v < BAGUA_MAX_WORKERS;
             p[j] = static_cast<int>(v);
         }
+    }
+    // A list of workers' matrices (2-D, the elements of a row next to each other, all rows equally far apart) of one type: addresses and
+    // numbers of rows into p and rows, where those are given what they have to be (known: of the rows).  columns: -1 = of the first one.
+    struct Matrices {
+        int count = 0;
+        at::ScalarType type = at::kFloat;
+        int64_t columns = -1, ld = -1;
+        size_t stride() const { return static_cast<size_t>(ld < 0 ? columns : ld); }
+    };
+    Matrices matrices(int i, const void** p, size_t* rows, bool known, int64_t columns, int expected)
+    {
+        Matrices m;
+        m.columns = columns;
+        if (!ok || !(PyList_CheckExact(a[i]) || PyTuple_CheckExact(a[i]))) { ok = false; return m; }
+        const Py_ssize_t count = PySequence_Fast_GET_SIZE(a[i]);
+        if (count < 1 || count > BAGUA_MAX_WORKERS || (expected >= 0 && count != expected)) { ok = false; return m; }
+        m.count = static_cast<int>(count);
+        PyObject** items = PySequence_Fast_ITEMS(a[i]);
+        for (Py_ssize_t j = 0; j < count; ++j) {
+            if (!THPVariable_CheckTypeExact(Py_TYPE(items[j]))) { ok = false; return m; }
+            const at::Tensor& t = THPVariable_Unpack(items[j]);
+            if (!t.is_cuda() || t.layout() != at::kStrided || t.dim() != 2) { ok = false; return m; }
+            const int64_t r = t.size(0), c = t.size(1);
+            if (j == 0) m.type = t.scalar_type(), m.columns = m.columns < 0 ? c : m.columns;
+            if (t.scalar_type() != m.type || c != m.columns || (known && static_cast<size_t>(r) != rows[j]) || (r > 0 && c > 1 && t.stride(1) != 1)) { ok = false; return m; }
+            if (r > 1) {
+                if (t.stride(0) < c || (m.ld >= 0 && t.stride(0) != m.ld)) { ok = false; return m; }
+                m.ld = t.stride(0);
+            }
+            rows[j] = static_cast<size_t>(r);
+            p[j] = r ? t.data_ptr() : nullptr;
+        }
+        return m;
+    }
+    // The workers' masks, or nullptr for None.
+    const uint8_t* const* masks(int i, const uint8_t** p, const size_t* rows, int count)
+    {
+        if (!ok || !given(i)) return nullptr;
+        if (!(PyList_CheckExact(a[i]) || PyTuple_CheckExact(a[i])) || PySequence_Fast_GET_SIZE(a[i]) != count) { ok = false; return nullptr; }
+        PyObject** items = PySequence_Fast_ITEMS(a[i]);
+        for (int j = 0; j < count && ok; ++j) {
+            void* q = nullptr;
+            ok = items[j] != Py_None && tensor_ptr(items[j], kAny, rows[j], &q);
+            const at::ScalarType type = ok ? THPVariable_Unpack(items[j]).scalar_type() : at::kByte;
+            ok = ok && (type == at::kByte || type == at::kBool);
+            p[j] = rows[j] ? static_cast<const uint8_t*>(q) : nullptr;
+        }
+        return p;
     }
     size_t slots(size_t keep, size_t n, size_t chunk)
     {
@@ -481,6 +536,72 @@ PY(bagua_decompress_adam_step_topk, 15)
 PY_END
 
 #undef PY
+#define PY(name, expected)                                                              \
+    PyObject* py_##name(PyObject*, PyObject* const* a, Py_ssize_t given)                \
+    {                                                                                   \
+        return call("bagua_" #name, a, given, expected, [](Args& v) {
+
+// The address of a plan that its object holds.
+const bagua_tensor_plan_t* plan_at(size_t v) { return reinterpret_cast<const bagua_tensor_plan_t*>(v); }
+int type_of(at::ScalarType t) { return t == at::kFloat ? BAGUA_F32 : t == at::kBFloat16 ? BAGUA_BF16 : t == at::kHalf ? BAGUA_F16 : -1; }
+
+PY(grad_norm, 5)   // address of the plan, out, max_norm, grad_scale, stream
+    const size_t plan = v.size(0);
+    float* out = v.f32(1, 2);
+    const double most = v.number(2), scale = v.number(3);
+    v.ok = v.ok && out;
+    return [=](void* s) { return f_bagua_grad_norm(plan_at(plan), scale, most, out, s); };
+PY_END
+
+PY(adamw_step, 10)   // address of the plan, step, lr, beta1, beta2, eps, weight_decay, clip, seed, stream
+    const size_t plan = v.size(0), step = v.size(1), seed = v.size(8);
+    const double lr = v.number(2), b1 = v.number(3), b2 = v.number(4), eps = v.number(5), wd = v.number(6);
+    const float* clip = v.f32(7, 2);
+    v.ok = v.ok && seed <= 0xffffffffu;
+    return [=](void* s) { return f_bagua_adamw_step(plan_at(plan), step, lr, b1, b2, eps, wd, clip, static_cast<uint32_t>(seed), s); };
+PY_END
+
+PY(balance_stats, 10)   // logits, ids, mask, counts, prob, workspace, alpha, loss, weight, stream
+    struct {
+        const void *x[BAGUA_MAX_WORKERS], *i[BAGUA_MAX_WORKERS];
+        const uint8_t* m[BAGUA_MAX_WORKERS];
+        size_t rows[BAGUA_MAX_WORKERS];
+    } p;
+    const auto x = v.matrices(0, p.x, p.rows, false, -1, -1);
+    const auto i = v.matrices(1, p.i, p.rows, true, -1, x.count);
+    const bool masked = v.masks(2, p.m, p.rows, x.count) != nullptr;
+    v.ok = v.ok && type_of(x.type) >= 0 && (i.type == at::kInt || i.type == at::kLong) && x.columns <= BAGUA_MAX_EXPERTS && i.columns <= x.columns;
+    const size_t e = v.ok ? static_cast<size_t>(x.columns) : 0;
+    int32_t* counts = static_cast<int32_t*>(v.ptr(3, kI32, (e + 1) * sizeof(int32_t)));
+    float *prob = v.f32(4, e), *loss = v.f32(7, 1), *weight = v.f32(8, e);
+    void* ws = v.ptr(5, kAny, 0);
+    const size_t bytes = v.ok && v.given(5) ? THPVariable_Unpack(v.a[5]).nbytes() : 0;
+    const double alpha = v.number(6);
+    return [=](void* s) {
+        return f_bagua_balance_stats(type_of(x.type), p.x, x.stride(), p.rows, x.count, static_cast<int>(e), p.i, i.type == at::kInt ? 4 : 8, i.stride(),
+                                     static_cast<int>(i.columns), masked ? p.m : nullptr, counts, prob, alpha, loss, weight, ws, bytes, s);
+    };
+PY_END
+
+PY(balance_grad, 6)   // logits, mask, weight, upstream, dlogits, stream
+    struct {
+        const void *x[BAGUA_MAX_WORKERS], *o[BAGUA_MAX_WORKERS];
+        const uint8_t* m[BAGUA_MAX_WORKERS];
+        size_t rows[BAGUA_MAX_WORKERS];
+    } p;
+    const auto x = v.matrices(0, p.x, p.rows, false, -1, -1);
+    const bool masked = v.masks(1, p.m, p.rows, x.count) != nullptr;
+    const auto o = v.matrices(4, p.o, p.rows, true, x.columns, x.count);
+    v.ok = v.ok && type_of(x.type) >= 0 && o.type == x.type && x.columns <= BAGUA_MAX_EXPERTS;
+    const size_t e = v.ok ? static_cast<size_t>(x.columns) : 0;
+    const float *weight = v.f32(2, e), *up = v.f32(3, 1);
+    return [=](void* s) {
+        return f_bagua_balance_grad(type_of(x.type), p.x, x.stride(), p.rows, x.count, static_cast<int>(e), masked ? p.m : nullptr, weight, up,
+                                    const_cast<void* const*>(p.o), o.stride(), s);
+    };
+PY_END
+
+#undef PY
 #undef PY_END
 
 // bind(library, error, raw_stream, device): library = {name of an entry point: its address}
@@ -502,6 +623,18 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t given)
     }
     BAGUA_NATIVE(X)
 #undef X
+#define X(name)                                                                     \
+    {                                                                               \
+        PyObject* at = PyDict_GetItemString(a[0], "bagua_" #name);                  \
+        void* p = at ? PyLong_AsVoidPtr(at) : nullptr;                              \
+        if (!p) {                                                                   \
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_KeyError, "bagua_" #name); \
+            return nullptr;                                                         \
+        }                                                                           \
+        f_bagua_##name = reinterpret_cast<decltype(&bagua_##name)>(p);              \
+    }
+    BAGUA_NATIVE_STEPS(X)
+#undef X
     PyObject** keep[3] = {&g_error, &g_raw_stream, &g_device};
     for (int i = 0; i < 3; ++i) {
         Py_INCREF(a[1 + i]);
@@ -511,7 +644,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t given)
 }
 
 #define X(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr},
-PyMethodDef g_methods[] = {BAGUA_NATIVE(X){"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind)), METH_FASTCALL, nullptr},
+PyMethodDef g_methods[] = {BAGUA_NATIVE(X) BAGUA_NATIVE_STEPS(X){"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind)), METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 #undef X
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

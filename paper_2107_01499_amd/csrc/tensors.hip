@@ -251,16 +251,11 @@ k_grad_norm(TensorPlanView plan, uint32_t tiles, double scale, double max_norm, 
     __shared__ bool last;
     if (lane == 0) part[wave] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        const double s = (part[0] + part[1]) + (part[2] + part[3]);
-        __hip_atomic_store(plan.partial + blockIdx.x, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        last = __hip_atomic_fetch_add(plan.counter, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
-    }
-    __syncthreads();
-    if (!last) return;
+    if (threadIdx.x == 0) publish(plan.partial + blockIdx.x, (part[0] + part[1]) + (part[2] + part[3]));
+    if (!last_to_arrive(plan.counter, &last)) return;
     sum = 0.0;
-    for (uint32_t i = threadIdx.x; i < gridDim.x; i += kWave * kNormWaves)
-        sum += __hip_atomic_load(plan.partial + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll 8
+    for (uint32_t i = threadIdx.x; i < gridDim.x; i += kWave * kNormWaves) sum += plan.partial[i];
 #pragma unroll
     for (int s = 32; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
     if (lane == 0) part[wave] = sum;
