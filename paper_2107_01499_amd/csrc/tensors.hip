@@ -5,6 +5,7 @@
 // Tensors need the alignment of their elements only: the accesses are declared so, and the hardware takes them at any address.
 #include <cmath>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "batch.hpp"
@@ -16,6 +17,18 @@ namespace bagua {
 
 constexpr int kTensorTile = 1024;
 constexpr int kTileRows = kTensorTile / kRow;
+// Rows of 256 elements that a wave (the whole workgroup) takes of a tile.  32 bits: the step is bound by memory, and one row streams
+// fastest: 1 | 2 | 4 rows, 335 M elements, bf16 gradients and copies, 1524 | 1639 | 1644 us, 25.6 M fp32 113 | 115 | 118.  8 bits: bound by the
+// vector ALU, of which a block's maximum and reciprocals take less where blocks share them (blocks_most): 335 M elements, bf16 parameters
+// 733 | 566 | 569 us, 109 M with fp32 parameters and bf16 copies 300 | 275 | 284, 49 small tensors 16.5 | 4.0 | 5.5.
+#ifndef BAGUA_ADAM8_ROWS
+#define BAGUA_ADAM8_ROWS 2
+#endif
+#ifndef BAGUA_ADAM32_ROWS
+#define BAGUA_ADAM32_ROWS 1
+#endif
+static_assert((BAGUA_ADAM8_ROWS == 1 || BAGUA_ADAM8_ROWS == 2 || BAGUA_ADAM8_ROWS == 4) && (BAGUA_ADAM32_ROWS == 1 || BAGUA_ADAM32_ROWS == 2 || BAGUA_ADAM32_ROWS == 4),
+              "rows that divide a tile");
 constexpr unsigned kNormGroups = 2048;    // most workgroups of the norm: eight waves of four on every SIMD
 constexpr unsigned kNormWaves = 4;
 
@@ -44,45 +57,55 @@ inline TensorPlanView tensor_plan_view(const bagua_tensor_plan_t* p)
 }
 
 // ---------------------------------------------------------------- four elements of a row
-// `remain`: valid elements from the row's start on (wave-uniform).  Absent ones read as 0.
-template <int TYPE>
-__device__ __forceinline__ f4 load_four(const typename Elem<TYPE>::one* row, int lane, int remain)
+// Four elements of a lane, from element e on, as they are in memory.  FULL: all are there.  Otherwise a lane that reaches over the end makes
+// the last access that does not, and moves what it gets into place: no load stands behind a test, or each would be waited for before
+// the next.  What lanes beyond the end hold means nothing.  `left`: valid elements; ANY: fewer than four, one by one.
+template <typename T>
+struct Four {
+    typedef T v __attribute__((ext_vector_type(4)));
+    typedef T u __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+};
+enum Edge { kFull, kCut, kFew };
+template <Edge EDGE, typename T>
+__device__ __forceinline__ typename Four<T>::v fetch(const T* x, int e, int left)
 {
-    typedef Elem<TYPE> E;
-    const int e = lane * 4;
-    if (remain >= kRow) return E::load(row + e);
-    f4 r = f4{0.f, 0.f, 0.f, 0.f};
-    if (e + 0 < remain) r.x = E::widen(row[e + 0]);
-    if (e + 1 < remain) r.y = E::widen(row[e + 1]);
-    if (e + 2 < remain) r.z = E::widen(row[e + 2]);
-    if (e + 3 < remain) r.w = E::widen(row[e + 3]);
-    return r;
+    if (EDGE == kFew) {
+        const int last = left - 1;
+        return typename Four<T>::v{x[min(e, last)], x[min(e + 1, last)], x[min(e + 2, last)], x[min(e + 3, last)]};
+    }
+    return __builtin_nontemporal_load(reinterpret_cast<const typename Four<T>::u*>(x + (EDGE == kFull ? e : min(e, left - 4))));
 }
-template <int TYPE>
-__device__ __forceinline__ void store_four(typename Elem<TYPE>::one* row, int lane, int remain, f4 v)
+template <Edge EDGE, typename T>
+__device__ __forceinline__ T in_place(T q, int e, int left)
 {
-    typedef Elem<TYPE> E;
-    const int e = lane * 4;
-    if (remain >= kRow) {
-        E::store(row + e, v);
+    if (EDGE != kCut) return q;
+    const int skip = e - min(e, left - 4);
+    const T s = (skip & 2) != 0 ? T{q.z, q.w, q.w, q.w} : q;
+    return (skip & 1) != 0 ? T{s.y, s.z, s.w, s.w} : s;
+}
+template <Edge EDGE, typename T>
+__device__ __forceinline__ void put(T* x, int e, int left, typename Four<T>::v v)
+{
+    if (EDGE == kFull || e + 4 <= left) {
+        __builtin_nontemporal_store(static_cast<typename Four<T>::u>(v), reinterpret_cast<typename Four<T>::u*>(x + e));
     } else {
-        if (e + 0 < remain) row[e + 0] = E::narrow(v.x);
-        if (e + 1 < remain) row[e + 1] = E::narrow(v.y);
-        if (e + 2 < remain) row[e + 2] = E::narrow(v.z);
-        if (e + 3 < remain) row[e + 3] = E::narrow(v.w);
+        if (e + 0 < left) x[e + 0] = v.x;
+        if (e + 1 < left) x[e + 1] = v.y;
+        if (e + 2 < left) x[e + 2] = v.z;
     }
 }
-__device__ __forceinline__ uint32_t load_four_codes(const uint8_t* row, int lane, int remain)
+template <int TYPE>
+__device__ __forceinline__ f4 widened(typename Four<typename Elem<TYPE>::one>::v q)
 {
-    if (remain >= kRow) return __builtin_nontemporal_load(reinterpret_cast<const u32u*>(row + lane * 4));
-    return load_codes_row(row, lane, remain);
+    typedef Elem<TYPE> E;
+    return f4{E::widen(q.x), E::widen(q.y), E::widen(q.z), E::widen(q.w)};
 }
-__device__ __forceinline__ void store_four_codes(uint8_t* row, int lane, int remain, uint32_t w)
+template <int TYPE>
+__device__ __forceinline__ typename Four<typename Elem<TYPE>::one>::v narrowed(f4 v)
 {
-    if (remain >= kRow) __builtin_nontemporal_store(static_cast<u32u>(w), reinterpret_cast<u32u*>(row + lane * 4));
-    else store_codes_row(row, lane, remain, w, 0);
+    typedef Elem<TYPE> E;
+    return {E::narrow(v.x), E::narrow(v.y), E::narrow(v.z), E::narrow(v.w)};
 }
-
 // ---------------------------------------------------------------- E4M3 codes with a scale
 typedef float f2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ f4 widen_codes(uint32_t w, float scale)
@@ -90,14 +113,15 @@ __device__ __forceinline__ f4 widen_codes(uint32_t w, float scale)
     const f2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w), true);
     return f4{lo.x * scale, lo.y * scale, hi.x * scale, hi.y * scale};
 }
-// Scale of a block whose largest magnitude is `most`, and its reciprocal; a block that is (nearly) zero has neither.
+// Scale of a block whose largest magnitude is `most`, and its reciprocal; a block that is (nearly) zero has neither, and what is no
+// number stays none.
 struct Scale {
     float scale, inverse;
 };
 __device__ __forceinline__ Scale scale_of(float most)
 {
     const float s = most * static_cast<float>(1.0 / 448.0);
-    return s >= 0x1p-126f ? Scale{s, 1.0f / s} : Scale{0.0f, 0.0f};
+    return s < 0x1p-126f ? Scale{0.0f, 0.0f} : Scale{s, 1.0f / s};
 }
 __device__ __forceinline__ uint32_t nearest_codes(f4 y)
 {
@@ -105,13 +129,18 @@ __device__ __forceinline__ uint32_t nearest_codes(f4 y)
     return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(y.z, y.w, w, true));
 }
 // y >= 0 times 2^-120 has E4M3's exponent field in the low bits of fp32's own (and its subnormals where fp32 has them), so
-// the bits above the 20 lowest are the code, and what lies below them is how far y is on the way to the next one.
-__device__ __forceinline__ uint32_t random_code(float y, float r, uint32_t random)
+// the bits above the 20 lowest are the code, and what lies below them is how far y is on the way to the next one.  Two codes at a time
+// in the halves of a register; a code is not below 1 where the root is above 0 (its upper half is not zero then) and not above 126.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2 upper_halves(uint32_t a, uint32_t b) { return __builtin_bit_cast(u16x2, __builtin_amdgcn_perm(b, a, 0x07060302u)); }
+__device__ __forceinline__ uint32_t code_bits(float y, uint32_t random) { return __float_as_uint(y * 0x1p-120f) + (random >> 12); }
+__device__ __forceinline__ u16x2 two_codes(uint32_t a, uint32_t b, float ra, float rb)
 {
-    uint32_t c = (__float_as_uint(y * 0x1p-120f) + (random >> 12)) >> 20;
-    c = c < 1 ? 1 : c > 126 ? 126 : c;
-    c = r == r ? c : 127;                 // what is no number stays none
-    return r == 0.0f ? 0 : c;
+    u16x2 one = u16x2{1, 1};
+    asm("" : "+v"(one));      // (a minimum with a constant 1 becomes a comparison and a selection for each half)
+    const u16x2 least = __builtin_elementwise_min(upper_halves(__float_as_uint(ra), __float_as_uint(rb)), one);
+    const u16x2 c = __builtin_elementwise_min(upper_halves(a, b) >> static_cast<uint16_t>(4), u16x2{126, 126});
+    return __builtin_elementwise_max(c, least);
 }
 
 __device__ __forceinline__ uint32_t mix(uint32_t x)
@@ -131,87 +160,208 @@ __device__ __forceinline__ uint16_t random_bf16(float x, uint32_t random)
 struct AdamArgs {
     const float* clip;
     float beta1, omb1, beta2, omb2, root, eps, rate, decay;   // root: 1/sqrt(1-beta2^t), rate: lr/(1-beta1^t), decay: lr*weight_decay
-    uint32_t seed, rows;
+    uint32_t seed;
+    bool in_range;             // see root_in_range
 };
 
-__device__ __forceinline__ float max4(f4 x) { return fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)); }
-__device__ __forceinline__ f4 abs4(f4 x) { return f4{fabsf(x.x), fabsf(x.y), fabsf(x.z), fabsf(x.w)}; }
+// The largest magnitude of four, as the bits of a number that is not negative: these are ordered as the numbers are, and across
+// lanes the integer maximum comes without the instructions that make a NaN quiet.
+__device__ __forceinline__ uint32_t most_of(f4 x) { return __float_as_uint(fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(x.z), fabsf(x.w)))); }
+struct OpMaxU { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); } };
 
-// G, P, C: types of gradient, parameter and copy (C < 0: none).
+// The largest of each of K blocks of 256 values, of which every lane holds one: that of block k in the 64 / K lanes from k * 64 / K on.
+// Blocks are put side by side on the way (two in the halves of a register, four in its rows of 16), so that four cost what one does.
+template <int K>
+__device__ __forceinline__ uint32_t blocks_most(const uint32_t (&x)[K])
+{
+    static_assert(K == 1 || K == 2 || K == 4, "");
+    const OpMaxU op;
+    auto halves = [&](uint32_t a, uint32_t b) { const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false); return op(r[0], r[1]); };
+    auto rows = [&](uint32_t a, uint32_t b) { const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false); return op(r[0], r[1]); };
+    if constexpr (K == 4) return row16_reduce(rows(halves(x[0], x[2]), halves(x[1], x[3])), op);
+    const uint32_t v = halves(x[0], x[K - 1]);
+    return row16_reduce(rows(v, v), op);
+}
+
+// Square root and quotient, correctly rounded, in 10 and 9 instruction slots instead of the 20 and 14 that they take for operands of any
+// size: the step with 8-bit states is bound by the vector ALU.  The operands are kept in a range that allows it: first moments times
+// 2^64, second ones times 2^64, roots times 2^32, which is exact, and the products with what belongs to them (rate, scales) undo it.
+//   root:      y = rsqrt, g = t*y and h = y/2 are a few units off; t - g*g is exact in a fused operation, and g + h * that rounds to the
+//              root: compared with sqrtf for every mantissa and both parities of the exponent.  Zero stays zero, as the reciprocal root is
+//              taken of something above it.
+//   quotient:  one Newton step makes the reciprocal of b the correctly rounded one (compared with 1/b for every mantissa); the remainder of
+//              a quotient that is a unit off at most is exact, and adding its product with the reciprocal rounds to the quotient.
+constexpr float kFirstScale = 0x1p64f, kSecondScale = 0x1p64f, kRootScale = 0x1p32f;
+__device__ __forceinline__ float root_in_range(float t)   // 0, or 2^-90 <= t < 2^126
+{
+    const float y = __builtin_amdgcn_rsqf(fmaxf(t, 0x1p-90f)), g = t * y;
+    return __builtin_fmaf(__builtin_fmaf(-g, g, t), 0.5f * y, g);
+}
+__device__ __forceinline__ float quotient_in_range(float a, float b)   // 2^-40 <= b < 2^21; a = 0, or 2^-101 <= |a| <= 2^84
+{
+    float y = __builtin_amdgcn_rcpf(b);
+    y = __builtin_fmaf(y, __builtin_fmaf(-b, y, 1.0f), y);
+    const float q = a * y;
+    return __builtin_fmaf(-__builtin_fmaf(b, q, -a), y, q);             // (the remainder's sign keeps that of a zero)
+}
+// Blocks that keep to the ranges: first moments up to 2^20, roots up to 2^10 (in their scaled forms).  What is no number does not.
+constexpr float kMostFirst = 0x1p84f, kMostRoot = 0x1p42f;
+inline bool in_range(float root, float eps) { return root <= 0x1p10f && eps >= 0x1p-40f && eps <= 1.0f; }
+
+constexpr int share_rows(int bits) { return bits == 8 ? BAGUA_ADAM8_ROWS : BAGUA_ADAM32_ROWS; }
+
+// K rows of 256 elements of a tile.  G, P, C: types of gradient, parameter and copy (C < 0: none).  e0: the first element
+// in its tensor; left: elements from there on.  FAST (8 bits): with the functions above; false, and nothing done, where a block does not
+// keep to their ranges.
+template <int G, int P, int C, int BITS, int K, Edge EDGE, bool FAST>
+__device__ __forceinline__ bool adamw_share(const TensorEntry& d, size_t e0, int lane, int left, float factor, const AdamArgs& a)
+{
+    static_assert(BITS == 8 || !FAST, "");
+    constexpr float kFirst = FAST ? kFirstScale : 1.0f, kSecond = FAST ? kSecondScale : 1.0f, kRoot = FAST ? kRootScale : 1.0f;
+    typedef typename Elem<P>::one param_t;
+    typedef typename Elem<G>::one grad_t;
+    typedef typename std::conditional<BITS == 8, uint8_t, float>::type state_t;
+    param_t* pp = table_ptr<param_t>(d.param) + e0;
+    const grad_t* gp = table_ptr<const grad_t>(d.grad) + e0;
+    state_t *mp = table_ptr<state_t>(d.m) + e0, *vp = table_ptr<state_t>(d.v) + e0;
+    float ms[K], vs[K];
+    if constexpr (BITS == 8) {
+        const float *msp = table_ptr<const float>(d.m_scale) + e0 / kRow, *vsp = table_ptr<const float>(d.v_scale) + e0 / kRow;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int block = EDGE == kFull || k * kRow < left ? k : 0;     // of a block that is not there: any
+            ms[k] = msp[block];
+            vs[k] = vsp[block];
+        }
+    }
+    typename Four<param_t>::v qp[K];
+    typename Four<grad_t>::v qg[K];
+    typename Four<state_t>::v qm[K], qv[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int e = k * kRow + lane * 4;
+        qm[k] = fetch<EDGE>(mp, e, left);
+        qv[k] = fetch<EDGE>(vp, e, left);
+        qg[k] = fetch<EDGE>(gp, e, left);
+        qp[k] = fetch<EDGE>(pp, e, left);
+    }
+    f4 m[K], r[K];
+    uint32_t m_most[K], r_most[K], over = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int e = k * kRow + lane * 4;
+        const f4 g = widened<G>(in_place<EDGE>(qg[k], e, left)) * factor;
+        f4 v;
+        if constexpr (BITS == 8) {
+            m[k] = widen_codes(__builtin_bit_cast(uint32_t, in_place<EDGE>(qm[k], e, left)), ms[k] * kFirst);
+            v = widen_codes(__builtin_bit_cast(uint32_t, in_place<EDGE>(qv[k], e, left)), vs[k]);
+            v = v * v;
+        } else {
+            m[k] = in_place<EDGE>(qm[k], e, left);
+            v = in_place<EDGE>(qv[k], e, left);
+        }
+        m[k] = m[k] * a.beta1 + g * (a.omb1 * kFirst);
+        v = v * a.beta2 + (g * g) * a.omb2;
+        if constexpr (BITS == 32) {
+            put<EDGE>(mp, e, left, m[k]);
+            put<EDGE>(vp, e, left, v);
+        }
+        if constexpr (FAST) {
+            v = v * kSecond;
+            r[k] = f4{root_in_range(v.x), root_in_range(v.y), root_in_range(v.z), root_in_range(v.w)};
+        } else {
+            r[k] = f4{sqrtf(v.x), sqrtf(v.y), sqrtf(v.z), sqrtf(v.w)};
+        }
+        if constexpr (BITS == 8) {
+            if (EDGE != kFull) {
+                clear_absent(m[k], e, left);
+                clear_absent(r[k], e, left);
+            }
+            m_most[k] = most_of(m[k]);
+            r_most[k] = most_of(r[k]);
+            if (FAST) over |= static_cast<uint32_t>(m_most[k] > __float_as_uint(kMostFirst)) | static_cast<uint32_t>(r_most[k] > __float_as_uint(kMostRoot));
+        }
+    }
+    if constexpr (FAST) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) asm volatile("" : "+v"(qp[k]));     // have arrived with the others, and are not asked for only now
+        if (__any(over != 0)) return false;
+    }
+    const float decay = d.decay * a.decay, root = a.root * (1.0f / kRoot), rate = a.rate * (1.0f / kFirst);
+    const uint32_t random = (static_cast<uint32_t>(e0 / 4) + lane) * kGolden + mix(d.index * kGolden + a.seed);
+    uint32_t h[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int e = k * kRow + lane * 4;
+        f4 p = widened<P>(in_place<EDGE>(qp[k], e, left));
+        const f4 b = r[k] * root + a.eps;
+        f4 u;
+        if constexpr (FAST) u = f4{quotient_in_range(m[k].x, b.x), quotient_in_range(m[k].y, b.y), quotient_in_range(m[k].z, b.z), quotient_in_range(m[k].w, b.w)};
+        else u = m[k] / b;
+        p = p - (u * rate + p * decay);
+        if (BITS == 8 || P == BAGUA_BF16) h[k] = mix(random + static_cast<uint32_t>(k) * (kRow / 4 * kGolden));
+        if constexpr (P == BAGUA_BF16) {
+            const uint32_t w = mix(h[k] + kGolden);
+            put<EDGE>(pp, e, left, h4{random_bf16(p.x, turned(w, 0)), random_bf16(p.y, turned(w, 8)), random_bf16(p.z, turned(w, 16)),
+                                      random_bf16(p.w, turned(w, 24))});
+        } else {
+            put<EDGE>(pp, e, left, p);
+        }
+        if constexpr (C >= 0) put<EDGE>(table_ptr<typename Elem<C>::one>(d.copy) + e0, e, left, narrowed<C>(p));
+    }
+    if constexpr (BITS == 8) {
+        constexpr int kLanes = kWave / K;      // that have a block's largest value
+        const Scale sm = scale_of(__uint_as_float(blocks_most<K>(m_most)) * (1.0f / kFirst)), sv = scale_of(__uint_as_float(blocks_most<K>(r_most)) * (1.0f / kRoot));
+        const float im = sm.inverse * (1.0f / kFirst), iv = sv.inverse * (1.0f / kRoot);
+        auto of_block = [&](float x, int k) { return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_readlane(__float_as_int(x), k * kLanes))); };
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int e = k * kRow + lane * 4;
+            const f4 y = r[k] * of_block(iv, k);
+            const u16x2 lo = two_codes(code_bits(y.x, turned(h[k], 0)), code_bits(y.y, turned(h[k], 8)), r[k].x, r[k].y);
+            const u16x2 hi = two_codes(code_bits(y.z, turned(h[k], 16)), code_bits(y.w, turned(h[k], 24)), r[k].z, r[k].w);
+            put<EDGE>(mp, e, left, __builtin_bit_cast(Four<uint8_t>::v, nearest_codes(m[k] * of_block(im, k))));
+            put<EDGE>(vp, e, left, __builtin_bit_cast(Four<uint8_t>::v, __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x06040200u)));
+        }
+        if (lane % kLanes == 0 && (EDGE == kFull || lane / kLanes * kRow < left)) {
+            table_ptr<float>(d.m_scale)[e0 / kRow + lane / kLanes] = sm.scale;
+            table_ptr<float>(d.v_scale)[e0 / kRow + lane / kLanes] = sv.scale;
+        }
+    }
+    return true;
+}
+
 template <int G, int P, int C, int BITS>
-__global__ void __launch_bounds__(kWave * kRowWaves)
+__global__ void __launch_bounds__(kWave)
 k_adamw(const TensorEntry* __restrict__ entries, const uint32_t* __restrict__ tile_tensor, AdamArgs a)
 {
-    const uint32_t row = blockIdx.x * kRowWaves + wave_index();
-    if (row >= a.rows) return;
-    const uint32_t tile = row / kTileRows;
+    constexpr int K = share_rows(BITS), kElements = K * kRow, kShares = kTensorTile / kElements;     // of a share; of a tile
+    const uint32_t tile = blockIdx.x / kShares;
     const TensorEntry d = entries[tile_tensor[tile]];
-    const size_t e0 = static_cast<size_t>(tile - d.first_tile) * kTensorTile + (row % kTileRows) * kRow;
+    const size_t e0 = static_cast<size_t>(tile - d.first_tile) * kTensorTile + blockIdx.x % kShares * kElements;
     if (e0 >= d.numel) return;
     float factor = 1.0f;
     if (a.clip) {
         if (!(fabsf(a.clip[0]) < INFINITY)) return;
         factor = a.clip[1];
     }
-    const int lane = threadIdx.x & 63;
-    const int remain = d.numel - e0 < static_cast<size_t>(kRow) ? static_cast<int>(d.numel - e0) : kRow;
-    typedef typename Elem<P>::one param_t;
-    param_t* pp = table_ptr<param_t>(d.param) + e0;
-
-    f4 p = load_four<P>(pp, lane, remain);
-    f4 g = load_four<G>(table_ptr<const typename Elem<G>::one>(d.grad) + e0, lane, remain);
-    f4 m, v;
-    if (BITS == 32) {
-        m = load_four<BAGUA_F32>(table_ptr<const float>(d.m) + e0, lane, remain);
-        v = load_four<BAGUA_F32>(table_ptr<const float>(d.v) + e0, lane, remain);
-    } else {
-        const size_t block = e0 / kRow;
-        m = widen_codes(load_four_codes(table_ptr<const uint8_t>(d.m) + e0, lane, remain), table_ptr<const float>(d.m_scale)[block]);
-        const f4 r = widen_codes(load_four_codes(table_ptr<const uint8_t>(d.v) + e0, lane, remain), table_ptr<const float>(d.v_scale)[block]);
-        v = r * r;
-    }
-    if (a.clip) g = g * factor;
-    m = m * a.beta1 + g * a.omb1;
-    v = v * a.beta2 + (g * g) * a.omb2;
-    const f4 r = f4{sqrtf(v.x), sqrtf(v.y), sqrtf(v.z), sqrtf(v.w)};
-    const f4 u = m / (r * a.root + a.eps);
-    p = p - (u * a.rate + p * (d.decay * a.decay));
-
-    uint32_t h = 0;
-    if (BITS == 8 || P == BAGUA_BF16)
-        h = mix((static_cast<uint32_t>(e0 / 4) + lane) * kGolden + mix(d.index * kGolden + a.seed));
-    if (BITS == 32) {
-        store_four<BAGUA_F32>(table_ptr<float>(d.m) + e0, lane, remain, m);
-        store_four<BAGUA_F32>(table_ptr<float>(d.v) + e0, lane, remain, v);
-    } else {
-        // the absent elements of a last row hold 0
-        const Scale ms = scale_of(wave_reduce(max4(abs4(m)), OpMaxF())), vs = scale_of(wave_reduce(max4(r), OpMaxF()));
-        const f4 y = r * vs.inverse;
-        const uint32_t w = random_code(y.x, r.x, turned(h, 0)) | random_code(y.y, r.y, turned(h, 8)) << 8 |
-                           random_code(y.z, r.z, turned(h, 16)) << 16 | random_code(y.w, r.w, turned(h, 24)) << 24;
-        store_four_codes(table_ptr<uint8_t>(d.m) + e0, lane, remain, nearest_codes(m * ms.inverse));
-        store_four_codes(table_ptr<uint8_t>(d.v) + e0, lane, remain, w);
-        if (lane == 0) {
-            table_ptr<float>(d.m_scale)[e0 / kRow] = ms.scale;
-            table_ptr<float>(d.v_scale)[e0 / kRow] = vs.scale;
-        }
-    }
-    if constexpr (P == BAGUA_BF16) {
-        const uint32_t h2 = mix(h + kGolden);
-        const h4 q = h4{random_bf16(p.x, turned(h2, 0)), random_bf16(p.y, turned(h2, 8)), random_bf16(p.z, turned(h2, 16)), random_bf16(p.w, turned(h2, 24))};
-        const int e = lane * 4;
-        if (remain >= kRow) {
-            __builtin_nontemporal_store(static_cast<h4e>(q), reinterpret_cast<h4e*>(pp + e));
+    const int lane = threadIdx.x;
+    const size_t left = d.numel - e0;
+    if (left >= static_cast<size_t>(kElements)) {
+        if constexpr (BITS == 8) {
+            if (a.in_range && adamw_share<G, P, C, BITS, K, kFull, true>(d, e0, lane, kElements, factor, a)) return;
+            // rare: reads for itself, keeps nothing in registers up to here, and does with few
+            asm volatile("" ::: "memory");
+#pragma unroll 1
+            for (int k = 0; k < K; ++k) adamw_share<G, P, C, BITS, 1, kFull, false>(d, e0 + k * kRow, lane, kRow, factor, a);
         } else {
-            if (e + 0 < remain) pp[e + 0] = q.x;
-            if (e + 1 < remain) pp[e + 1] = q.y;
-            if (e + 2 < remain) pp[e + 2] = q.z;
-            if (e + 3 < remain) pp[e + 3] = q.w;
+            adamw_share<G, P, C, BITS, K, kFull, false>(d, e0, lane, kElements, factor, a);
         }
+    } else if (left >= 4) {
+        adamw_share<G, P, C, BITS, K, kCut, false>(d, e0, lane, static_cast<int>(left), factor, a);
     } else {
-        store_four<P>(pp, lane, remain, p);
+        adamw_share<G, P, C, BITS, 1, kFew, false>(d, e0, lane, static_cast<int>(left), factor, a);
     }
-    if constexpr (C >= 0) store_four<C>(table_ptr<typename Elem<C>::one>(d.copy) + e0, lane, remain, p);
 }
 
 // ---------------------------------------------------------------- norm
@@ -231,11 +381,20 @@ k_grad_norm(TensorPlanView plan, uint32_t tiles, double scale, double max_norm, 
         const size_t left = d.numel - e0;
         f4 x[kTileRows];
         if (left >= kTensorTile) {
+            typename Four<typename Elem<G>::one>::v q[kTileRows];
 #pragma unroll
-            for (int i = 0; i < kTileRows; ++i) x[i] = Elem<G>::load(g + i * kRow + lane * 4);
+            for (int i = 0; i < kTileRows; ++i) q[i] = fetch<kFull>(g + i * kRow, lane * 4, kRow);
+#pragma unroll
+            for (int i = 0; i < kTileRows; ++i) x[i] = widened<G>(q[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < kTileRows; ++i) x[i] = load_four<G>(g + i * kRow, lane, static_cast<int>(left) - i * kRow);
+            for (int i = 0; i < kTileRows; ++i) {
+                const int remain = static_cast<int>(left) - i * kRow;
+                x[i] = f4{0.f, 0.f, 0.f, 0.f};
+                if (remain <= 0) continue;
+                x[i] = widened<G>(fetch<kFew>(g + i * kRow, lane * 4, remain));
+                clear_absent(x[i], lane * 4, remain);
+            }
         }
 #pragma unroll
         for (int i = 0; i < kTileRows; ++i)
@@ -413,14 +572,15 @@ extern "C" int bagua_adamw_step(const bagua_tensor_plan_t* plan, uint64_t step, 
     if (!aligned4(clip)) return BAGUA_ERR_ALIGNMENT;
     if (plan->tiles == 0) return BAGUA_OK;
     const TensorPlanView view = tensor_plan_view(plan);
-    const uint32_t rows = static_cast<uint32_t>(plan->tiles * kTileRows);
+    const uint32_t groups = static_cast<uint32_t>(plan->tiles * (kTileRows / share_rows(plan->state_bits)));
     const double t = static_cast<double>(step);
+    const float root = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(beta2, t)));
     const AdamArgs a{clip, static_cast<float>(beta1), static_cast<float>(1.0 - beta1), static_cast<float>(beta2), static_cast<float>(1.0 - beta2),
-                     static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(beta2, t))), static_cast<float>(eps),
-                     static_cast<float>(lr / (1.0 - std::pow(beta1, t))), static_cast<float>(lr * weight_decay), seed, rows};
+                     root, static_cast<float>(eps),
+                     static_cast<float>(lr / (1.0 - std::pow(beta1, t))), static_cast<float>(lr * weight_decay), seed, in_range(root, static_cast<float>(eps))};
     const AdamKernel kernel = plan->state_bits == 32 ? pick_adamw<32>(plan->grad_type, plan->param_type, plan->copy_type)
                                                      : pick_adamw<8>(plan->grad_type, plan->param_type, plan->copy_type);
-    launch_kernel(kernel, dim3((rows + kRowWaves - 1) / kRowWaves), dim3(kWave * kRowWaves), 0, static_cast<hipStream_t>(stream), view.entry,
+    launch_kernel(kernel, dim3(groups), dim3(kWave), 0, static_cast<hipStream_t>(stream), view.entry,
                   view.tile_tensor, a);
     return launch_status();
 }

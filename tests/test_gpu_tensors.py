@@ -326,6 +326,44 @@ def test_a_norm_that_is_not_finite_changes_nothing(bg):
         assert not torch.equal(before[0], p)
 
 
+@pytest.mark.parametrize("eps", [0.0, 1e-13, 1e-8, 0.5, 3.0])
+@pytest.mark.parametrize("beta2", [0.5, 0.999, 0.99999999])
+def test_8_bits_over_the_whole_range(bg, eps, beta2):
+    """Whole tiles of blocks that are tiny, ordinary and huge: within the range of the short square root and quotient, outside it, and
+    across its edges in one tile.  Bit for bit as the operations of any range."""
+    n, f = 64 * 256, np.float32
+    r = np.random.default_rng(int(eps * 1000) + int(beta2 * 1e8))
+    size = 10.0 ** np.linspace(-17, 17, 64)[r.permutation(64)]
+    size[:8] = [2.0 ** -30, 2.0 ** 10, 2.0 ** 20, 2.0 ** 21, 2.0 ** 23, 2.0 ** 24, 1.0, 1.0]
+    grads = [(r.standard_normal(n) * np.repeat(size, 256)).astype(f) for _ in range(3)]
+    for g in grads:
+        g[g == 0] = 1.0
+        if eps > 0:
+            g.reshape(64, 256)[7:9, ::3] = 0.0
+    P = r.standard_normal(n).astype(f)
+    p, m, v = torch.from_numpy(P.copy()).cuda(), torch.zeros(n, device="cuda").to(F8), torch.zeros(n, device="cuda").to(F8)
+    ms, vs, g = torch.zeros(64, device="cuda"), torch.zeros(64, device="cuda"), torch.zeros(n, device="cuda")
+    plan = plan_of(bg, [n], [g], params=[p], m=[m], v=[v], m_scales=[ms], v_scales=[vs])
+    M, V = np.zeros(n, f), np.zeros(n, f)
+    hyper = dict(lr=1e-3, beta1=0.9, beta2=beta2, eps=eps, weight_decay=0.1)
+    for t in (1, 2, 3):
+        g.copy_(torch.from_numpy(grads[t - 1]).cuda())
+        bg.bagua_adamw_step(plan, t, seed=t, **hyper)
+        with np.errstate(divide="ignore", invalid="ignore"):      # without eps a square that underflows leaves m / 0
+            P, M, V, root = step_in_fp32(P, grads[t - 1], M, V, t, None, 1.0, **hyper)
+        got = p.cpu().numpy()
+        assert np.all((got.view(np.uint32) == P.view(np.uint32)) | (np.isnan(got) & np.isnan(P)))
+        s, inv = scales(M)
+        codes = nearest_code(M * np.repeat(inv, 256))
+        assert np.array_equal(ms.cpu().numpy(), s) and np.array_equal(m.view(torch.uint8).cpu().numpy(), codes)
+        M = decode(codes, s)
+        s, inv = scales(root)
+        c = (((root * np.repeat(inv, 256)) * f(2.0 ** -120)).view(np.uint32) + (hashes(n, 0, t)[0] >> np.uint32(12))) >> np.uint32(20)
+        c = np.where(root > 0, c.clip(1, 126), 0).astype(np.uint8)
+        assert np.array_equal(vs.cpu().numpy(), s) and np.array_equal(v.view(torch.uint8).cpu().numpy(), c)
+        V = decode(c, s) ** 2
+
+
 def test_tiny_and_huge_blocks_in_8_bits(bg):
     """Blocks whose first moment is below what a scale can hold are stored as 0; a root above zero never becomes zero."""
     n = 1024
