@@ -212,13 +212,12 @@ __device__ __forceinline__ void balance_loss(const BalanceOut& o, int32_t tokens
         o.weight[e] = static_cast<float>(w);
         if (tokens > 0) sum += w * prob(e);
     }
-#pragma unroll
-    for (int s = 32; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
+    sum = wave_sum(sum);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x / kWave] = sum;
     __syncthreads();
-    if (threadIdx.x != 0) return;
-    for (int w = 1; w < THREADS / kWave; ++w) sum += part[w];
-    o.loss[0] = static_cast<float>(sum);
+    if (threadIdx.x >= kWave) return;
+    sum = wave_sum(threadIdx.x < THREADS / kWave ? part[threadIdx.x] : 0.0);
+    if (threadIdx.x == 0) o.loss[0] = static_cast<float>(sum);
 }
 
 constexpr int kSumFloats = 8192;   // of LDS for the waves' sums

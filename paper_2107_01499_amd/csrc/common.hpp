@@ -369,6 +369,20 @@ __device__ __forceinline__ T wave_reduce(T v, const F& op)
     v = op(v, dpp<kBcast31>(v));
     return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
+// The sum over the wave in 64 bits, in every lane: rows of 16 lanes by exchanges as above, then the four rows.
+__device__ __forceinline__ double wave_sum(double v)
+{
+    auto of = [](double x, auto exchange) {
+        const uint64_t b = __builtin_bit_cast(uint64_t, x);
+        return __builtin_bit_cast(double, static_cast<uint64_t>(exchange(static_cast<uint32_t>(b >> 32))) << 32 | exchange(static_cast<uint32_t>(b)));
+    };
+    v += of(v, [](uint32_t x) { return dpp<kXor1>(x); });
+    v += of(v, [](uint32_t x) { return dpp<kXor2>(x); });
+    v += of(v, [](uint32_t x) { return dpp<kHalfMirror>(x); });
+    v += of(v, [](uint32_t x) { return dpp<kMirror>(x); });
+    auto row = [&](int i) { return of(v, [&](uint32_t x) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(x), 16 * i)); }); };
+    return (row(0) + row(1)) + (row(2) + row(3));
+}
 struct OpMinF { __device__ __forceinline__ float operator()(float a, float b) const { return fminf(a, b); } };
 struct OpMaxF { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 struct OpAddF { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };

@@ -27,10 +27,29 @@ constexpr int kTileRows = kTensorTile / kRow;
 #ifndef BAGUA_ADAM32_ROWS
 #define BAGUA_ADAM32_ROWS 1
 #endif
+// Waves of a long launch with 32-bit states that share a CU (see lds_for_residency): more of them only spread what is in flight over more
+// pages.  0 (as many as fit) | 11 | 12 | 13 | 16 waves: 335 M elements, bf16 gradients and copies, 1480 .. 1523 | 1433 | 1429 .. 1437 | 1456 | 1440 ..
+// 1449 us, fp32 1479 | 1473 | 1467 | 1480 | 1497, bf16 parameters 1183 | 1200 | 1154 | 1138 | 1137; 109 M, bf16 gradients and copies, 477 | 466 | 472 |
+// 474 | 480; 25.6 M fp32 111.1 | 109.6 | 110.4 | 110.8 | 110.7.  Shorter launches lose: 5 M, bf16 gradients and copies, 24.8 -> 25.1, 1 M fp32 6.8 -> 7.1.
+// With 8-bit states, which need the waves for their arithmetic, 16 lose 10 % and more.
+inline size_t adamw_lds(size_t tiles, int param_type, int bits)
+{
+    if (bits != 32 || tiles < (static_cast<size_t>(1) << 24) / kTensorTile) return 0;
+    return lds_for_residency(param_type == BAGUA_F32 ? 12 : 16);
+}
 static_assert((BAGUA_ADAM8_ROWS == 1 || BAGUA_ADAM8_ROWS == 2 || BAGUA_ADAM8_ROWS == 4) && (BAGUA_ADAM32_ROWS == 1 || BAGUA_ADAM32_ROWS == 2 || BAGUA_ADAM32_ROWS == 4),
               "rows that divide a tile");
-constexpr unsigned kNormGroups = 2048;    // most workgroups of the norm: eight waves of four on every SIMD
-constexpr unsigned kNormWaves = 4;
+// The norm: one workgroup on a CU, with the waves that keep 32 KB of loads in flight there.  More waves read no faster, and each group more
+// is one more that has to be counted at the end, 13 ns apiece: 335 M fp32 elements, 2048 groups of 4 waves 215 us, 512 of 8 197, 512 of
+// 4 191, 256 of 8 192; bf16, 256 groups of 8 142, of 16 100; 25.6 M bf16, 2048 groups of 4 32.3, 256 of 16 14.3.
+constexpr unsigned kNormGroups = kCus;
+constexpr unsigned norm_waves(int type) { return type == BAGUA_F32 ? 8 : 16; }
+// Up to four tiles a wave, one group alone is faster than several that have to meet: 20 K elements in 30 tensors 4.5 -> 3.5 us, 5 K 4.3 ->
+// 3.4; 41 K in 49 tensors (eight tiles a wave) 4.9 -> 6.8.
+inline unsigned norm_groups(size_t tiles, unsigned waves)
+{
+    return tiles <= 4 * waves ? 1 : static_cast<unsigned>(std::min<size_t>((tiles + waves - 1) / waves, kNormGroups));
+}
 
 struct TensorEntry {
     uint64_t grad, param, m, v, m_scale, v_scale, copy, numel;
@@ -366,62 +385,83 @@ k_adamw(const TensorEntry* __restrict__ entries, const uint32_t* __restrict__ ti
 
 // ---------------------------------------------------------------- norm
 // Squares are exact in 64 bits and their sum loses nothing that an fp32 result could show, whatever the order; 64-bit additions
-// run at half the rate of fp32 ones, a twentieth of what the loads leave time for.  Each workgroup sums every gridDim-th tile;
-// the workgroup that finishes last adds the groups' sums in ascending order.
+// run at half the rate of fp32 ones, a twentieth of what the loads leave time for.  A wave takes every so many-th tile, and looks up the
+// next one while the present one is on its way; the workgroup that finishes last adds the groups' sums in a fixed order.
 template <int G>
-__global__ void __launch_bounds__(kWave * kNormWaves)
+__device__ __forceinline__ double add_squares(double sum, const typename Four<typename Elem<G>::one>::v (&q)[kTileRows], int lane, int left)
+{
+    double part[4] = {sum, 0.0, 0.0, 0.0};
+#pragma unroll
+    for (int i = 0; i < kTileRows; ++i) {
+        f4 x = widened<G>(q[i]);
+        if (left < kTensorTile) clear_absent(x, i * kRow + lane * 4, left);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const double y = static_cast<double>(x[j]);
+            part[j] = __builtin_fma(y, y, part[j]);
+        }
+    }
+    return (part[0] + part[1]) + (part[2] + part[3]);
+}
+template <int G>
+__global__ void __launch_bounds__(kWave * norm_waves(G))
 k_grad_norm(TensorPlanView plan, uint32_t tiles, double scale, double max_norm, float* __restrict__ out)
 {
+    typedef typename Elem<G>::one one;
+    constexpr unsigned kNormWaves = norm_waves(G);
     const int lane = threadIdx.x & 63, wave = wave_index();
+    const uint32_t step = gridDim.x * kNormWaves;
     double sum = 0.0;
-    for (uint32_t tile = blockIdx.x * kNormWaves + wave; tile < tiles; tile += gridDim.x * kNormWaves) {
-        const TensorEntry d = plan.entry[plan.tile_tensor[tile]];
-        const size_t e0 = static_cast<size_t>(tile - d.first_tile) * kTensorTile;
-        const typename Elem<G>::one* g = table_ptr<const typename Elem<G>::one>(d.grad) + e0;
-        const size_t left = d.numel - e0;
-        f4 x[kTileRows];
-        if (left >= kTensorTile) {
-            typename Four<typename Elem<G>::one>::v q[kTileRows];
+    uint32_t tile = blockIdx.x * kNormWaves + wave;
+    if (tile < tiles) {
+        TensorEntry d = plan.entry[plan.tile_tensor[tile]];
+        for (;;) {
+            const size_t e0 = static_cast<size_t>(tile - d.first_tile) * kTensorTile;
+            const one* g = table_ptr<const one>(d.grad) + e0;
+            const int left = static_cast<int>(min(d.numel - e0, static_cast<uint64_t>(kTensorTile)));
+            typename Four<one>::v q[kTileRows];
+            if (left == kTensorTile) {
 #pragma unroll
-            for (int i = 0; i < kTileRows; ++i) q[i] = fetch<kFull>(g + i * kRow, lane * 4, kRow);
+                for (int i = 0; i < kTileRows; ++i) q[i] = fetch<kFull>(g, i * kRow + lane * 4, left);
+            } else if (left >= 4) {
 #pragma unroll
-            for (int i = 0; i < kTileRows; ++i) x[i] = widened<G>(q[i]);
-        } else {
+                for (int i = 0; i < kTileRows; ++i) q[i] = fetch<kCut>(g, i * kRow + lane * 4, left);
+            } else {
 #pragma unroll
-            for (int i = 0; i < kTileRows; ++i) {
-                const int remain = static_cast<int>(left) - i * kRow;
-                x[i] = f4{0.f, 0.f, 0.f, 0.f};
-                if (remain <= 0) continue;
-                x[i] = widened<G>(fetch<kFew>(g + i * kRow, lane * 4, remain));
-                clear_absent(x[i], lane * 4, remain);
+                for (int i = 0; i < kTileRows; ++i) q[i] = fetch<kFew>(g, i * kRow + lane * 4, left);
             }
+            tile += step;
+            const bool more = tile < tiles;
+            if (more) d = plan.entry[plan.tile_tensor[tile]];
+            if (left >= 4 && left < kTensorTile) {
+#pragma unroll
+                for (int i = 0; i < kTileRows; ++i) q[i] = in_place<kCut>(q[i], i * kRow + lane * 4, left);
+            }
+            sum = add_squares<G>(sum, q, lane, left);
+            if (!more) break;
         }
-#pragma unroll
-        for (int i = 0; i < kTileRows; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const double y = static_cast<double>(x[i][j]);
-                sum = __builtin_fma(y, y, sum);
-            }
     }
-#pragma unroll
-    for (int s = 32; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
     __shared__ double part[kNormWaves];
     __shared__ bool last;
-    if (lane == 0) part[wave] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) publish(plan.partial + blockIdx.x, (part[0] + part[1]) + (part[2] + part[3]));
-    if (!last_to_arrive(plan.counter, &last)) return;
-    sum = 0.0;
-#pragma unroll 8
-    for (uint32_t i = threadIdx.x; i < gridDim.x; i += kWave * kNormWaves) sum += plan.partial[i];
-#pragma unroll
-    for (int s = 32; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
-    if (lane == 0) part[wave] = sum;
-    __syncthreads();
+    auto group_sum = [&](double x) {      // in thread 0
+        x = wave_sum(x);
+        if (lane == 0) part[wave] = x;
+        __syncthreads();
+        x = threadIdx.x < kNormWaves ? part[threadIdx.x] : 0.0;
+        return wave == 0 ? wave_sum(x) : 0.0;
+    };
+    sum = group_sum(sum);
+    if (gridDim.x > 1) {
+        if (threadIdx.x == 0) publish(plan.partial + blockIdx.x, sum);
+        if (!last_to_arrive(plan.counter, &last)) return;
+        sum = 0.0;
+        static_assert(kNormGroups <= kWave * kNormWaves, "a thread for every group");
+        sum = threadIdx.x < gridDim.x ? plan.partial[threadIdx.x] : 0.0;
+        sum = group_sum(sum);
+        if (threadIdx.x == 0) __hip_atomic_store(plan.counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next call
+    }
     if (threadIdx.x != 0) return;
-    __hip_atomic_store(plan.counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next call
-    const double n = scale * sqrt((part[0] + part[1]) + (part[2] + part[3]));
+    const double n = scale * sqrt(sum);
     const float norm = static_cast<float>(n);
     out[0] = norm;
     const double c = max_norm / (n + 1e-6);
@@ -535,8 +575,8 @@ extern "C" int bagua_grad_norm(const bagua_tensor_plan_t* plan, double grad_scal
 {
     if (!plan_ok(plan) || !out || !(std::fabs(grad_scale) < INFINITY) || !(max_norm >= 0.0)) return BAGUA_ERR_INVALID_ARG;
     if (!aligned4(out)) return BAGUA_ERR_ALIGNMENT;
-    const size_t groups = (plan->tiles + kNormWaves - 1) / kNormWaves;
-    const dim3 grid(static_cast<unsigned>(std::min<size_t>(std::max<size_t>(groups, 1), kNormGroups))), block(kWave * kNormWaves);
+    const unsigned waves = norm_waves(plan->grad_type);
+    const dim3 grid(norm_groups(plan->tiles, waves)), block(kWave * waves);
     const TensorPlanView view = tensor_plan_view(plan);
     auto* kernel = plan->grad_type == BAGUA_F32 ? k_grad_norm<BAGUA_F32> : plan->grad_type == BAGUA_BF16 ? k_grad_norm<BAGUA_BF16> : k_grad_norm<BAGUA_F16>;
     launch_kernel(kernel, grid, block, 0, static_cast<hipStream_t>(stream), view, static_cast<uint32_t>(plan->tiles), grad_scale, max_norm, out);
@@ -580,7 +620,7 @@ extern "C" int bagua_adamw_step(const bagua_tensor_plan_t* plan, uint64_t step, 
                      static_cast<float>(lr / (1.0 - std::pow(beta1, t))), static_cast<float>(lr * weight_decay), seed, in_range(root, static_cast<float>(eps))};
     const AdamKernel kernel = plan->state_bits == 32 ? pick_adamw<32>(plan->grad_type, plan->param_type, plan->copy_type)
                                                      : pick_adamw<8>(plan->grad_type, plan->param_type, plan->copy_type);
-    launch_kernel(kernel, dim3(groups), dim3(kWave), 0, static_cast<hipStream_t>(stream), view.entry,
+    launch_kernel(kernel, dim3(groups), dim3(kWave), adamw_lds(plan->tiles, plan->param_type, plan->state_bits), static_cast<hipStream_t>(stream), view.entry,
                   view.tile_tensor, a);
     return launch_status();
 }
