@@ -485,8 +485,8 @@ int bagua_adamw_step(const bagua_tensor_plan_t* plan, uint64_t step, double lr, 
  *   counts    device int32[experts + 1], written: C_e, and N behind them
  *   prob      device fp32[experts], written: S_e
  *   loss, weight   device fp32[1], fp32[experts], written; NULL together where other GPUs' sums are still to be added
- *   workspace device, >= bagua_balance_workspace_bytes(experts) bytes, 16-byte aligned.  Its first 64 bytes must be 0 before the
- *             first call; every call leaves them so.  Calls on one workspace must not overlap in time.
+ *   workspace device, >= bagua_balance_workspace_bytes(experts) bytes, 16-byte aligned.  It must be 0 before the first call; a call
+ *             leaves it fit for the next.  Calls on one workspace must not overlap in time.
  *   limits    1 <= k <= BAGUA_MAX_WORKERS, experts <= BAGUA_MAX_EXPERTS, top_k <= experts, all choices together below 2^31
  * bagua_balance_loss: loss and weights from counts and prob that were added up over GPUs.
  * bagua_balance_grad: backward; dlogits[i] (rows ld_out apart) = *upstream * d loss / d x, 0 for padding.  upstream: device

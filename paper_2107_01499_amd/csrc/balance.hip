@@ -5,6 +5,7 @@
 // more (in bounds, whatever the length): these are left out of the sums by a factor of 0, and where they are stored both lanes
 // store the same bits.
 #include <cmath>
+#include <type_traits>
 
 #include "batch.hpp"
 #include "elements.hpp"
@@ -14,6 +15,7 @@
 namespace bagua {
 
 constexpr unsigned kBalanceGroups = kCus;    // most workgroups of the forward pass: the last one adds up their sums
+static_assert(kBalanceGroups <= kArriveMost, "groups that can be counted");
 constexpr int kGradWaves = 4;
 constexpr uint32_t kGradMostWaves = 65536;   // of a launch of the backward pass
 
@@ -22,7 +24,7 @@ struct Workers {
     const void* ids[BAGUA_MAX_WORKERS];      // of the backward pass: where the gradients go
     const uint8_t* mask[BAGUA_MAX_WORKERS];
     uint32_t tokens[BAGUA_MAX_WORKERS];
-    uint32_t first_unit[BAGUA_MAX_WORKERS + 1];   // a unit: the rows that a wave holds at a time
+    uint32_t first_tile[BAGUA_MAX_WORKERS + 1];   // a tile: the rows, of one worker, that a wave has in flight together
     uint32_t k;
 };
 
@@ -33,27 +35,44 @@ struct Raw<T, 1> {
     typedef T v __attribute__((ext_vector_type(1), aligned(sizeof(T))));
 };
 template <typename T>
+struct Raw<T, 4> {
+    typedef T v __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+};
+template <typename T>
 struct Raw<T, 8> {
     typedef T v __attribute__((ext_vector_type(8), aligned(sizeof(T))));
 };
 
 // op over the L lanes of a row, in every one of them.
-template <int L, typename F>
-__device__ __forceinline__ float lanes_reduce(float v, const F& op)
+template <int L, typename T, typename F>
+__device__ __forceinline__ T lanes_reduce(T v, const F& op)
 {
     if (L >= 2) v = op(v, dpp<kXor1>(v));
     if (L >= 4) v = op(v, dpp<kXor2>(v));
     if (L >= 8) v = op(v, dpp<kHalfMirror>(v));
     if (L >= 16) v = op(v, dpp<kMirror>(v));
     if (L >= 32) {
-        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        const uint32_t b = __builtin_bit_cast(uint32_t, v);
+        const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+        v = op(__builtin_bit_cast(T, static_cast<uint32_t>(r[0])), __builtin_bit_cast(T, static_cast<uint32_t>(r[1])));
     }
     if (L >= 64) {
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        const uint32_t b = __builtin_bit_cast(uint32_t, v);
+        const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+        v = op(__builtin_bit_cast(T, static_cast<uint32_t>(r[0])), __builtin_bit_cast(T, static_cast<uint32_t>(r[1])));
     }
     return v;
+}
+
+// The largest over the L lanes of a row.  Numbers are ordered as integers once those below zero have their other bits turned, and the
+// integer maximum takes another lane's value in the same instruction, where that of numbers takes three to make a NaN quiet.
+struct OpMaxI { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return static_cast<uint32_t>(max(static_cast<int32_t>(a), static_cast<int32_t>(b))); } };
+__device__ __forceinline__ uint32_t in_order(uint32_t bits) { return bits ^ (static_cast<uint32_t>(static_cast<int32_t>(bits) >> 31) & 0x7fffffffu); }
+template <int L>
+__device__ __forceinline__ float lanes_most(float x)
+{
+    if (L == 1) return x;
+    return __uint_as_float(in_order(lanes_reduce<L>(in_order(__float_as_uint(x)), OpMaxI())));
 }
 
 constexpr int kRor1 = 0x121, kRor2 = 0x122, kRor4 = 0x124, kRor8 = 0x128;   // lane l reads l + 1, ... of its row of 16, around its end
@@ -96,33 +115,34 @@ struct Row {
             if (there) q[j] = __builtin_nontemporal_load(reinterpret_cast<const raw*>(row + at(j, experts)));
         }
     }
-    // e = exp(x - max) of the lane's elements; the value: 1 / sum of the row's.
-    __device__ __forceinline__ float exponentials(const float (&own)[NV][VEC], float (&e)[NV][VEC]) const
+    // The lane's elements as fp32, and the row's largest.
+    __device__ __forceinline__ float largest(float (&x)[NV][VEC]) const
     {
-        float most = -INFINITY, sum = 0.0f;
+        float most = -INFINITY;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                e[j][i] = Elem<TYPE>::widen(q[j][i]);
-                most = fmaxf(most, e[j][i]);
+                x[j][i] = Elem<TYPE>::widen(q[j][i]);
+                most = fmaxf(most, x[j][i]);
             }
-        most = lanes_reduce<L>(most, OpMaxF());
+        return lanes_most<L>(most);
+    }
+    // x = exp(x - most); the value: 1 / sum of the row's.
+    template <bool HUGE>
+    static __device__ __forceinline__ void exponentials(float (&x)[NV][VEC], float most)
+    {
         constexpr float kLog2e = 1.44269504088896340736f;
-        if (TYPE != BAGUA_F16 && __any(fabsf(most) > 0x1p126f)) {
-            // a largest one that leaves fp32 when it is multiplied: the type's lowest number (or -infinity) throughout a row
-            const float top = most == -INFINITY ? 0.0f : most;
+        const float top = most == -INFINITY ? 0.0f : most, shift = -top * kLog2e;   // (nothing but -infinity: all become 0)
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) e[j][i] = __builtin_amdgcn_exp2f((e[j][i] - top) * kLog2e);
-        } else {
-            const float shift = most == -INFINITY ? 0.0f : -most * kLog2e;    // its rounding is the same factor on all of a row
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) e[j][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(e[j][i], kLog2e, shift));
-        }
+            for (int i = 0; i < VEC; ++i)   // the rounding of the shift is the same factor on all of a row
+                x[j][i] = __builtin_amdgcn_exp2f(HUGE ? (x[j][i] - top) * kLog2e : __builtin_fmaf(x[j][i], kLog2e, shift));
+    }
+    static __device__ __forceinline__ float reciprocal_sum(const float (&own)[NV][VEC], const float (&e)[NV][VEC])
+    {
+        float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -140,15 +160,32 @@ struct Row {
     }
 };
 
-// The workers' table with worker i in lane i: which worker has a unit is one comparison and a count of bits, and what belongs to it
+// exp(x - largest) of a wave's U times rows, without a branch between them that would keep their exchanges from filling each other's gaps.
+template <typename R, int U, int NV, int VEC>
+__device__ __forceinline__ void exponentials_of(float (&e)[U][NV][VEC], const float (&most)[U], bool may_be_huge)
+{
+    bool huge = false;
+#pragma unroll
+    for (int u = 0; u < U; ++u) huge |= fabsf(most[u]) > 0x1p126f;
+    // a largest one that leaves fp32 when it is multiplied: the type's lowest number, or an infinity
+    if (may_be_huge && __any(huge)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) R::template exponentials<true>(e[u], most[u]);
+    } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) R::template exponentials<false>(e[u], most[u]);
+    }
+}
+
+// The workers' table with worker i in lane i: which worker has a tile is one comparison and a count of bits, and what belongs to it
 // is read from its lane.  (From the arguments that is a chain of scalar loads, a new one for every worker that is passed over.)
 struct LaneTable {
-    uint32_t first_unit, tokens;
+    uint32_t first_tile, tokens;
     uint64_t logits, other, mask;
     __device__ __forceinline__ explicit LaneTable(const Workers& ws)
     {
         const uint32_t i = threadIdx.x & (BAGUA_MAX_WORKERS - 1);
-        first_unit = ws.first_unit[i];
+        first_tile = ws.first_tile[i];
         tokens = ws.tokens[i];
         logits = reinterpret_cast<uintptr_t>(ws.logits[i]);
         other = reinterpret_cast<uintptr_t>(ws.ids[i]);
@@ -159,39 +196,41 @@ struct LaneTable {
     {
         return static_cast<uint64_t>(of(static_cast<uint32_t>(v >> 32), w)) << 32 | of(static_cast<uint32_t>(v), w);
     }
-    // The last worker whose units begin at `unit` or before it (of workers without tokens, which begin there too, the one behind them).
-    __device__ __forceinline__ uint32_t worker(uint32_t unit) const
+    // The last worker whose tiles begin at `tile` or before it (of workers without tokens, which begin there too, the one behind them).
+    __device__ __forceinline__ uint32_t worker(uint32_t tile) const
     {
-        return static_cast<uint32_t>(__popc(static_cast<uint32_t>(__ballot(first_unit <= unit)))) - 1u;
+        return static_cast<uint32_t>(__popc(static_cast<uint32_t>(__ballot(first_tile <= tile)))) - 1u;
     }
 };
 static_assert(BAGUA_MAX_WORKERS == 32, "a worker for each lane of half a wave");
 
-// A unit's rows: of one worker, from token t0 on.
-struct Unit {
-    uint64_t logits, other;
-    const uint8_t* flag;       // of the lane's own row; where there is no mask, or no such row, some other address that can be read
-    uint32_t t0, t, rows;      // t: the token of the lane's own row;  rows: that exist (one at least)
-    bool exists, masked;
+// A tile's rows: of one worker, from token t0 on; all of it wave-uniform.
+struct Tile {
+    uint64_t logits, other, mask;
+    uint32_t t0, rows;         // rows: that exist, one at least
+    bool there;                // false: beyond the last tile; its addresses are those of the last one, and can be read
 };
-template <int ROWS, int L>
-__device__ __forceinline__ Unit unit_of(const LaneTable& table, uint32_t unit, uint32_t units)
+template <int ROWS>
+__device__ __forceinline__ Tile tile_of(const LaneTable& table, uint32_t tile, uint32_t tiles)
 {
-    const bool there = unit < units;
-    unit = there ? unit : units - 1;
-    const uint32_t w = table.worker(unit), row = (threadIdx.x & 63) / L;
-    Unit u;
-    u.t0 = (unit - LaneTable::of(table.first_unit, w)) * ROWS;
-    u.rows = min(static_cast<uint32_t>(ROWS), LaneTable::of(table.tokens, w) - u.t0);
-    u.logits = LaneTable::of(table.logits, w);
-    u.other = LaneTable::of(table.other, w);
-    u.t = u.t0 + min(row, u.rows - 1);
-    u.exists = there && row < u.rows;
-    const uint64_t mask = LaneTable::of(table.mask, w);
-    u.masked = mask != 0;
-    u.flag = mask ? table_ptr<const uint8_t>(mask) + u.t : table_ptr<const uint8_t>(u.logits);
-    return u;
+    Tile k;
+    k.there = tile < tiles;
+    tile = k.there ? tile : tiles - 1;
+    const uint32_t w = table.worker(tile);
+    k.t0 = (tile - LaneTable::of(table.first_tile, w)) * ROWS;
+    k.rows = min(static_cast<uint32_t>(ROWS), LaneTable::of(table.tokens, w) - k.t0);
+    k.logits = LaneTable::of(table.logits, w);
+    k.other = LaneTable::of(table.other, w);
+    k.mask = LaneTable::of(table.mask, w);
+    return k;
 }
+// Whether a row of the tile counts, or an address to read instead where there is no mask or no such row.
+__device__ __forceinline__ uint8_t flag_of(const Tile& k, uint32_t row)
+{
+    const uint8_t* p = k.mask ? table_ptr<const uint8_t>(k.mask) + k.t0 + min(row, k.rows - 1) : table_ptr<const uint8_t>(k.logits);
+    return *p;
+}
+__device__ __forceinline__ bool counts_in(const Tile& k, uint32_t row, uint8_t flag) { return k.there && row < k.rows && (k.mask == 0 || flag != 0); }
 
 struct BalanceOut {
     int32_t* counts;
@@ -230,10 +269,10 @@ __host__ __device__ constexpr int sum_rows(int waves, int experts)
 }
 
 // The forward pass.  Dynamic LDS: float sums[sum_rows][experts], then uint32 counters[(experts + 1) << lg]: 2^lg copies of each, one of
-// which a lane adds to, so that popular experts are not waited for.  Workspace: counter (64 bytes), then every workgroup's sums and counts.
+// which a lane adds to, so that popular experts are not waited for.  Workspace: counters (last_to_arrive), then every workgroup's sums and counts.
 template <int TYPE, int VEC, int L, int NV, int UNROLL, int WAVES>
 __global__ void __launch_bounds__(kWave * WAVES)
-k_balance_stats(Workers ws, size_t ld, size_t ids_ld, int id_bytes, uint32_t units, uint32_t per_k, int lg, uint32_t* workspace, BalanceOut o)
+k_balance_stats(Workers ws, size_t ld, size_t ids_ld, int id_bytes, uint32_t tiles, uint32_t per_k, int lg, uint32_t* workspace, BalanceOut o)
 {
     typedef Row<TYPE, VEC, L, NV> R;
     constexpr int kThreads = kWave * WAVES;
@@ -252,51 +291,84 @@ k_balance_stats(Workers ws, size_t ld, size_t ids_ld, int id_bytes, uint32_t uni
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) acc[j][i] = 0.0f;
-    const uint32_t waves = gridDim.x * WAVES, top = static_cast<uint32_t>(o.top_k);
-    uint32_t tokens = 0;
-    for (uint32_t unit = blockIdx.x * WAVES + wave; unit < units; unit += UNROLL * waves) {
-        // All loads of the units are in flight together, and none stands behind a test: the rows' flags and the first 64 choices, then
-        // the rows.
-        Unit k[UNROLL];
-        R row[UNROLL];
-        uint8_t flag[UNROLL];
-        uint64_t id[UNROLL];
-        bool counts[UNROLL];
+    // A tile's choices are taken one after another, 64 at a time, whatever rows they belong to; kAhead times 64 are asked for with the rows.
+    constexpr int kRows = UNROLL * R::kRows, kAhead = NV == 1 ? 2 : 1;
+    const uint32_t waves = gridDim.x * WAVES, top = static_cast<uint32_t>(o.top_k), own_row = static_cast<uint32_t>(lane) / L;
+    struct Choice {
+        uint64_t id;
+        uint8_t flag;
+    };
+    auto row_of = [&](uint32_t i) { return per_k ? __umulhi(i, per_k) : i; };
+    auto choice = [&](const Tile& k, uint32_t i) {      // beyond the last one: the last
+        i = min(i, k.rows * top - 1);
+        const uint32_t r = row_of(i);
+        const size_t at = (k.t0 + r) * ids_ld + (i - r * top);
+        return Choice{id_bytes == 8 ? table_ptr<const uint64_t>(k.other)[at] : static_cast<uint64_t>(static_cast<int64_t>(table_ptr<const int32_t>(k.other)[at])),
+                      flag_of(k, r)};
+    };
+    auto count = [&](const Tile& k, Choice c, uint32_t i) {
+        if (c.id < static_cast<uint64_t>(experts) && counts_in(k, row_of(i), c.flag))
+            atomicAdd(counters + (static_cast<uint32_t>(c.id) << lg) + (lane & ((1 << lg) - 1)), 1u);
+    };
+    R row[UNROLL];
+    uint8_t flag[UNROLL];
+    Choice ahead[kAhead];
+    // No load stands behind a test of another one of the tile except the rows behind their flags.
+    auto ask = [&](const Tile& k) {
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) k[u] = unit_of<R::kRows, L>(table, unit + u * waves, units);
-        auto choice = [&](const Unit& n, uint32_t i) {      // choice i of the unit, of its row i / top; beyond the last one: the last
-            i = min(i, n.rows * top - 1);
-            const uint32_t r = per_k ? __umulhi(i, per_k) : i;
-            const size_t at = (n.t0 + r) * ids_ld + (i - r * top);
-            return id_bytes == 8 ? table_ptr<const uint64_t>(n.other)[at]
-                                 : static_cast<uint64_t>(static_cast<int64_t>(table_ptr<const int32_t>(n.other)[at]));
-        };
-        auto count = [&](uint64_t who, uint64_t rows, uint32_t i) {     // rows: bit L * r is set where row r counts
-            const uint32_t r = per_k ? __umulhi(i, per_k) : i;
-            if (who < static_cast<uint64_t>(experts) && r < R::kRows && (rows >> ((r * L) & 63) & 1))
-                atomicAdd(counters + (static_cast<uint32_t>(who) << lg) + (lane & ((1 << lg) - 1)), 1u);
-        };
+        for (int u = 0; u < UNROLL; ++u) flag[u] = flag_of(k, u * R::kRows + own_row);
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) flag[u] = *k[u].flag;
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) id[u] = choice(k[u], static_cast<uint32_t>(lane));
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) counts[u] = k[u].exists && (!k[u].masked || flag[u] != 0);
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) row[u].load(table_ptr<const typename R::one>(k[u].logits) + k[u].t * ld, experts, counts[u]);
+        for (int s = 0; s < kAhead; ++s) ahead[s] = choice(k, s * kWave + lane);
+    };
+    bool counts[UNROLL];
+    auto ask_rows = [&](const Tile& k) {
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            const uint64_t counting = __ballot(counts[u]);
-            tokens += __popcll(counting) / L;
-            count(id[u], counting, static_cast<uint32_t>(lane));
-            for (uint32_t i = kWave + lane; i < k[u].rows * top; i += kWave) count(choice(k[u], i), counting, i);
-            float e[NV][VEC];
-            float inverse = row[u].exponentials(own, e);
-            inverse = counts[u] ? inverse : 0.0f;         // (rows that do not count were read as zeros)
+            const uint32_t r = u * R::kRows + own_row;
+            counts[u] = counts_in(k, r, flag[u]);
+            row[u].load(table_ptr<const typename R::one>(k.logits) + (k.t0 + min(r, k.rows - 1)) * ld, experts, counts[u]);
+        }
+    };
+    uint32_t tokens = 0, tile = blockIdx.x * WAVES + wave;
+    if (tile < tiles) {
+        Tile k = tile_of<kRows>(table, tile, tiles);
+        ask(k);
+        ask_rows(k);
+        while (k.there) {
+            // the present tile's rows arrive; the next one's flags and choices, and then its rows, are on their way while the present
+            // one is worked on
+            tile += waves;
+            const Tile next = tile_of<kRows>(table, tile, tiles);
+            float e[UNROLL][NV][VEC], most[UNROLL];
+            bool counted[UNROLL];
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
+            for (int u = 0; u < UNROLL; ++u) {
+                counted[u] = counts[u];
+                most[u] = row[u].largest(e[u]);
+                tokens += __popcll(__ballot(counts[u])) / L;
+            }
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) acc[j][i] = __builtin_fmaf(e[j][i], inverse, acc[j][i]);
+            for (int s = 0; s < kAhead; ++s) count(k, ahead[s], s * kWave + lane);
+            for (uint32_t i0 = kAhead * kWave; i0 < k.rows * top; i0 += kAhead * kWave) {
+                Choice more[kAhead];
+#pragma unroll
+                for (int s = 0; s < kAhead; ++s) more[s] = choice(k, i0 + s * kWave + lane);
+#pragma unroll
+                for (int s = 0; s < kAhead; ++s) count(k, more[s], i0 + s * kWave + lane);
+            }
+            ask(next);
+            exponentials_of<R>(e, most, TYPE != BAGUA_F16);
+            ask_rows(next);
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                float inverse = R::reciprocal_sum(own, e[u]);
+                inverse = counted[u] ? inverse : 0.0f;      // (rows that do not count were read as zeros)
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) acc[j][i] = __builtin_fmaf(e[u][j][i], inverse, acc[j][i]);
+            }
+            k = next;
         }
     }
     if (lane == 0 && tokens) atomicAdd(counters + (experts << lg), tokens);
@@ -344,7 +416,7 @@ k_balance_stats(Workers ws, size_t ld, size_t ids_ld, int id_bytes, uint32_t uni
     }
 
     // [group][expert] of a sum and a count, and every group's tokens behind them
-    uint64_t* pairs = reinterpret_cast<uint64_t*>(workspace + 16);
+    uint64_t* pairs = reinterpret_cast<uint64_t*>(workspace + kArriveBytes / sizeof(uint32_t));
     uint32_t* group_tokens = reinterpret_cast<uint32_t*>(pairs + static_cast<size_t>(gridDim.x) * experts);
     for (int e = threadIdx.x; e < experts; e += kThreads)
         publish(pairs + blockIdx.x * experts + e, static_cast<uint64_t>(copies(e)) << 32 | __float_as_uint(wave_sums(e)));
@@ -396,7 +468,6 @@ k_balance_stats(Workers ws, size_t ld, size_t ids_ld, int id_bytes, uint32_t uni
     for (int s = 32; s > 0; s >>= 1) all += __shfl_xor(all, s);
     if (lane == 0 && all) atomicAdd(counters + experts, all);
     __syncthreads();
-    if (threadIdx.x == 0) __hip_atomic_store(workspace, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next call
     finish([&](int e) { return counters[e]; }, [&](int e) { return sums[e]; });
 }
 
@@ -410,8 +481,8 @@ k_balance_loss(const int32_t* __restrict__ counts, const float* __restrict__ pro
 
 // The backward pass: the probabilities are formed again from the logits, which are read anyway.
 template <int TYPE, int VEC, int L, int NV, int UNROLL>
-__global__ void __launch_bounds__(kWave * kGradWaves, NV == 1 ? 8 : 1)
-k_balance_grad(Workers ws, size_t ld, size_t ld_out, uint32_t units, int experts, const float* __restrict__ weight, const float* __restrict__ upstream)
+__global__ void __launch_bounds__(kWave * kGradWaves, NV == 1 ? 7 : 1)
+k_balance_grad(Workers ws, size_t ld, size_t ld_out, uint32_t tiles, int experts, const float* __restrict__ weight, const float* __restrict__ upstream)
 {
     typedef Row<TYPE, VEC, L, NV> R;
     typedef typename R::one one;
@@ -424,36 +495,41 @@ k_balance_grad(Workers ws, size_t ld, size_t ld_out, uint32_t units, int experts
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) g[j][i] = weight[R::at(j, experts) + i];
-    for (uint32_t unit = blockIdx.x * kGradWaves + wave_index(); unit < units; unit += UNROLL * waves) {
-        Unit k[UNROLL];
+    const uint32_t own_row = (threadIdx.x & 63) / L;
+    for (uint32_t tile = blockIdx.x * kGradWaves + wave_index(); tile < tiles; tile += waves) {
+        const Tile k = tile_of<UNROLL * R::kRows>(table, tile, tiles);
         R row[UNROLL];
         uint8_t flag[UNROLL];
         bool counts[UNROLL];
+        float e[UNROLL][NV][VEC], most[UNROLL];
+        auto token = [&](int u) { return k.t0 + min(static_cast<uint32_t>(u) * R::kRows + own_row, k.rows - 1); };
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) k[u] = unit_of<R::kRows, L>(table, unit + u * waves, units);
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) flag[u] = *k[u].flag;
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) counts[u] = k[u].exists && (!k[u].masked || flag[u] != 0);
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) row[u].load(table_ptr<const one>(k[u].logits) + k[u].t * ld, experts, counts[u]);
+        for (int u = 0; u < UNROLL; ++u) flag[u] = flag_of(k, u * R::kRows + own_row);
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            float e[NV][VEC], dot = 0.0f;
-            const float inverse = row[u].exponentials(own, e);
+            counts[u] = counts_in(k, u * R::kRows + own_row, flag[u]);
+            row[u].load(table_ptr<const one>(k.logits) + token(u) * ld, experts, counts[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) most[u] = row[u].largest(e[u]);
+        exponentials_of<R>(e, most, TYPE != BAGUA_F16);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            float dot = 0.0f;
+            const float inverse = R::reciprocal_sum(own, e[u]);
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) dot = __builtin_fmaf(e[j][i], g[j][i] * own[j][i], dot);
+                for (int i = 0; i < VEC; ++i) dot = __builtin_fmaf(e[u][j][i], g[j][i] * own[j][i], dot);
             // (rows that do not count were read as zeros)
             const float scale = counts[u] ? inverse * up : 0.0f, shift = -(lanes_reduce<L>(dot, OpAddF()) * inverse) * scale;
-            one* out = table_ptr<one>(k[u].other) + k[u].t * ld_out;
+            one* out = table_ptr<one>(k.other) + token(u) * ld_out;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 typename R::raw q;
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) q[i] = Elem<TYPE>::narrow(e[j][i] * __builtin_fmaf(g[j][i], scale, shift));
-                if (k[u].exists) __builtin_nontemporal_store(q, reinterpret_cast<typename R::raw*>(out + R::at(j, experts)));
+                for (int i = 0; i < VEC; ++i) q[i] = Elem<TYPE>::narrow(e[u][j][i] * __builtin_fmaf(g[j][i], scale, shift));
+                if (u * R::kRows + own_row < k.rows) __builtin_nontemporal_store(q, reinterpret_cast<typename R::raw*>(out + R::at(j, experts)));
             }
         }
     }
@@ -464,33 +540,37 @@ template <int VEC_, int L_, int NV_, int UNROLL_, int WAVES_ = 16>
 struct Layout {
     static constexpr int VEC = VEC_, L = L_, NV = NV_, UNROLL = UNROLL_, WAVES = WAVES_, GRAD_UNROLL = NV_ == 1 ? 2 : 1;   // WAVES: of a workgroup of the forward pass
 };
-template <typename F>
-inline void with_layout(int experts, const F& f)
+// The forward pass of 16-bit rows beyond 128 elements is bound by the vector ALU: twice the elements in half the lanes take half the
+// exchanges (524288 x 256, bf16, 78 -> 67 us, 250 K x 512, fp16, 82 -> 72; 8 x 32768 x 64 loses, 21.8 -> 22.0).
+template <int V, bool FORWARD, typename F>
+inline void with_vectors(int experts, const F& f)
 {
-    if (experts < 8) {
+    if (experts < V) {
         if (experts <= 1) f(Layout<1, 1, 1, 4>());
         else if (experts <= 2) f(Layout<1, 2, 1, 4>());
         else if (experts <= 4) f(Layout<1, 4, 1, 4>());
         else f(Layout<1, 8, 1, 4>());
-    } else if (experts <= 8) f(Layout<8, 1, 1, 4>());
-    else if (experts <= 16) f(Layout<8, 2, 1, 4>());
-    else if (experts <= 32) f(Layout<8, 4, 1, 4>());
-    else if (experts <= 64) f(Layout<8, 8, 1, 4>());
-    else if (experts <= 128) f(Layout<8, 16, 1, 4>());
-    else if (experts <= 256) f(Layout<8, 32, 1, 4>());
-    else if (experts <= 512) f(Layout<8, 64, 1, 4>());
-    else if (experts <= 1024) f(Layout<8, 64, 2, 2>());
-    else f(Layout<8, 64, 4, 1, 8>());
+    } else if (experts <= V) f(Layout<V, 1, 1, 4>());
+    else if (experts <= 2 * V) f(Layout<V, 2, 1, 4>());
+    else if (experts <= 4 * V) f(Layout<V, 4, 1, 4>());
+    else if (experts <= 8 * V) f(Layout<V, 8, 1, 4>());
+    else if (experts <= 16 * V) f(Layout<V, 16, 1, 4>());
+    else if (experts <= 32 * V) f(std::conditional_t<FORWARD && V == 8, Layout<V, 16, 2, 2>, Layout<V, 32, 1, 4>>());
+    else if (experts <= 64 * V) f(std::conditional_t<FORWARD && V == 8, Layout<V, 32, 2, 2>, Layout<V, 64, 1, 4>>());
+    else if (experts <= 128 * V) f(Layout<V, 64, 2, 2>());
+    else if (experts <= 256 * V) f(Layout<V, 64, 4, 1, V == 8 ? 8 : 16>());
+    else if constexpr (V == 4) f(Layout<V, 64, 8, 1, 8>());
 }
-template <typename F>
-inline void with_type(int dtype, const F& f)
+// 16 bytes of a row in a lane: a wider vector of fp32 is two accesses that each leave out every other 16 bytes, and a store of half a
+// line costs a whole one (gradient of 1 M rows of 64, fp32: eight elements 101.8 us, four E64).
+template <bool FORWARD, typename F>
+inline void with_layout(int dtype, int experts, const F& f)
 {
-    if (dtype == BAGUA_F32) f(std::integral_constant<int, BAGUA_F32>());
-    else if (dtype == BAGUA_BF16) f(std::integral_constant<int, BAGUA_BF16>());
-    else f(std::integral_constant<int, BAGUA_F16>());
+    if (dtype == BAGUA_F32) with_vectors<4, FORWARD>(experts, [&](auto layout) { f(layout, std::integral_constant<int, BAGUA_F32>()); });
+    else if (dtype == BAGUA_BF16) with_vectors<8, FORWARD>(experts, [&](auto layout) { f(layout, std::integral_constant<int, BAGUA_BF16>()); });
+    else with_vectors<8, FORWARD>(experts, [&](auto layout) { f(layout, std::integral_constant<int, BAGUA_F16>()); });
 }
-
-// Arguments that both passes have, and the workers' table.  rows: of a unit.
+// Arguments that both passes have, and the workers' table.
 inline int balance_check(int dtype, const void* const* logits, size_t ld, const size_t* tokens, int k, int experts, Workers& ws)
 {
     if (!logits || !tokens || !type_ok(dtype) || k < 1 || k > BAGUA_MAX_WORKERS || experts < 1 || ld < static_cast<size_t>(experts)) return BAGUA_ERR_INVALID_ARG;
@@ -507,15 +587,15 @@ inline int balance_check(int dtype, const void* const* logits, size_t ld, const 
     }
     return BAGUA_OK;
 }
-inline bool units_of(Workers& ws, int rows)
+inline bool tiles_of(Workers& ws, int rows)
 {
-    uint64_t units = 0;
+    uint64_t tiles = 0;
     for (uint32_t w = 0; w < ws.k; ++w) {
-        ws.first_unit[w] = static_cast<uint32_t>(units);
-        units += (ws.tokens[w] + static_cast<uint32_t>(rows) - 1) / static_cast<uint32_t>(rows);
-        if (units > kMaxGrid) return false;
+        ws.first_tile[w] = static_cast<uint32_t>(tiles);
+        tiles += (ws.tokens[w] + static_cast<uint32_t>(rows) - 1) / static_cast<uint32_t>(rows);
+        if (tiles > kMaxGrid) return false;
     }
-    for (uint32_t w = ws.k; w <= BAGUA_MAX_WORKERS; ++w) ws.first_unit[w] = static_cast<uint32_t>(units);
+    for (uint32_t w = ws.k; w <= BAGUA_MAX_WORKERS; ++w) ws.first_tile[w] = static_cast<uint32_t>(tiles);
     return true;
 }
 inline size_t matrix_bytes(size_t rows, size_t ld, size_t columns, size_t element) { return rows ? ((rows - 1) * ld + columns) * element : 0; }
@@ -527,7 +607,7 @@ using namespace bagua;
 extern "C" size_t bagua_balance_workspace_bytes(int experts)
 {
     if (experts < 1 || experts > BAGUA_MAX_EXPERTS) return 0;
-    return 64 + kBalanceGroups * (2 * static_cast<size_t>(experts) + 1) * sizeof(uint32_t);
+    return kArriveBytes + kBalanceGroups * (2 * static_cast<size_t>(experts) + 1) * sizeof(uint32_t);
 }
 
 extern "C" int bagua_balance_stats(int dtype, const void* const* logits, size_t ld, const size_t* tokens, int k, int experts,
@@ -570,19 +650,17 @@ extern "C" int bagua_balance_stats(int dtype, const void* const* logits, size_t 
     int lg = 3;                                             // copies of a counter: what fits 16 KiB, eight at most
     while (lg > 0 && ((e + 1) << lg) > 4096) --lg;
     int status = BAGUA_OK;
-    with_layout(experts, [&](auto layout) {
+    with_layout<true>(dtype, experts, [&](auto layout, auto type) {
         typedef decltype(layout) Lay;
-        if (!units_of(ws, kWave / Lay::L)) {
+        if (!tiles_of(ws, Lay::UNROLL * kWave / Lay::L)) {
             status = BAGUA_ERR_UNSUPPORTED;
             return;
         }
-        const uint32_t units = ws.first_unit[BAGUA_MAX_WORKERS];
-        const dim3 grid(std::min<uint32_t>(std::max<uint32_t>((units + Lay::WAVES - 1) / Lay::WAVES, 1), kBalanceGroups)), block(kWave * Lay::WAVES);
+        const uint32_t tiles = ws.first_tile[BAGUA_MAX_WORKERS];
+        const dim3 grid(std::min<uint32_t>(std::max<uint32_t>((tiles + Lay::WAVES - 1) / Lay::WAVES, 1), kBalanceGroups)), block(kWave * Lay::WAVES);
         const size_t lds = (static_cast<size_t>(sum_rows(Lay::WAVES, experts)) * e + ((e + 1) << lg)) * sizeof(float);
-        with_type(dtype, [&](auto type) {
-            launch_kernel(k_balance_stats<decltype(type)::value, Lay::VEC, Lay::L, Lay::NV, Lay::UNROLL, Lay::WAVES>, grid, block, lds, static_cast<hipStream_t>(stream),
-                          ws, ld, ids_ld, id_bytes, units, per_k, lg, static_cast<uint32_t*>(workspace), out);
-        });
+        launch_kernel(k_balance_stats<decltype(type)::value, Lay::VEC, Lay::L, Lay::NV, Lay::UNROLL, Lay::WAVES>, grid, block, lds,
+                      static_cast<hipStream_t>(stream), ws, ld, ids_ld, id_bytes, tiles, per_k, lg, static_cast<uint32_t*>(workspace), out);
         status = launch_status();
     });
     return status;
@@ -631,20 +709,18 @@ extern "C" int bagua_balance_grad(int dtype, const void* const* logits, size_t l
     if (!rc.disjoint()) return BAGUA_ERR_INVALID_ARG;
     if (!aligned4(weight) || !aligned4(upstream)) return BAGUA_ERR_ALIGNMENT;
     int status = BAGUA_OK;
-    with_layout(experts, [&](auto layout) {
+    with_layout<false>(dtype, experts, [&](auto layout, auto type) {
         typedef decltype(layout) Lay;
-        if (!units_of(ws, kWave / Lay::L)) {
+        if (!tiles_of(ws, Lay::GRAD_UNROLL * kWave / Lay::L)) {
             status = BAGUA_ERR_UNSUPPORTED;
             return;
         }
-        const uint32_t units = ws.first_unit[BAGUA_MAX_WORKERS];
-        if (units == 0) return;
-        const uint32_t waves = std::min<uint32_t>((units + Lay::GRAD_UNROLL - 1) / Lay::GRAD_UNROLL, kGradMostWaves);
+        const uint32_t tiles = ws.first_tile[BAGUA_MAX_WORKERS];
+        if (tiles == 0) return;
+        const uint32_t waves = std::min<uint32_t>(tiles, kGradMostWaves);
         const dim3 grid((waves + kGradWaves - 1) / kGradWaves), block(kWave * kGradWaves);
-        with_type(dtype, [&](auto type) {
-            launch_kernel(k_balance_grad<decltype(type)::value, Lay::VEC, Lay::L, Lay::NV, Lay::GRAD_UNROLL>, grid, block, 0, static_cast<hipStream_t>(stream), ws, ld,
-                          ld_out, units, experts, weight, upstream);
-        });
+        launch_kernel(k_balance_grad<decltype(type)::value, Lay::VEC, Lay::L, Lay::NV, Lay::GRAD_UNROLL>, grid, block, 0, static_cast<hipStream_t>(stream), ws,
+                      ld, ld_out, tiles, experts, weight, upstream);
         status = launch_status();
     });
     return status;

@@ -43,6 +43,7 @@ static_assert((BAGUA_ADAM8_ROWS == 1 || BAGUA_ADAM8_ROWS == 2 || BAGUA_ADAM8_ROW
 // is one more that has to be counted at the end, 13 ns apiece: 335 M fp32 elements, 2048 groups of 4 waves 215 us, 512 of 8 197, 512 of
 // 4 191, 256 of 8 192; bf16, 256 groups of 8 142, of 16 100; 25.6 M bf16, 2048 groups of 4 32.3, 256 of 16 14.3.
 constexpr unsigned kNormGroups = kCus;
+static_assert(kNormGroups <= kArriveMost, "groups that can be counted");
 constexpr unsigned norm_waves(int type) { return type == BAGUA_F32 ? 8 : 16; }
 // Up to four tiles a wave, one group alone is faster than several that have to meet: 20 K elements in 30 tensors 4.5 -> 3.5 us, 5 K 4.3 ->
 // 3.4; 41 K in 49 tensors (eight tiles a wave) 4.9 -> 6.8.
@@ -59,8 +60,8 @@ struct TensorEntry {
 };
 static_assert(sizeof(TensorEntry) == 80, "the table is a whole number of 16-byte words");
 
-// The plan's workspace: [counter, padding | partial sums of the norm | entries | tensor of every tile].
-constexpr size_t kPartialsAt = 64, kEntriesAt = kPartialsAt + kNormGroups * sizeof(double);
+// The plan's workspace: [counters | partial sums of the norm | entries | tensor of every tile].
+constexpr size_t kPartialsAt = kArriveBytes, kEntriesAt = kPartialsAt + kNormGroups * sizeof(double);
 struct TensorPlanView {
     uint32_t* counter;
     double* partial;
@@ -137,10 +138,18 @@ __device__ __forceinline__ f4 widen_codes(uint32_t w, float scale)
 struct Scale {
     float scale, inverse;
 };
+// 1 / b, correctly rounded (compared with the division for every mantissa), for b and 1 / b from 2^-126 on
+__device__ __forceinline__ float reciprocal_in_range(float b)
+{
+    const float y = __builtin_amdgcn_rcpf(b);
+    return __builtin_fmaf(y, __builtin_fmaf(-b, y, 1.0f), y);
+}
+template <bool FAST>
 __device__ __forceinline__ Scale scale_of(float most)
 {
     const float s = most * static_cast<float>(1.0 / 448.0);
-    return s < 0x1p-126f ? Scale{0.0f, 0.0f} : Scale{s, 1.0f / s};
+    if (s < 0x1p-126f) return Scale{0.0f, 0.0f};
+    return Scale{s, FAST ? reciprocal_in_range(s) : 1.0f / s};
 }
 __device__ __forceinline__ uint32_t nearest_codes(f4 y)
 {
@@ -208,7 +217,7 @@ __device__ __forceinline__ uint32_t blocks_most(const uint32_t (&x)[K])
 //   root:      y = rsqrt, g = t*y and h = y/2 are a few units off; t - g*g is exact in a fused operation, and g + h * that rounds to the
 //              root: compared with sqrtf for every mantissa and both parities of the exponent.  Zero stays zero, as the reciprocal root is
 //              taken of something above it.
-//   quotient:  one Newton step makes the reciprocal of b the correctly rounded one (compared with 1/b for every mantissa); the remainder of
+//   quotient:  with the correctly rounded reciprocal of b (reciprocal_in_range) the remainder of
 //              a quotient that is a unit off at most is exact, and adding its product with the reciprocal rounds to the quotient.
 constexpr float kFirstScale = 0x1p64f, kSecondScale = 0x1p64f, kRootScale = 0x1p32f;
 __device__ __forceinline__ float root_in_range(float t)   // 0, or 2^-90 <= t < 2^126
@@ -218,9 +227,7 @@ __device__ __forceinline__ float root_in_range(float t)   // 0, or 2^-90 <= t < 
 }
 __device__ __forceinline__ float quotient_in_range(float a, float b)   // 2^-40 <= b < 2^21; a = 0, or 2^-101 <= |a| <= 2^84
 {
-    float y = __builtin_amdgcn_rcpf(b);
-    y = __builtin_fmaf(y, __builtin_fmaf(-b, y, 1.0f), y);
-    const float q = a * y;
+    const float y = reciprocal_in_range(b), q = a * y;
     return __builtin_fmaf(-__builtin_fmaf(b, q, -a), y, q);             // (the remainder's sign keeps that of a zero)
 }
 // Blocks that keep to the ranges: first moments up to 2^20, roots up to 2^10 (in their scaled forms).  What is no number does not.
@@ -330,7 +337,7 @@ __device__ __forceinline__ bool adamw_share(const TensorEntry& d, size_t e0, int
     }
     if constexpr (BITS == 8) {
         constexpr int kLanes = kWave / K;      // that have a block's largest value
-        const Scale sm = scale_of(__uint_as_float(blocks_most<K>(m_most)) * (1.0f / kFirst)), sv = scale_of(__uint_as_float(blocks_most<K>(r_most)) * (1.0f / kRoot));
+        const Scale sm = scale_of<FAST>(__uint_as_float(blocks_most<K>(m_most)) * (1.0f / kFirst)), sv = scale_of<FAST>(__uint_as_float(blocks_most<K>(r_most)) * (1.0f / kRoot));
         const float im = sm.inverse * (1.0f / kFirst), iv = sv.inverse * (1.0f / kRoot);
         auto of_block = [&](float x, int k) { return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_readlane(__float_as_int(x), k * kLanes))); };
 #pragma unroll
@@ -458,7 +465,6 @@ k_grad_norm(TensorPlanView plan, uint32_t tiles, double scale, double max_norm, 
         static_assert(kNormGroups <= kWave * kNormWaves, "a thread for every group");
         sum = threadIdx.x < gridDim.x ? plan.partial[threadIdx.x] : 0.0;
         sum = group_sum(sum);
-        if (threadIdx.x == 0) __hip_atomic_store(plan.counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next call
     }
     if (threadIdx.x != 0) return;
     const double n = scale * sqrt(sum);
