@@ -608,10 +608,17 @@ def _type_of(tensors, what, allowed):
     return dtype
 
 
-def _tensors(tensors, dtype, numels):
-    """Addresses of contiguous tensors that hold at least those numbers of elements."""
+def _tensors(tensors, dtype, sizes, per=1, exact=False):
+    """Addresses of contiguous GPU tensors that hold an element for `per` of each size (`exact`: no more than these)."""
+    if tensors[0].dtype is dtype:
+        at = _native.tensor_addresses(tensors, tensors[0], sizes, per, exact)
+        if at is not False:
+            return at
     at = (ctypes.c_void_p * len(tensors))()
-    for i, (t, n) in enumerate(zip(tensors, numels)):
+    for i, (t, n) in enumerate(zip(tensors, (ctypes.c_size_t * len(tensors)).from_buffer_copy(sizes))):
+        n = -(-n // per)
+        if exact and t.numel() != n:
+            raise ValueError("a parameter of %d elements has a gradient of %d" % (t.numel(), n))
         at[i] = _ptr(t, dtype, n * t.element_size()) if n else None
     return at
 
@@ -631,27 +638,27 @@ def bagua_tensor_plan(grads, workspace, params=None, m=None, v=None, m_scales=No
     if (params is None) != (m is None) or (params is None) != (v is None):
         raise ValueError("params, m and v go together")
     _same_len(T, params=params, m=m, v=v, m_scales=m_scales, v_scales=v_scales, copies=copies, decay=decay)
-    ns = [g.numel() for g in grads]
+    lists = [None if ts is None else list(ts) for ts in (grads, params, m, v, m_scales, v_scales, copies)]
+    grads, params, m, v, m_scales, v_scales, copies = lists
+    ns = _native.tensor_sizes(grads)
+    if ns is False:
+        ns = bytes(_sizes([g.numel() for g in grads]))
     gt = _type_of(grads, "gradients", (torch.float32, torch.bfloat16, torch.float16))
     pt = mt = ct = None
     if params is not None:
         pt = _type_of(params, "parameters", (torch.float32, torch.bfloat16))
         mt = _type_of(m, "moments", (torch.float32, torch.float8_e4m3fn))
-        for p, n in zip(params, ns):
-            if p.numel() != n:
-                raise ValueError("a parameter of %d elements has a gradient of %d" % (p.numel(), n))
     if copies is not None:
         ct = _type_of(copies, "copies", (torch.bfloat16, torch.float16))
-    blocks = [(n + 255) // 256 for n in ns]
-    array = lambda ts, dtype, sizes: None if ts is None else _tensors(ts, dtype, sizes)  # noqa: E731
+    array = lambda ts, dtype, per=1, exact=False: None if ts is None else _tensors(ts, dtype, ns, per, exact)  # noqa: E731
     plan = _PlanStruct()
     wp, wb = _ws(workspace)
     _check("bagua_tensor_plan", _lib.bagua_tensor_plan(
-        _sizes(ns), T, _tensors(grads, gt, ns), _TYPES[gt], array(params, pt, ns), _TYPES.get(pt, 0), array(m, mt, ns), array(v, mt, ns),
-        0 if mt is None else 32 if mt is torch.float32 else 8, array(m_scales, torch.float32, blocks), array(v_scales, torch.float32, blocks),
-        array(copies, ct, ns), _TYPES.get(ct, 0), None if decay is None else (ctypes.c_float * T)(*[float(d) for d in decay]), wp, wb,
+        ns, T, array(grads, gt), _TYPES[gt], array(params, pt, 1, True), _TYPES.get(pt, 0), array(m, mt), array(v, mt),
+        0 if mt is None else 32 if mt is torch.float32 else 8, array(m_scales, torch.float32, 256), array(v_scales, torch.float32, 256),
+        array(copies, ct), _TYPES.get(ct, 0), None if decay is None else (ctypes.c_float * T)(*[float(d) for d in decay]), wp, wb,
         ctypes.addressof(plan), _stream(stream)))
-    return TensorPlan(plan, (list(grads), params, m, v, m_scales, v_scales, copies, workspace))
+    return TensorPlan(plan, (lists, workspace))
 
 
 def bagua_grad_norm(plan, out, max_norm=float("inf"), grad_scale=1.0, stream=None):

@@ -604,6 +604,62 @@ PY_END
 #undef PY
 #undef PY_END
 
+// The marshalling of a plan, which has thousands of tensors: numbers of elements, and addresses, as the words of a bytes object that the
+// entry point reads in place of an array.  False where anything is out of the ordinary, as above.
+//
+// tensor_sizes(tensors)
+PyObject* tensor_sizes(PyObject*, PyObject* const* a, Py_ssize_t given)
+{
+    if (given != 1 || !PyList_CheckExact(a[0])) Py_RETURN_FALSE;
+    const Py_ssize_t count = PyList_GET_SIZE(a[0]);
+    PyObject* out = PyBytes_FromStringAndSize(nullptr, count * static_cast<Py_ssize_t>(sizeof(size_t)));
+    if (!out) return nullptr;
+    size_t* n = reinterpret_cast<size_t*>(PyBytes_AS_STRING(out));
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        PyObject* o = PyList_GET_ITEM(a[0], i);
+        if (!THPVariable_CheckTypeExact(Py_TYPE(o))) {
+            Py_DECREF(out);
+            Py_RETURN_FALSE;
+        }
+        n[i] = static_cast<size_t>(THPVariable_Unpack(o).numel());
+    }
+    return out;
+}
+
+// tensor_addresses(tensors, one tensor of their type, sizes, per, exact): of contiguous tensors on the GPU with an element for `per` of
+// each size, rounded up, or exactly as many
+PyObject* tensor_addresses(PyObject*, PyObject* const* a, Py_ssize_t given)
+{
+    if (given != 5 || !PyList_CheckExact(a[0]) || !THPVariable_CheckTypeExact(Py_TYPE(a[1])) || !PyBytes_CheckExact(a[2])) Py_RETURN_FALSE;
+    const Py_ssize_t count = PyList_GET_SIZE(a[0]);
+    const size_t per = PyLong_AsSize_t(a[3]);
+    if (PyErr_Occurred()) return nullptr;
+    if (per == 0 || PyBytes_GET_SIZE(a[2]) != count * static_cast<Py_ssize_t>(sizeof(size_t))) Py_RETURN_FALSE;
+    const at::ScalarType type = THPVariable_Unpack(a[1]).scalar_type();
+    const size_t* n = reinterpret_cast<const size_t*>(PyBytes_AS_STRING(a[2]));
+    PyObject* out = PyBytes_FromStringAndSize(nullptr, count * static_cast<Py_ssize_t>(sizeof(void*)));
+    if (!out) return nullptr;
+    void** p = reinterpret_cast<void**>(PyBytes_AS_STRING(out));
+    bool ok = true;
+    try {
+        for (Py_ssize_t i = 0; i < count && ok; ++i) {
+            PyObject* o = PyList_GET_ITEM(a[0], i);
+            ok = THPVariable_CheckTypeExact(Py_TYPE(o));
+            if (!ok) break;
+            const at::Tensor& t = THPVariable_Unpack(o);
+            const size_t need = n[i] / per + (n[i] % per != 0), has = static_cast<size_t>(t.numel());
+            ok = t.is_cuda() && t.layout() == at::kStrided && t.is_contiguous() && t.scalar_type() == type && (a[4] == Py_True ? has == need : has >= need);
+            if (ok) p[i] = need ? t.data_ptr() : nullptr;
+        }
+    } catch (...) {
+        if (PyErr_Occurred()) PyErr_Clear();
+        ok = false;
+    }
+    if (ok) return out;
+    Py_DECREF(out);
+    Py_RETURN_FALSE;
+}
+
 // bind(library, error, raw_stream, device): library = {name of an entry point: its address}
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t given)
 {
@@ -645,6 +701,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t given)
 
 #define X(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr},
 PyMethodDef g_methods[] = {BAGUA_NATIVE(X) BAGUA_NATIVE_STEPS(X){"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind)), METH_FASTCALL, nullptr},
+                           {"tensor_sizes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(tensor_sizes)), METH_FASTCALL, nullptr},
+                           {"tensor_addresses", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(tensor_addresses)), METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 #undef X
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

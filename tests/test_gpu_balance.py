@@ -274,3 +274,18 @@ def test_refusals(bg):
     with pytest.raises(bg.BaguaError, match="UNSUPPORTED"):
         big = torch.zeros(2, 2049, device="cuda")
         bg.bagua_balance_grad([big], None, torch.zeros(2049, device="cuda"), None, [torch.zeros_like(big)])
+
+
+def test_both_paths_make_the_same_calls(bg, monkeypatch):
+    """Statistics and gradient through the host extension and through the general path: the same bits."""
+    got = []
+    for native in (True, False):
+        s = inputs([300, 0, 77], 24, 3, "f16", 8, ids=torch.int32, masked=0.2, pad=2)
+        b, out = buffers(bg, 24), [torch.zeros(x.shape[0], 24, device="cuda", dtype=x.dtype) for x in s["logits"]]
+        with monkeypatch.context() as patch:
+            patch.setattr(bg.binding, "_lib" if native else "_native", None if native else bg.binding._Declines())
+            stats(bg, s, b)
+            bg.bagua_balance_grad(s["logits"], s["mask"], b["weight"], None, out)
+        got.append([b[k].clone() for k in ("counts", "prob", "loss", "weight")] + out)
+    for x, y in zip(*got):
+        assert torch.equal(x, y)

@@ -477,3 +477,25 @@ def test_refusals(bg):
             bg.bagua_adamw_step(plan, **dict(dict(step=1, lr=1e-3), **bad))
     torch.cuda.synchronize()
     assert bool((ok["params"][0] == 0).all())
+
+
+def test_both_paths_make_the_same_calls(bg, monkeypatch):
+    """Plan, norm and step through the host extension and through the general path: the same bits."""
+    ns, got = [700, 0, 3, 5000], []
+    for native in (True, False):
+        r = torch.Generator(device="cuda").manual_seed(4)
+        p, g = ([torch.randn(n, device="cuda", generator=r) for n in ns] for _ in range(2))
+        m, v = ([torch.zeros(n, device="cuda").to(F8) for n in ns] for _ in range(2))
+        ms, vs = ([torch.zeros(blocks(n), device="cuda") for n in ns] for _ in range(2))
+        copies, clip = [x.bfloat16() for x in p], torch.zeros(2, device="cuda")
+        with monkeypatch.context() as patch:
+            if not native:
+                patch.setattr(bg.binding, "_native", bg.binding._Declines())
+            plan = plan_of(bg, ns, g, params=p, m=m, v=v, m_scales=ms, v_scales=vs, copies=copies)
+            if native:   # the two calls leave nothing to the general path
+                patch.setattr(bg.binding, "_lib", None)
+            bg.bagua_grad_norm(plan, clip, 1.0, 0.5)
+            bg.bagua_adamw_step(plan, 3, 1e-3, weight_decay=0.1, clip=clip, seed=7)
+        got.append([t.clone() for t in p + m + v + ms + vs + copies + [clip]])
+    for a, b in zip(*got):
+        assert torch.equal(a.view(torch.uint8) if a.numel() else a, b.view(torch.uint8) if b.numel() else b)

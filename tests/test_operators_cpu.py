@@ -112,3 +112,24 @@ def test_statistics_refuse(bg, kw, status):
 def test_gradient_refuses(bg, kw, status):
     a = dict(GRAD, **kw)
     assert bg.binding.raw().bagua_balance_grad(*[a[k] for k in GRAD], None) == status
+
+
+def test_calls_that_are_not_ordinary_are_declined(bg):
+    """The host extension's part of these calls leaves what it does not know to the general path, and does nothing."""
+    import torch
+    native = bg.binding._native
+    x, ids, c, p = torch.zeros(4, 8), torch.zeros(4, 2, dtype=torch.int64), torch.zeros(9, dtype=torch.int32), torch.zeros(8)
+    for f, count in ((native.grad_norm, 5), (native.adamw_step, 10), (native.balance_stats, 10), (native.balance_grad, 6)):
+        for n in (0, count - 1, count, count + 1):
+            assert f(*[None] * n) is False
+    assert native.balance_stats([x], [ids], None, c, p, c, 0.01, None, None, None) is False        # not on the GPU
+    assert native.balance_grad([x], None, p, None, [x], None) is False
+    assert native.grad_norm(0, p, 1.0, 1.0, None) is False and native.grad_norm("plan", p, 1.0, 1.0, None) is False
+    assert native.tensor_sizes((x,)) is False and native.tensor_sizes([x, 3]) is False
+    assert native.tensor_sizes([x, ids]) == bytes(sizes(32, 8))
+    assert native.tensor_addresses([x], x, bytes(sizes(32)), 1, False) is False                    # not on the GPU
+    assert native.tensor_addresses([x], x, b"", 1, False) is False and native.tensor_addresses([x], x, bytes(sizes(32)), 0, False) is False
+    with pytest.raises(ValueError, match="contiguous GPU tensor"):
+        bg.bagua_tensor_plan([x], torch.zeros(10, dtype=torch.uint8))
+    with pytest.raises(ValueError, match="expected GPU tensors"):
+        bg.bagua_balance_grad([x], None, p, None, [x])
