@@ -415,60 +415,77 @@ k_balance_stats(Workers ws, size_t ld, size_t ids_ld, int id_bytes, uint32_t til
         return;
     }
 
-    // [group][expert] of a sum and a count, and every group's tokens behind them
+    // Pairs of a sum and a count, [group][experts], behind them those of the clusters of groups, and behind these the tokens of both.
+    const uint32_t pair_rows = gridDim.x + clusters();
     uint64_t* pairs = reinterpret_cast<uint64_t*>(workspace + kArriveBytes / sizeof(uint32_t));
-    uint32_t* group_tokens = reinterpret_cast<uint32_t*>(pairs + static_cast<size_t>(gridDim.x) * experts);
-    for (int e = threadIdx.x; e < experts; e += kThreads)
-        publish(pairs + blockIdx.x * experts + e, static_cast<uint64_t>(copies(e)) << 32 | __float_as_uint(wave_sums(e)));
-    if (threadIdx.x == 0) publish(group_tokens + blockIdx.x, copies(experts));
-    if (!last_to_arrive(workspace, &last)) return;
-
-    // The groups' sums, by as many threads per expert as there are, in a fixed order.
+    uint32_t* pair_tokens = reinterpret_cast<uint32_t*>(pairs + static_cast<size_t>(pair_rows) * experts);
+    auto publish_row = [&](uint32_t row, auto&& count, auto&& prob) {
+        for (int e = threadIdx.x; e < experts; e += kThreads)
+            publish(pairs + static_cast<size_t>(row) * experts + e, static_cast<uint64_t>(count(e)) << 32 | __float_as_uint(prob(e)));
+        if (threadIdx.x == 0) publish(pair_tokens + row, static_cast<uint32_t>(count(experts)));
+    };
     __shared__ double slice_sum[kThreads];
     __shared__ uint32_t slice_count[kThreads];
-    uint32_t all = threadIdx.x < gridDim.x ? group_tokens[threadIdx.x] : 0;     // (no more groups than threads)
-    static_assert(kThreads >= kBalanceGroups, "a thread for every group");
     int width = 1;                                          // threads of a slice, a power of two
     while (width < experts && width < kThreads) width *= 2;
     const uint32_t slices = kThreads / width, slice = threadIdx.x / width;
-    for (int e0 = 0; e0 < experts; e0 += width) {
-        const int e = e0 + threadIdx.x % width;
-        double s = 0.0;
-        uint32_t c = 0;
-        const uint64_t* from = pairs + min(e, experts - 1);
-        // sixteen at a time and without a test before a load, or each would be waited for
-        for (uint32_t g = slice; g < gridDim.x; g += 16 * slices) {
-            uint64_t pair[16];
+    // The sums over `n` rows of pairs, by as many threads per expert as there are, in a fixed order: in sums and counters.
+    auto together = [&](uint32_t row, uint32_t n) {
+        static_assert(kThreads >= kBalanceGroups, "a thread for every row");
+        uint32_t all = threadIdx.x < n ? pair_tokens[row + threadIdx.x] : 0;
+        for (int e0 = 0; e0 < experts; e0 += width) {
+            const int e = e0 + threadIdx.x % width;
+            double s = 0.0;
+            uint32_t c = 0;
+            const uint64_t* from = pairs + static_cast<size_t>(row) * experts + min(e, experts - 1);
+            // sixteen at a time and without a test before a load, or each would be waited for
+            for (uint32_t g = slice; g < n; g += 16 * slices) {
+                uint64_t pair[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) pair[i] = from[static_cast<size_t>(min(g + i * slices, gridDim.x - 1)) * experts];
+                for (int i = 0; i < 16; ++i) pair[i] = from[static_cast<size_t>(min(g + i * slices, n - 1)) * experts];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                if (g + i * slices >= gridDim.x) pair[i] = 0;
-                s += __uint_as_float(static_cast<uint32_t>(pair[i]));
-                c += static_cast<uint32_t>(pair[i] >> 32);
+                for (int i = 0; i < 16; ++i) {
+                    if (g + i * slices >= n) pair[i] = 0;
+                    s += __uint_as_float(static_cast<uint32_t>(pair[i]));
+                    c += static_cast<uint32_t>(pair[i] >> 32);
+                }
             }
-        }
-        slice_sum[threadIdx.x] = s;
-        slice_count[threadIdx.x] = c;
-        __syncthreads();
-        if (slice == 0 && e < experts) {
+            slice_sum[threadIdx.x] = s;
+            slice_count[threadIdx.x] = c;
+            __syncthreads();
+            if (slice == 0 && e < experts) {
 #pragma unroll 8
-            for (uint32_t i = 1; i < slices; ++i) {
-                s += slice_sum[i * width + threadIdx.x];
-                c += slice_count[i * width + threadIdx.x];
+                for (uint32_t i = 1; i < slices; ++i) {
+                    s += slice_sum[i * width + threadIdx.x];
+                    c += slice_count[i * width + threadIdx.x];
+                }
+                sums[e] = static_cast<float>(s);
+                counters[e] = c;
             }
-            sums[e] = static_cast<float>(s);
-            counters[e] = c;
+            if (e0 == 0 && threadIdx.x == 0) counters[experts] = 0;
+            __syncthreads();
         }
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) counters[experts] = 0;
-    __syncthreads();
 #pragma unroll
-    for (int s = 32; s > 0; s >>= 1) all += __shfl_xor(all, s);
-    if (lane == 0 && all) atomicAdd(counters + experts, all);
-    __syncthreads();
-    finish([&](int e) { return counters[e]; }, [&](int e) { return sums[e]; });
+        for (int s = 32; s > 0; s >>= 1) all += __shfl_xor(all, s);
+        if (lane == 0 && all) atomicAdd(counters + experts, all);
+        __syncthreads();
+    };
+    auto summed_count = [&](int e) { return counters[e]; };
+    auto summed_prob = [&](int e) { return sums[e]; };
+    publish_row(blockIdx.x, copies, wave_sums);
+    // In two steps where one group would read too much: 250 K x 512, fp16, 73.5 -> 65 us, but 8 x 32768 x 64 20.8 -> 25.3, 524288 x 256 66.8 -> 67.1.
+    if (experts <= 256 || gridDim.x <= kArriveDirect) {
+        if (!last_to_arrive(workspace, &last)) return;
+        together(0, gridDim.x);
+    } else {
+        if (!last_of_cluster(workspace, &last)) return;
+        const uint32_t cluster = blockIdx.x / kArriveGroup;
+        together(cluster * kArriveGroup, cluster_groups(cluster));
+        publish_row(gridDim.x + cluster, summed_count, summed_prob);
+        if (!last_cluster(workspace, &last)) return;
+        together(gridDim.x, clusters());
+    }
+    finish(summed_count, summed_prob);
 }
 
 __global__ void __launch_bounds__(256)
@@ -607,7 +624,7 @@ using namespace bagua;
 extern "C" size_t bagua_balance_workspace_bytes(int experts)
 {
     if (experts < 1 || experts > BAGUA_MAX_EXPERTS) return 0;
-    return kArriveBytes + kBalanceGroups * (2 * static_cast<size_t>(experts) + 1) * sizeof(uint32_t);
+    return kArriveBytes + (kBalanceGroups + kBalanceGroups / kArriveGroup) * (static_cast<size_t>(experts) * sizeof(uint64_t) + sizeof(uint32_t));
 }
 
 extern "C" int bagua_balance_stats(int dtype, const void* const* logits, size_t ld, const size_t* tokens, int k, int experts,
@@ -652,16 +669,26 @@ extern "C" int bagua_balance_stats(int dtype, const void* const* logits, size_t 
     int status = BAGUA_OK;
     with_layout<true>(dtype, experts, [&](auto layout, auto type) {
         typedef decltype(layout) Lay;
-        if (!tiles_of(ws, Lay::UNROLL * kWave / Lay::L)) {
-            status = BAGUA_ERR_UNSUPPORTED;
-            return;
+        auto launch = [&](auto chosen) -> int {
+            typedef decltype(chosen) C;
+            if (!tiles_of(ws, C::UNROLL * kWave / C::L)) return BAGUA_ERR_UNSUPPORTED;
+            const uint32_t tiles = ws.first_tile[BAGUA_MAX_WORKERS];
+            const dim3 grid(std::min<uint32_t>(std::max<uint32_t>((tiles + C::WAVES - 1) / C::WAVES, 1), kBalanceGroups)), block(kWave * C::WAVES);
+            const size_t lds = (static_cast<size_t>(sum_rows(C::WAVES, experts)) * e + ((e + 1) << lg)) * sizeof(float);
+            launch_kernel(k_balance_stats<decltype(type)::value, C::VEC, C::L, C::NV, C::UNROLL, C::WAVES>, grid, block, lds, static_cast<hipStream_t>(stream),
+                          ws, ld, ids_ld, id_bytes, tiles, per_k, lg, static_cast<uint32_t*>(workspace), out);
+            return launch_status();
+        };
+        // Rows of a wave at a time, 64 / L, in short launches one after another in different waves rather than together in one.  Together | apart:
+        // 100 tokens of 8 experts 6.7 | 5.4 us, 1000 8.2 | 6.6, 32768 15.0 | 11.2; 1000 of 64 11.2 | 10.1, 4096 12.3 | 10.2, 2 x 8192 12.6 | 15.8; 1000 of 256
+        // 11.8 | 10.4, 4096 12.9 | 15.1.  Not where that would make more than one group of one: 100 of 256 7.7 | 9.9.
+        size_t units = 0, tiles = 0;
+        for (int w = 0; w < k; ++w) {
+            units += (tokens[w] + kWave / Lay::L - 1) / (kWave / Lay::L);
+            tiles += (tokens[w] + Lay::UNROLL * kWave / Lay::L - 1) / (Lay::UNROLL * kWave / Lay::L);
         }
-        const uint32_t tiles = ws.first_tile[BAGUA_MAX_WORKERS];
-        const dim3 grid(std::min<uint32_t>(std::max<uint32_t>((tiles + Lay::WAVES - 1) / Lay::WAVES, 1), kBalanceGroups)), block(kWave * Lay::WAVES);
-        const size_t lds = (static_cast<size_t>(sum_rows(Lay::WAVES, experts)) * e + ((e + 1) << lg)) * sizeof(float);
-        launch_kernel(k_balance_stats<decltype(type)::value, Lay::VEC, Lay::L, Lay::NV, Lay::UNROLL, Lay::WAVES>, grid, block, lds,
-                      static_cast<hipStream_t>(stream), ws, ld, ids_ld, id_bytes, tiles, per_k, lg, static_cast<uint32_t*>(workspace), out);
-        status = launch_status();
+        if (units <= Lay::WAVES || (tiles > Lay::WAVES && units <= 512)) status = launch(Layout<Lay::VEC, Lay::L, Lay::NV, 1, Lay::WAVES>());
+        else status = launch(layout);
     });
     return status;
 }

@@ -257,41 +257,51 @@ inline int pace_for(size_t elements_per_launch) { return elements_per_launch >= 
 // so nothing has to be written back from a cache, which an atomic with release semantics would do, 1 - 2 us for every group that
 // ends (forward pass of the balance loss, 256 groups: 102 us with a fence in every thread, 36 in one, 29 without).  The last group drops
 // what its own caches hold and reads with ordinary loads, many in flight.
-// The counters: one for every kArriveGroup groups, whose last one counts at the one of all, each in a line of its own; a counter takes one
-// group after another, 13 ns apiece.  They are 0 before the launch, and left so.  At most kArriveMost groups.
-constexpr unsigned kArriveGroup = 16, kArriveMost = kArriveGroup * kArriveGroup;
-constexpr size_t kArriveLine = 64, kArriveBytes = kArriveLine * (1 + kArriveGroup);
+// The counters: one for every cluster of kArriveGroup groups, whose last one counts at the one of all, each in a line of its own; a counter
+// takes one group after another, 13 ns apiece, and the way to a second one is another round trip, 0.9 us.  They are 0 before the launch, and
+// left so.  At most kArriveMost groups.
+constexpr unsigned kArriveGroup = 16, kArriveMost = kArriveGroup * kArriveGroup, kArriveDirect = 2 * kArriveGroup;
+constexpr size_t kArriveLine = 64, kArriveBytes = kArriveLine * (1 + kArriveMost / kArriveGroup);
 template <typename T>
 __device__ __forceinline__ void publish(T* p, T v)
 {
     __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ bool counted_last(uint32_t* counter, uint32_t of)
+__device__ __forceinline__ bool counted_last(uint32_t* counter, uint32_t of)     // by one thread
 {
     const bool last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == of - 1;
     if (last) publish(counter, 0u);
     return last;
 }
-__device__ __forceinline__ bool last_to_arrive(uint32_t* counters, bool* flag /* in LDS */)
+__device__ __forceinline__ uint32_t clusters() { return (gridDim.x + kArriveGroup - 1) / kArriveGroup; }
+__device__ __forceinline__ uint32_t cluster_groups(uint32_t cluster) { return min(kArriveGroup, gridDim.x - cluster * kArriveGroup); }
+__device__ __forceinline__ bool counted_last_of_cluster(uint32_t* counters)
+{
+    const uint32_t mine = blockIdx.x / kArriveGroup;
+    return counted_last(counters + (1 + mine) * (kArriveLine / sizeof(uint32_t)), cluster_groups(mine));
+}
+// For the whole workgroup: what one thread finds out when the stores of all of them have arrived.  `flag`: in LDS.
+template <typename F>
+__device__ __forceinline__ bool after_arrival(bool* flag, const F& count)
 {
     pace_loads();
     __syncthreads();
-    if (threadIdx.x == 0) {
-        bool last = true;
-        uint32_t all = gridDim.x;
-        if (gridDim.x > 2 * kArriveGroup) {        // (the second counter is another round trip, 0.9 us)
-            const uint32_t mine = blockIdx.x / kArriveGroup;
-            all = (gridDim.x + kArriveGroup - 1) / kArriveGroup;
-            last = counted_last(counters + (1 + mine) * (kArriveLine / sizeof(uint32_t)), min(kArriveGroup, gridDim.x - mine * kArriveGroup));
-        }
-        if (last) last = counted_last(counters, all);
-        *flag = last;
-    }
+    if (threadIdx.x == 0) *flag = count();
     __syncthreads();
     if (!*flag) return false;
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
     return true;
 }
+// The last group of all; or in two steps, the last one of its cluster, and then the last cluster.
+__device__ __forceinline__ bool last_to_arrive(uint32_t* counters, bool* flag)
+{
+    return after_arrival(flag, [&] {
+        if (gridDim.x <= kArriveDirect) return counted_last(counters, gridDim.x);
+        return counted_last_of_cluster(counters) && counted_last(counters, clusters());
+    });
+}
+__device__ __forceinline__ bool last_of_cluster(uint32_t* counters, bool* flag) { return after_arrival(flag, [&] { return counted_last_of_cluster(counters); }); }
+__device__ __forceinline__ bool last_cluster(uint32_t* counters, bool* flag) { return after_arrival(flag, [&] { return counted_last(counters, clusters()); }); }
 
 // Index of this wavefront in its workgroup, as a scalar.  The compiler cannot tell that threadIdx.x >> 6 is the same
 // in all 64 lanes and would carry every row offset and tail test derived from it through 64-bit vector arithmetic
