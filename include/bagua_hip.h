@@ -27,6 +27,8 @@
  *     a multiple of 256 in [256, 16384]; nc = ceil(n / C); the last chunk may be short.
  *   - All arithmetic is IEEE binary32, one rounding per operation in a fixed order (no fused
  *     multiply-add), so results are reproducible bit for bit.  Inputs must be finite.
+ *   - The calls over plans of many tensors and those of the balance loss, further down, have other
+ *     types, alignments and roundings, and take any input; each says its own.
  *   - The primitives return averages (the paper states sums): the sum over workers in
  *     ascending index order is multiplied by fl(1/k), on the ring by fl(1/3).
  *   - Error compensation follows the C_LP_S equations with the stored error carried in as

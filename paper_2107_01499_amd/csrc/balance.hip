@@ -268,7 +268,12 @@ __host__ __device__ constexpr int sum_rows(int waves, int experts)
     return rows;
 }
 
-// The forward pass.  Dynamic LDS: float sums[sum_rows][experts], then uint32 counters[(experts + 1) << lg]: 2^lg copies of each, one of
+// The forward pass: over the rows that count, the sums of softmax(row)[e] and how often expert e was chosen.  A wave takes one tile after another
+// and keeps its sums in registers, a group joins its waves' in LDS, and the group that ends last adds up the groups' in a fixed order and forms
+// the loss, so that one launch reads each logit and choice once and no sum depends on which group came first.  Bound by what comes before and
+// after the loop, not by memory: 8 workers' 32768 rows of 64, bf16, 20.7 us, where the 41 MB are read in 6: the launch, the wait for the first rows
+// and the meeting of 256 groups are 10 to 13.  Long ones by the vector ALU (524288 x 256, bf16, 67 us, 4.1 TB/s).
+// Dynamic LDS: float sums[sum_rows][experts], then uint32 counters[(experts + 1) << lg]: 2^lg copies of each, one of
 // which a lane adds to, so that popular experts are not waited for.  Workspace: counters (last_to_arrive), then every workgroup's sums and counts.
 template <int TYPE, int VEC, int L, int NV, int UNROLL, int WAVES>
 __global__ void __launch_bounds__(kWave * WAVES)
@@ -496,7 +501,10 @@ k_balance_loss(const int32_t* __restrict__ counts, const float* __restrict__ pro
                       [&](int e) { return static_cast<double>(prob[e]); }, part);
 }
 
-// The backward pass: the probabilities are formed again from the logits, which are read anyway.
+// The backward pass: with p the softmax of a row and w[e] = coefficient * count[e], the gradient is p[e] * (w[e] - sum of w[j] * p[j]), 0 in a
+// row that does not count.  The probabilities are formed again from the logits, which costs no second reading: a row stays in its lanes from
+// the one load to the one store, so the pass reads and writes each logit once.  Bound by memory: 524288 rows of 256, bf16, 89.5 us, 6.0 TB/s,
+// where a copy of as many bytes takes 78; 4 x 4099 rows of 60, fp32, 4.6 us, of which all but 1 is launching.
 template <int TYPE, int VEC, int L, int NV, int UNROLL>
 __global__ void __launch_bounds__(kWave * kGradWaves, NV == 1 ? 7 : 1)
 k_balance_grad(Workers ws, size_t ld, size_t ld_out, uint32_t tiles, int experts, const float* __restrict__ weight, const float* __restrict__ upstream)
@@ -579,7 +587,7 @@ inline void with_vectors(int experts, const F& f)
     else if constexpr (V == 4) f(Layout<V, 64, 8, 1, 8>());
 }
 // 16 bytes of a row in a lane: a wider vector of fp32 is two accesses that each leave out every other 16 bytes, and a store of half a
-// line costs a whole one (gradient of 1 M rows of 64, fp32: eight elements 101.8 us, four E64).
+// line costs a whole one (gradient of 1 M rows of 64, fp32: eight elements 101.8 us, four 82).
 template <bool FORWARD, typename F>
 inline void with_layout(int dtype, int experts, const F& f)
 {
