@@ -115,6 +115,11 @@ struct Row {
             if (there) q[j] = __builtin_nontemporal_load(reinterpret_cast<const raw*>(row + at(j, experts)));
         }
     }
+    __device__ __forceinline__ void keep_if(bool there)
+    {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) q[j] = there ? q[j] : raw(0);
+    }
     // The lane's elements as fp32, and the row's largest.
     __device__ __forceinline__ float largest(float (&x)[NV][VEC]) const
     {
@@ -271,8 +276,8 @@ __host__ __device__ constexpr int sum_rows(int waves, int experts)
 // The forward pass: over the rows that count, the sums of softmax(row)[e] and how often expert e was chosen.  A wave takes one tile after another
 // and keeps its sums in registers, a group joins its waves' in LDS, and the group that ends last adds up the groups' in a fixed order and forms
 // the loss, so that one launch reads each logit and choice once and no sum depends on which group came first.  Bound by what comes before and
-// after the loop, not by memory: 8 workers' 32768 rows of 64, bf16, 20.7 us, where the 41 MB are read in 6: the launch, the wait for the first rows
-// and the meeting of 256 groups are 10 to 13.  Long ones by the vector ALU (524288 x 256, bf16, 67 us, 4.1 TB/s).
+// after the loop, not by memory: 8 workers' 32768 rows of 64, bf16, 20.4 us, where the 41 MB are read in 6: the launch, the wait for the first rows
+// and the meeting of 256 groups are 10 to 13.  Long ones by the vector ALU (524288 x 256, bf16, 64.7 us, 4.4 TB/s).
 // Dynamic LDS: float sums[sum_rows][experts], then uint32 counters[(experts + 1) << lg]: 2^lg copies of each, one of
 // which a lane adds to, so that popular experts are not waited for.  Workspace: counters (last_to_arrive), then every workgroup's sums and counts.
 template <int TYPE, int VEC, int L, int NV, int UNROLL, int WAVES>
@@ -318,7 +323,7 @@ k_balance_stats(Workers ws, size_t ld, size_t ids_ld, int id_bytes, uint32_t til
     R row[UNROLL];
     uint8_t flag[UNROLL];
     Choice ahead[kAhead];
-    // No load stands behind a test of another one of the tile except the rows behind their flags.
+    // No load stands behind a test of another one of the tile except the rows behind their flags, from a wave's second tile on.
     auto ask = [&](const Tile& k) {
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) flag[u] = flag_of(k, u * R::kRows + own_row);
@@ -338,7 +343,15 @@ k_balance_stats(Workers ws, size_t ld, size_t ids_ld, int id_bytes, uint32_t til
     if (tile < tiles) {
         Tile k = tile_of<kRows>(table, tile, tiles);
         ask(k);
-        ask_rows(k);
+        // The first tile's rows do not wait for their flags: those that do not count are read and dropped.  32768 x 128, bf16, 15.3 -> 14.5 us.
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+            row[u].load(table_ptr<const typename R::one>(k.logits) + (k.t0 + min(u * R::kRows + own_row, k.rows - 1)) * ld, experts, true);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            counts[u] = counts_in(k, u * R::kRows + own_row, flag[u]);
+            row[u].keep_if(counts[u]);
+        }
         while (k.there) {
             // the present tile's rows arrive; the next one's flags and choices, and then its rows, are on their way while the present
             // one is worked on
@@ -503,7 +516,7 @@ k_balance_loss(const int32_t* __restrict__ counts, const float* __restrict__ pro
 
 // The backward pass: with p the softmax of a row and w[e] = coefficient * count[e], the gradient is p[e] * (w[e] - sum of w[j] * p[j]), 0 in a
 // row that does not count.  The probabilities are formed again from the logits, which costs no second reading: a row stays in its lanes from
-// the one load to the one store, so the pass reads and writes each logit once.  Bound by memory: 524288 rows of 256, bf16, 89.5 us, 6.0 TB/s,
+// the one load to the one store, so the pass reads and writes each logit once.  Bound by memory: 524288 rows of 256, bf16, 85.1 us, 6.3 TB/s,
 // where a copy of as many bytes takes 78; 4 x 4099 rows of 60, fp32, 4.6 us, of which all but 1 is launching.
 template <int TYPE, int VEC, int L, int NV, int UNROLL>
 __global__ void __launch_bounds__(kWave * kGradWaves, NV == 1 ? 7 : 1)
@@ -528,12 +541,20 @@ k_balance_grad(Workers ws, size_t ld, size_t ld_out, uint32_t tiles, int experts
         bool counts[UNROLL];
         float e[UNROLL][NV][VEC], most[UNROLL];
         auto token = [&](int u) { return k.t0 + min(static_cast<uint32_t>(u) * R::kRows + own_row, k.rows - 1); };
+        if (k.mask == 0) {                                      // nothing to wait for: 524288 x 256, bf16, 89.9 -> 85.1 us, 32768 x 128 6.1 -> 5.2
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) flag[u] = flag_of(k, u * R::kRows + own_row);
+            for (int u = 0; u < UNROLL; ++u) {
+                counts[u] = u * R::kRows + own_row < k.rows;
+                row[u].load(table_ptr<const one>(k.logits) + token(u) * ld, experts, true);
+            }
+        } else {
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            counts[u] = counts_in(k, u * R::kRows + own_row, flag[u]);
-            row[u].load(table_ptr<const one>(k.logits) + token(u) * ld, experts, counts[u]);
+            for (int u = 0; u < UNROLL; ++u) flag[u] = flag_of(k, u * R::kRows + own_row);
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                counts[u] = counts_in(k, u * R::kRows + own_row, flag[u]);
+                row[u].load(table_ptr<const one>(k.logits) + token(u) * ld, experts, counts[u]);
+            }
         }
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) most[u] = row[u].largest(e[u]);
@@ -546,7 +567,7 @@ k_balance_grad(Workers ws, size_t ld, size_t ld_out, uint32_t tiles, int experts
             for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) dot = __builtin_fmaf(e[u][j][i], g[j][i] * own[j][i], dot);
-            // (rows that do not count were read as zeros)
+            // (rows that do not count were read as zeros, or do not exist and are not stored)
             const float scale = counts[u] ? inverse * up : 0.0f, shift = -(lanes_reduce<L>(dot, OpAddF()) * inverse) * scale;
             one* out = table_ptr<one>(k.other) + token(u) * ld_out;
 #pragma unroll
