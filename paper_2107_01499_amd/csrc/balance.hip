@@ -248,19 +248,21 @@ struct BalanceOut {
 template <int THREADS, typename COUNT, typename PROB>
 __device__ __forceinline__ void balance_loss(const BalanceOut& o, int32_t tokens, const COUNT& count, const PROB& prob, double* part)
 {
-    const double n = tokens;
-    const double scale = tokens > 0 ? o.alpha * o.experts / (static_cast<double>(o.top_k) * n * n) : 0.0;
+    const int waves = min(THREADS, o.experts + kWave - 1) / kWave;     // that have an expert: the others would take the time of these
     double sum = 0.0;
-    for (int e = threadIdx.x; e < o.experts; e += THREADS) {
-        const double w = scale * count(e);
-        o.weight[e] = static_cast<float>(w);
-        if (tokens > 0) sum += w * prob(e);
+    if (wave_index() < waves) {
+        const double n = tokens, scale = tokens > 0 ? o.alpha * o.experts / (static_cast<double>(o.top_k) * n * n) : 0.0;
+        for (int e = threadIdx.x; e < o.experts; e += THREADS) {
+            const double w = scale * count(e), p = prob(e);
+            o.weight[e] = static_cast<float>(w);
+            if (tokens > 0) sum += w * p;
+        }
+        sum = wave_sum(sum);
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x / kWave] = sum;
     }
-    sum = wave_sum(sum);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x / kWave] = sum;
-    __syncthreads();
+    if (waves > 1) __syncthreads();
     if (threadIdx.x >= kWave) return;
-    sum = wave_sum(threadIdx.x < THREADS / kWave ? part[threadIdx.x] : 0.0);
+    if (waves > 1) sum = wave_sum(static_cast<int>(threadIdx.x) < waves ? part[threadIdx.x] : 0.0);
     if (threadIdx.x == 0) o.loss[0] = static_cast<float>(sum);
 }
 
@@ -276,8 +278,8 @@ __host__ __device__ constexpr int sum_rows(int waves, int experts)
 // The forward pass: over the rows that count, the sums of softmax(row)[e] and how often expert e was chosen.  A wave takes one tile after another
 // and keeps its sums in registers, a group joins its waves' in LDS, and the group that ends last adds up the groups' in a fixed order and forms
 // the loss, so that one launch reads each logit and choice once and no sum depends on which group came first.  Bound by what comes before and
-// after the loop, not by memory: 8 workers' 32768 rows of 64, bf16, 20.4 us, where the 41 MB are read in 6: the launch, the wait for the first rows
-// and the meeting of 256 groups are 10 to 13.  Long ones by the vector ALU (524288 x 256, bf16, 64.7 us, 4.4 TB/s).
+// after the loop, not by memory: 8 workers' 32768 rows of 64, bf16, 20.0 us, where the 41 MB are read in 6: the launch, the wait for the first rows
+// and the meeting of 256 groups are 9 to 12.  Long ones by the vector ALU (524288 x 256, bf16, 64.7 us, 4.4 TB/s).
 // Dynamic LDS: float sums[sum_rows][experts], then uint32 counters[(experts + 1) << lg]: 2^lg copies of each, one of
 // which a lane adds to, so that popular experts are not waited for.  Workspace: counters (last_to_arrive), then every workgroup's sums and counts.
 template <int TYPE, int VEC, int L, int NV, int UNROLL, int WAVES>
@@ -420,13 +422,25 @@ k_balance_stats(Workers ws, size_t ld, size_t ids_ld, int id_bytes, uint32_t til
         return c;
     };
     auto finish = [&](auto&& count, auto&& prob) {       // by what the whole workgroup sees
-        for (int e = threadIdx.x; e <= experts; e += kThreads) {
-            o.counts[e] = static_cast<int32_t>(count(e));
-            if (e < experts) o.prob[e] = prob(e);
+        auto count_out = [&](int e) {
+            const int32_t c = static_cast<int32_t>(count(e));
+            o.counts[e] = c;
+            return static_cast<double>(c);
+        };
+        auto prob_out = [&](int e) {
+            const float p = prob(e);
+            o.prob[e] = p;
+            return static_cast<double>(p);
+        };
+        if (threadIdx.x == 0) o.counts[experts] = static_cast<int32_t>(count(experts));
+        if (o.loss) {
+            balance_loss<kThreads>(o, static_cast<int32_t>(count(experts)), count_out, prob_out, part);
+        } else {
+            for (int e = threadIdx.x; e < experts; e += kThreads) {
+                count_out(e);
+                prob_out(e);
+            }
         }
-        if (o.loss)
-            balance_loss<kThreads>(o, static_cast<int32_t>(count(experts)), [&](int e) { return static_cast<double>(count(e)); },
-                                   [&](int e) { return static_cast<double>(prob(e)); }, part);
     };
     if (gridDim.x == 1) {
         finish(copies, wave_sums);
@@ -446,36 +460,51 @@ k_balance_stats(Workers ws, size_t ld, size_t ids_ld, int id_bytes, uint32_t til
     __shared__ uint32_t slice_count[kThreads];
     int width = 1;                                          // threads of a slice, a power of two
     while (width < experts && width < kThreads) width *= 2;
-    const uint32_t slices = kThreads / width, slice = threadIdx.x / width;
-    // The sums over `n` rows of pairs, by as many threads per expert as there are, in a fixed order: in sums and counters.
+    const uint32_t slices = kThreads / width, slice = threadIdx.x / width, column = threadIdx.x & (width - 1);
+    // The sums over `n` rows of pairs, by as many threads per expert as there are, in a fixed order: in sums and counters.  One group does it
+    // while the chip waits, so it takes few instructions (32-bit indexes, no more rows asked for than there are, no test where all are there) and
+    // the lanes of one expert together first: with the loss left to the waves that have experts, 4096 x 64, bf16, 11.7 -> 10.0 us, 500 x 8 5.4 -> 5.0.
     auto together = [&](uint32_t row, uint32_t n) {
         static_assert(kThreads >= kBalanceGroups, "a thread for every row");
         uint32_t all = threadIdx.x < n ? pair_tokens[row + threadIdx.x] : 0;
         for (int e0 = 0; e0 < experts; e0 += width) {
-            const int e = e0 + threadIdx.x % width;
+            const int e = e0 + column;
+            const uint32_t step = slices * experts, first = row * experts + min(e, experts - 1), last_one = first + (n - 1) * experts;
+            uint32_t at = first + slice * experts, taken = 0;   // taken: rows, by all slices
             double s = 0.0;
             uint32_t c = 0;
-            const uint64_t* from = pairs + static_cast<size_t>(row) * experts + min(e, experts - 1);
-            // sixteen at a time and without a test before a load, or each would be waited for
-            for (uint32_t g = slice; g < n; g += 16 * slices) {
-                uint64_t pair[16];
+            // N rows of a slice; without a test before a load, or each would be waited for
+            auto add = [&](auto batch, auto all_there) {
+                constexpr int N = decltype(batch)::value;
+                uint64_t pair[N];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) pair[i] = from[static_cast<size_t>(min(g + i * slices, n - 1)) * experts];
+                for (int i = 0; i < N; ++i) pair[i] = pairs[decltype(all_there)::value ? at + i * step : min(at + i * step, last_one)];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    if (g + i * slices >= n) pair[i] = 0;
+                for (int i = 0; i < N; ++i) {
+                    if (!decltype(all_there)::value && taken + i * slices + slice >= n) pair[i] = 0;
                     s += __uint_as_float(static_cast<uint32_t>(pair[i]));
                     c += static_cast<uint32_t>(pair[i] >> 32);
                 }
+                at += N * step;
+                taken += N * slices;
+            };
+            while (taken + 16 * slices <= n) add(std::integral_constant<int, 16>(), std::true_type());
+            if (taken + 4 * slices < n) add(std::integral_constant<int, 16>(), std::false_type());
+            else if (taken + slices < n) add(std::integral_constant<int, 4>(), std::false_type());
+            else if (taken < n) add(std::integral_constant<int, 1>(), std::false_type());
+            for (int d = kWave / 2; d >= width; d /= 2) {
+                s += __shfl_xor(s, d);
+                c += __shfl_xor(c, d);
             }
-            slice_sum[threadIdx.x] = s;
-            slice_count[threadIdx.x] = c;
+            const uint32_t parts = kThreads / max(width, kWave), mine = threadIdx.x / max(width, kWave) * width + column;
+            slice_sum[mine] = s;                                // (lanes of one expert have the same)
+            slice_count[mine] = c;
             __syncthreads();
             if (slice == 0 && e < experts) {
-#pragma unroll 8
-                for (uint32_t i = 1; i < slices; ++i) {
-                    s += slice_sum[i * width + threadIdx.x];
-                    c += slice_count[i * width + threadIdx.x];
+#pragma unroll 4
+                for (uint32_t i = 1; i < parts; ++i) {
+                    s += slice_sum[i * width + column];
+                    c += slice_count[i * width + column];
                 }
                 sums[e] = static_cast<float>(s);
                 counters[e] = c;
@@ -483,9 +512,10 @@ k_balance_stats(Workers ws, size_t ld, size_t ids_ld, int id_bytes, uint32_t til
             if (e0 == 0 && threadIdx.x == 0) counters[experts] = 0;
             __syncthreads();
         }
-#pragma unroll
-        for (int s = 32; s > 0; s >>= 1) all += __shfl_xor(all, s);
-        if (lane == 0 && all) atomicAdd(counters + experts, all);
+        if (wave * kWave < static_cast<int>(n)) {
+            all = lanes_reduce<kWave>(all, [](uint32_t a, uint32_t b) { return a + b; });
+            if (lane == 0 && all) atomicAdd(counters + experts, all);
+        }
         __syncthreads();
     };
     auto summed_count = [&](int e) { return counters[e]; };
@@ -711,6 +741,7 @@ extern "C" int bagua_balance_stats(int dtype, const void* const* logits, size_t 
         // Rows of a wave at a time, 64 / L, in short launches one after another in different waves rather than together in one.  Together | apart:
         // 100 tokens of 8 experts 6.7 | 5.4 us, 1000 8.2 | 6.6, 32768 15.0 | 11.2; 1000 of 64 11.2 | 10.1, 4096 12.3 | 10.2, 2 x 8192 12.6 | 15.8; 1000 of 256
         // 11.8 | 10.4, 4096 12.9 | 15.1.  Not where that would make more than one group of one: 100 of 256 7.7 | 9.9.
+        // (All of them before the groups' sums were put together in fewer instructions, which takes 0.4 to 1.8 us from both sides.)
         size_t units = 0, tiles = 0;
         for (int w = 0; w < k; ++w) {
             units += (tokens[w] + kWave / Lay::L - 1) / (kWave / Lay::L);

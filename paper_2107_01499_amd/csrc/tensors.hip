@@ -358,7 +358,8 @@ __device__ __forceinline__ bool adamw_share(const TensorEntry& d, size_t e0, int
 }
 
 // The step (in the order and with the roundings of bagua_hip.h): m = beta1 m + (1 - beta1) g, v = beta2 v + (1 - beta2) g^2,
-// p = (1 - lr decay) p - rate m / (root sqrt(v) + eps), every element by itself, read and written once; with 8 bits a wave holds whole blocks, so a block's new scale is an exchange among its lanes and the states are
+// p = (1 - lr decay) p - rate m / (root sqrt(v) + eps), every element by itself, read and written once; with 8 bits a wave holds whole
+// blocks, so that the new scale of a block is an exchange among its lanes and the states are
 // not read again.  A workgroup is one wave, which ends as soon as its own rows are written.  32-bit states: bound by memory, 335 M elements with bf16
 // gradients and copies 1436 us, 6.5 TB/s, 25.6 M fp32 109 us, 6.6 TB/s.  8-bit states: bound by the vector ALU, bf16 parameters and gradients,
 // 335 M elements, 574 us, 5.9 TB/s; with fp32 parameters and bf16 copies, 109 M, 278 us, 6.3 TB/s.
