@@ -362,7 +362,7 @@ __device__ __forceinline__ bool adamw_share(const TensorEntry& d, size_t e0, int
 // blocks, so that the new scale of a block is an exchange among its lanes and the states are
 // not read again.  A workgroup is one wave, which ends as soon as its own rows are written.  32-bit states: bound by memory, 335 M elements with bf16
 // gradients and copies 1436 us, 6.5 TB/s, 25.6 M fp32 109 us, 6.6 TB/s.  8-bit states: bound by the vector ALU, bf16 parameters and gradients,
-// 335 M elements, 574 us, 5.9 TB/s; with fp32 parameters and bf16 copies, 109 M, 278 us, 6.3 TB/s.
+// 335 M elements, 574 to 583 us, 5.8 TB/s; with fp32 parameters and bf16 copies, 109 M, 278 us, 6.3 TB/s.
 template <int G, int P, int C, int BITS>
 __global__ void __launch_bounds__(kWave)
 k_adamw(const TensorEntry* __restrict__ entries, const uint32_t* __restrict__ tile_tensor, AdamArgs a)
