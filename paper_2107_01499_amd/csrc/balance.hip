@@ -133,7 +133,9 @@ struct Row {
             }
         return lanes_most<L>(most);
     }
-    // x = exp(x - most); the value: 1 / sum of the row's.
+    // x = exp(x - most).  Not HUGE: log2(e) times both, and then the difference, in one fused operation; the rounding of the product with `most`
+    // is the same factor on all of a row, which the sum takes out again as long as it is near 1.  HUGE: the difference first, which costs an
+    // operation more, and is right whatever the magnitude.
     template <bool HUGE>
     static __device__ __forceinline__ void exponentials(float (&x)[NV][VEC], float most)
     {
@@ -142,7 +144,7 @@ struct Row {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i)   // the rounding of the shift is the same factor on all of a row
+            for (int i = 0; i < VEC; ++i)
                 x[j][i] = __builtin_amdgcn_exp2f(HUGE ? (x[j][i] - top) * kLog2e : __builtin_fmaf(x[j][i], kLog2e, shift));
     }
     static __device__ __forceinline__ float reciprocal_sum(const float (&own)[NV][VEC], const float (&e)[NV][VEC])
@@ -171,8 +173,9 @@ __device__ __forceinline__ void exponentials_of(float (&e)[U][NV][VEC], const fl
 {
     bool huge = false;
 #pragma unroll
-    for (int u = 0; u < U; ++u) huge |= fabsf(most[u]) > 0x1p126f;
-    // a largest one that leaves fp32 when it is multiplied: the type's lowest number, or an infinity
+    for (int u = 0; u < U; ++u) huge |= fabsf(most[u]) > 0x1p20f;
+    // up to 2^20 the shift is off by 2^-4 at most, half a unit of its last place: 4 % on all of a row.  Beyond 2^31 it would be off by more than 128,
+    // and leave nothing but zeros or infinities of the row
     if (may_be_huge && __any(huge)) {
 #pragma unroll
         for (int u = 0; u < U; ++u) R::template exponentials<true>(e[u], most[u]);
