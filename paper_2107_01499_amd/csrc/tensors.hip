@@ -195,6 +195,12 @@ struct AdamArgs {
 // The largest magnitude of four, as the bits of a number that is not negative: these are ordered as the numbers are, and across
 // lanes the integer maximum comes without the instructions that make a NaN quiet.
 __device__ __forceinline__ uint32_t most_of(f4 x) { return __float_as_uint(fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(x.z), fabsf(x.w)))); }
+// Of four roots: none is negative, and what is no number (also the root of what has left fp32 in its scaled form, see root_in_range) is above
+// all numbers in this order, where fmaxf would pass over it.
+__device__ __forceinline__ uint32_t most_of_roots(f4 x)
+{
+    return max(max(__float_as_uint(x.x), __float_as_uint(x.y)), max(__float_as_uint(x.z), __float_as_uint(x.w)));
+}
 struct OpMaxU { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); } };
 
 // The largest of each of K blocks of 256 values, of which every lane holds one: that of block k in the 64 / K lanes from k * 64 / K on.
@@ -220,7 +226,7 @@ __device__ __forceinline__ uint32_t blocks_most(const uint32_t (&x)[K])
 //   quotient:  with the correctly rounded reciprocal of b (reciprocal_in_range) the remainder of
 //              a quotient that is a unit off at most is exact, and adding its product with the reciprocal rounds to the quotient.
 constexpr float kFirstScale = 0x1p64f, kSecondScale = 0x1p64f, kRootScale = 0x1p32f;
-__device__ __forceinline__ float root_in_range(float t)   // 0, or 2^-90 <= t < 2^126
+__device__ __forceinline__ float root_in_range(float t)   // 0, or 2^-90 <= t < 2^126; infinity gives no number
 {
     const float y = __builtin_amdgcn_rsqf(fmaxf(t, 0x1p-90f)), g = t * y;
     return __builtin_fmaf(__builtin_fmaf(-g, g, t), 0.5f * y, g);
@@ -230,7 +236,8 @@ __device__ __forceinline__ float quotient_in_range(float a, float b)   // 2^-40 
     const float y = reciprocal_in_range(b), q = a * y;
     return __builtin_fmaf(-__builtin_fmaf(b, q, -a), y, q);             // (the remainder's sign keeps that of a zero)
 }
-// Blocks that keep to the ranges: first moments up to 2^20, roots up to 2^10 (in their scaled forms).  What is no number does not.
+// Blocks that keep to the ranges: first moments up to 2^20, roots up to 2^10 (in their scaled forms).  A root that is no number does not; a second
+// moment of 2^64 and more is one of these.
 constexpr float kMostFirst = 0x1p84f, kMostRoot = 0x1p42f;
 inline bool in_range(float root, float eps) { return root <= 0x1p10f && eps >= 0x1p-40f && eps <= 1.0f; }
 
@@ -304,7 +311,7 @@ __device__ __forceinline__ bool adamw_share(const TensorEntry& d, size_t e0, int
                 clear_absent(r[k], e, left);
             }
             m_most[k] = most_of(m[k]);
-            r_most[k] = most_of(r[k]);
+            r_most[k] = FAST ? most_of_roots(r[k]) : most_of(r[k]);
             if (FAST) over |= static_cast<uint32_t>(m_most[k] > __float_as_uint(kMostFirst)) | static_cast<uint32_t>(r_most[k] > __float_as_uint(kMostRoot));
         }
     }
