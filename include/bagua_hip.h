@@ -448,6 +448,8 @@ int bagua_bucket_flatten_batched_run(const void* const* plans, const size_t* T, 
  *            below 1 where r > 0 and not above 448.  (A step changes r by up to (1-beta2)/2 of itself, far less than half the
  *            distance of two codes; rounded to nearest, r would stay where it is for ever.)
  *            (m and u are formed without the loss that fp32 has below 2^-126.)
+ *            Of a moment that is not finite (a gradient was not, or its square, and no clip kept it out) the code is 127, which stands for NaN,
+ *            and stays so; the scale of its block is formed of the others.
  *   BF16 p:  stochastically, p = high half of (bits of p + random of 16 bits).
  *   random:  h(i) = mix(i/4 * 0x9E3779B9 + mix(tensor * 0x9E3779B9 + seed)) for element i of a tensor, turned left by 8 * (i mod 4),
  *            of which r takes the upper 20 bits; p the upper 16 of mix(h + 0x9E3779B9) turned in the same way;

@@ -133,8 +133,7 @@ __device__ __forceinline__ f4 widen_codes(uint32_t w, float scale)
     const f2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w), true);
     return f4{lo.x * scale, lo.y * scale, hi.x * scale, hi.y * scale};
 }
-// Scale of a block whose largest magnitude is `most`, and its reciprocal; a block that is (nearly) zero has neither, and what is no
-// number stays none.
+// Scale of a block whose largest finite magnitude is `most`, and its reciprocal; a block that is (nearly) zero has neither.
 struct Scale {
     float scale, inverse;
 };
@@ -159,6 +158,7 @@ __device__ __forceinline__ uint32_t nearest_codes(f4 y)
 // y >= 0 times 2^-120 has E4M3's exponent field in the low bits of fp32's own (and its subnormals where fp32 has them), so
 // the bits above the 20 lowest are the code, and what lies below them is how far y is on the way to the next one.  Two codes at a time
 // in the halves of a register; a code is not below 1 where the root is above 0 (its upper half is not zero then) and not above 126.
+// What is not finite gets code 127, E4M3's NaN, by not_finite.
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ u16x2 upper_halves(uint32_t a, uint32_t b) { return __builtin_bit_cast(u16x2, __builtin_amdgcn_perm(b, a, 0x07060302u)); }
 __device__ __forceinline__ uint32_t code_bits(float y, uint32_t random) { return __float_as_uint(y * 0x1p-120f) + (random >> 12); }
@@ -169,6 +169,20 @@ __device__ __forceinline__ u16x2 two_codes(uint32_t a, uint32_t b, float ra, flo
     const u16x2 least = __builtin_elementwise_min(upper_halves(__float_as_uint(ra), __float_as_uint(rb)), one);
     const u16x2 c = __builtin_elementwise_min(upper_halves(a, b) >> static_cast<uint16_t>(4), u16x2{126, 126});
     return __builtin_elementwise_max(c, least);
+}
+// 127 in the bytes of those of four that are not finite, 0 in the others
+__device__ __forceinline__ uint32_t not_finite(f4 x)
+{
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w |= fabsf(x[i]) < INFINITY ? 0u : 127u << (8 * i);
+    return w;
+}
+__device__ __forceinline__ f4 finite(f4 x)   // 0 for those that are not
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = fabsf(x[i]) < INFINITY ? x[i] : 0.0f;
+    return x;
 }
 
 __device__ __forceinline__ uint32_t mix(uint32_t x)
@@ -192,7 +206,7 @@ struct AdamArgs {
     bool in_range;             // see root_in_range
 };
 
-// The largest magnitude of four, as the bits of a number that is not negative: these are ordered as the numbers are, and across
+// The largest magnitude of four (of numbers among them), as the bits of a number that is not negative: these are ordered as the numbers are, and across
 // lanes the integer maximum comes without the instructions that make a NaN quiet.
 __device__ __forceinline__ uint32_t most_of(f4 x) { return __float_as_uint(fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(x.z), fabsf(x.w)))); }
 // Of four roots: none is negative, and what is no number (also the root of what has left fp32 in its scaled form, see root_in_range) is above
@@ -310,8 +324,8 @@ __device__ __forceinline__ bool adamw_share(const TensorEntry& d, size_t e0, int
                 clear_absent(m[k], e, left);
                 clear_absent(r[k], e, left);
             }
-            m_most[k] = most_of(m[k]);
-            r_most[k] = FAST ? most_of_roots(r[k]) : most_of(r[k]);
+            m_most[k] = most_of(FAST ? m[k] : finite(m[k]));
+            r_most[k] = most_of_roots(FAST ? r[k] : finite(r[k]));
             if (FAST) over |= static_cast<uint32_t>(m_most[k] > __float_as_uint(kMostFirst)) | static_cast<uint32_t>(r_most[k] > __float_as_uint(kMostRoot));
         }
     }
@@ -353,8 +367,14 @@ __device__ __forceinline__ bool adamw_share(const TensorEntry& d, size_t e0, int
             const f4 y = r[k] * of_block(iv, k);
             const u16x2 lo = two_codes(code_bits(y.x, turned(h[k], 0)), code_bits(y.y, turned(h[k], 8)), r[k].x, r[k].y);
             const u16x2 hi = two_codes(code_bits(y.z, turned(h[k], 16)), code_bits(y.w, turned(h[k], 24)), r[k].z, r[k].w);
-            put<EDGE>(mp, e, left, __builtin_bit_cast(Four<uint8_t>::v, nearest_codes(m[k] * of_block(im, k))));
-            put<EDGE>(vp, e, left, __builtin_bit_cast(Four<uint8_t>::v, __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x06040200u)));
+            uint32_t mc = nearest_codes(m[k] * of_block(im, k));
+            uint32_t vc = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x06040200u);
+            if (!FAST) {      // (there roots are finite, and so are first moments but for NaN, which the conversion keeps)
+                mc |= not_finite(m[k]);
+                vc |= not_finite(r[k]);
+            }
+            put<EDGE>(mp, e, left, __builtin_bit_cast(Four<uint8_t>::v, mc));
+            put<EDGE>(vp, e, left, __builtin_bit_cast(Four<uint8_t>::v, vc));
         }
         if (lane % kLanes == 0 && (EDGE == kFull || lane / kLanes * kRow < left)) {
             table_ptr<float>(d.m_scale)[e0 / kRow + lane / kLanes] = sm.scale;
