@@ -450,7 +450,7 @@ int bagua_bucket_flatten_batched_run(const void* const* plans, const size_t* T, 
  *            (m and u are formed without the loss that fp32 has below 2^-126.)
  *            Of a moment that is not finite (a gradient was not, or its square, and no clip kept it out) the code is 127, which stands for NaN,
  *            and stays so; the scale of its block is formed of the others.
- *   BF16 p:  stochastically, p = high half of (bits of p + random of 16 bits).
+ *   BF16 p:  stochastically, p = high half of (bits of p + random of 16 bits); NaN stays NaN.
  *   random:  h(i) = mix(i/4 * 0x9E3779B9 + mix(tensor * 0x9E3779B9 + seed)) for element i of a tensor, turned left by 8 * (i mod 4),
  *            of which r takes the upper 20 bits; p the upper 16 of mix(h + 0x9E3779B9) turned in the same way;
  *            mix(x): x ^= x>>16, x *= 0x6A09E667, x ^= x>>15, x *= 0xBB67AE85, x ^= x>>16.   `seed`: another one each step.

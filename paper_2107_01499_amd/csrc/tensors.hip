@@ -193,9 +193,12 @@ __device__ __forceinline__ uint32_t mix(uint32_t x)
 }
 constexpr uint32_t kGolden = 0x9E3779B9u;
 __device__ __forceinline__ uint32_t turned(uint32_t h, int by) { return by == 0 ? h : __builtin_amdgcn_alignbit(h, h, 32 - by); }
+// ANY: also what is no number, whose lower half may be so full that the random bits carry out of it.
+template <bool ANY>
 __device__ __forceinline__ uint16_t random_bf16(float x, uint32_t random)
 {
-    return static_cast<uint16_t>((__float_as_uint(x) + (random >> 16)) >> 16);
+    const uint16_t h = static_cast<uint16_t>((__float_as_uint(x) + (random >> 16)) >> 16);
+    return ANY && x != x ? 0x7fc0 : h;
 }
 
 // ---------------------------------------------------------------- AdamW
@@ -349,8 +352,9 @@ __device__ __forceinline__ bool adamw_share(const TensorEntry& d, size_t e0, int
         if (BITS == 8 || P == BAGUA_BF16) h[k] = mix(random + static_cast<uint32_t>(k) * (kRow / 4 * kGolden));
         if constexpr (P == BAGUA_BF16) {
             const uint32_t w = mix(h[k] + kGolden);
-            put<EDGE>(pp, e, left, h4{random_bf16(p.x, turned(w, 0)), random_bf16(p.y, turned(w, 8)), random_bf16(p.z, turned(w, 16)),
-                                      random_bf16(p.w, turned(w, 24))});
+            constexpr bool kAny = !FAST;      // (there it comes from codes and bf16 parameters alone, whose lower half is empty)
+            put<EDGE>(pp, e, left, h4{random_bf16<kAny>(p.x, turned(w, 0)), random_bf16<kAny>(p.y, turned(w, 8)), random_bf16<kAny>(p.z, turned(w, 16)),
+                                      random_bf16<kAny>(p.w, turned(w, 24))});
         } else {
             put<EDGE>(pp, e, left, p);
         }
