@@ -447,7 +447,7 @@ int bagua_bucket_flatten_batched_run(const void* const* plans, const size_t* T, 
  *            m: y to the nearest E4M3 (ties to even).  r: stochastically, code = floor(E4M3 position of y + random / 2^20), not
  *            below 1 where r > 0 and not above 448.  (A step changes r by up to (1-beta2)/2 of itself, far less than half the
  *            distance of two codes; rounded to nearest, r would stay where it is for ever.)
- *            (m and u are formed without the loss that fp32 has below 2^-126.)
+ *            (m and u are formed without the loss that fp32 has below 2^-126, wherever an element lies and whatever lies beside it.)
  *            Of a moment that is not finite (a gradient was not, or its square, and no clip kept it out) the code is 127, which stands for NaN,
  *            and stays so; the scale of its block is formed of the others.
  *   BF16 p:  stochastically, p = high half of (bits of p + random of 16 bits); NaN stays NaN.

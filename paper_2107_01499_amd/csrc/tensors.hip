@@ -255,18 +255,63 @@ __device__ __forceinline__ float quotient_in_range(float a, float b)   // 2^-40 
 }
 // Blocks that keep to the ranges: first moments up to 2^20, roots up to 2^10 (in their scaled forms).  A root that is no number does not; a second
 // moment of 2^64 and more is one of these.
+// Of the step's own factors: with these a first moment is 0 or 2^-101 and more in its scaled form, for its terms are 0 or at least 2^-9 * 2^-62 * beta1 (the
+// smallest code and scale) and 2^-85 * (1 - beta1), and their difference a multiple of the smaller one's last place; and the scale is taken out of
+// the rate without rounding.
 constexpr float kMostFirst = 0x1p84f, kMostRoot = 0x1p42f;
-inline bool in_range(float root, float eps) { return root <= 0x1p10f && eps >= 0x1p-40f && eps <= 1.0f; }
+inline bool in_range(float beta1, float omb1, float root, float eps, float rate)
+{
+    return (beta1 == 0.0f || beta1 >= 0x1p-6f) && omb1 >= 0x1p-15f && root <= 0x1p10f && eps >= 0x1p-40f && eps <= 1.0f &&
+           (rate == 0.0f || std::fabs(rate) >= 0x1p-62f);
+}
+
+// The general form's first moments: those below 2^-60 are held times kFirstScale, as all of the other form are, for fp32 ends for them as well; their bits
+// are set in `small`.  Where no end is near every operation rounds alike with and without a scale, so that a result does not show in
+// which form it was found.
+__device__ __forceinline__ f4 first_moments(uint32_t codes, float scale, f4 g, float beta1, float omb1, uint32_t& small)
+{
+    const f4 scaled = widen_codes(codes, scale * kFirstScale) * beta1 + g * (omb1 * kFirstScale);
+    f4 m = widen_codes(codes, scale) * beta1 + g * omb1;
+    small = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (fabsf(scaled[i]) < kFirstScale * 0x1p-60f) {
+            small |= 1u << i;
+            m[i] = scaled[i];
+        }
+    return m;
+}
+// x, times the reciprocal of kFirstScale where the bit in `small` is set.
+__device__ __forceinline__ f4 unscaled(f4 x, uint32_t small)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (small & 1u << i) != 0 ? x[i] * (1.0f / kFirstScale) : x[i];
+    return x;
+}
+// rate * m / b.  Of a small one by something smaller yet the quotient is formed as it is, or it would leave fp32 at the other end.  One element
+// after another: side by side the divisions take more registers than the other form needs.
+__device__ __forceinline__ f4 updates(f4 m, f4 b, float rate, uint32_t small)
+{
+    f4 u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool scaled = (small & 1u << i) != 0, as_is = b[i] < 0x1p-40f;
+        u[i] = m[i] / (scaled && as_is ? b[i] * kFirstScale : b[i]) * (scaled && !as_is ? rate * (1.0f / kFirstScale) : rate);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    return u;
+}
 
 constexpr int share_rows(int bits) { return bits == 8 ? BAGUA_ADAM8_ROWS : BAGUA_ADAM32_ROWS; }
 
 // K rows of 256 elements of a tile.  G, P, C: types of gradient, parameter and copy (C < 0: none).  e0: the first element
 // in its tensor; left: elements from there on.  FAST (8 bits): with the functions above; false, and nothing done, where a block does not
-// keep to their ranges.
+// keep to their ranges.  kAny: 8 bits without FAST, of any operands.
 template <int G, int P, int C, int BITS, int K, Edge EDGE, bool FAST>
 __device__ __forceinline__ bool adamw_share(const TensorEntry& d, size_t e0, int lane, int left, float factor, const AdamArgs& a)
 {
     static_assert(BITS == 8 || !FAST, "");
+    constexpr bool kAny = BITS == 8 && !FAST;
     constexpr float kFirst = FAST ? kFirstScale : 1.0f, kSecond = FAST ? kSecondScale : 1.0f, kRoot = FAST ? kRootScale : 1.0f;
     typedef typename Elem<P>::one param_t;
     typedef typename Elem<G>::one grad_t;
@@ -296,21 +341,22 @@ __device__ __forceinline__ bool adamw_share(const TensorEntry& d, size_t e0, int
         qp[k] = fetch<EDGE>(pp, e, left);
     }
     f4 m[K], r[K];
-    uint32_t m_most[K], r_most[K], over = 0;
+    uint32_t small[K], m_most[K], r_most[K], over = 0;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int e = k * kRow + lane * 4;
         const f4 g = widened<G>(in_place<EDGE>(qg[k], e, left)) * factor;
         f4 v;
         if constexpr (BITS == 8) {
-            m[k] = widen_codes(__builtin_bit_cast(uint32_t, in_place<EDGE>(qm[k], e, left)), ms[k] * kFirst);
+            const uint32_t codes = __builtin_bit_cast(uint32_t, in_place<EDGE>(qm[k], e, left));
+            m[k] = kAny ? first_moments(codes, ms[k], g, a.beta1, a.omb1, small[k]) : widen_codes(codes, ms[k] * kFirst);
             v = widen_codes(__builtin_bit_cast(uint32_t, in_place<EDGE>(qv[k], e, left)), vs[k]);
             v = v * v;
         } else {
             m[k] = in_place<EDGE>(qm[k], e, left);
             v = in_place<EDGE>(qv[k], e, left);
         }
-        m[k] = m[k] * a.beta1 + g * (a.omb1 * kFirst);
+        if constexpr (!kAny) m[k] = m[k] * a.beta1 + g * (a.omb1 * kFirst);
         v = v * a.beta2 + (g * g) * a.omb2;
         if constexpr (BITS == 32) {
             put<EDGE>(mp, e, left, m[k]);
@@ -327,7 +373,7 @@ __device__ __forceinline__ bool adamw_share(const TensorEntry& d, size_t e0, int
                 clear_absent(m[k], e, left);
                 clear_absent(r[k], e, left);
             }
-            m_most[k] = most_of(FAST ? m[k] : finite(m[k]));
+            m_most[k] = most_of(kAny ? finite(unscaled(m[k], small[k])) : m[k]);
             r_most[k] = most_of_roots(FAST ? r[k] : finite(r[k]));
             if (FAST) over |= static_cast<uint32_t>(m_most[k] > __float_as_uint(kMostFirst)) | static_cast<uint32_t>(r_most[k] > __float_as_uint(kMostRoot));
         }
@@ -345,16 +391,17 @@ __device__ __forceinline__ bool adamw_share(const TensorEntry& d, size_t e0, int
         const int e = k * kRow + lane * 4;
         f4 p = widened<P>(in_place<EDGE>(qp[k], e, left));
         const f4 b = r[k] * root + a.eps;
-        f4 u;
-        if constexpr (FAST) u = f4{quotient_in_range(m[k].x, b.x), quotient_in_range(m[k].y, b.y), quotient_in_range(m[k].z, b.z), quotient_in_range(m[k].w, b.w)};
-        else u = m[k] / b;
-        p = p - (u * rate + p * decay);
+        f4 u;       // times the rate
+        if constexpr (kAny) u = updates(m[k], b, rate, small[k]);
+        else if constexpr (FAST) u = f4{quotient_in_range(m[k].x, b.x), quotient_in_range(m[k].y, b.y), quotient_in_range(m[k].z, b.z), quotient_in_range(m[k].w, b.w)} * rate;
+        else u = m[k] / b * rate;
+        p = p - (u + p * decay);
         if (BITS == 8 || P == BAGUA_BF16) h[k] = mix(random + static_cast<uint32_t>(k) * (kRow / 4 * kGolden));
         if constexpr (P == BAGUA_BF16) {
             const uint32_t w = mix(h[k] + kGolden);
-            constexpr bool kAny = !FAST;      // (there it comes from codes and bf16 parameters alone, whose lower half is empty)
-            put<EDGE>(pp, e, left, h4{random_bf16<kAny>(p.x, turned(w, 0)), random_bf16<kAny>(p.y, turned(w, 8)), random_bf16<kAny>(p.z, turned(w, 16)),
-                                      random_bf16<kAny>(p.w, turned(w, 24))});
+            // (FAST: it comes from codes and bf16 parameters alone, whose lower half is empty)
+            put<EDGE>(pp, e, left, h4{random_bf16<!FAST>(p.x, turned(w, 0)), random_bf16<!FAST>(p.y, turned(w, 8)), random_bf16<!FAST>(p.z, turned(w, 16)),
+                                      random_bf16<!FAST>(p.w, turned(w, 24))});
         } else {
             put<EDGE>(pp, e, left, p);
         }
@@ -371,9 +418,11 @@ __device__ __forceinline__ bool adamw_share(const TensorEntry& d, size_t e0, int
             const f4 y = r[k] * of_block(iv, k);
             const u16x2 lo = two_codes(code_bits(y.x, turned(h[k], 0)), code_bits(y.y, turned(h[k], 8)), r[k].x, r[k].y);
             const u16x2 hi = two_codes(code_bits(y.z, turned(h[k], 16)), code_bits(y.w, turned(h[k], 24)), r[k].z, r[k].w);
-            uint32_t mc = nearest_codes(m[k] * of_block(im, k));
+            f4 inverse = of_block(im, k);
+            if constexpr (kAny) inverse = unscaled(inverse, small[k]);
+            uint32_t mc = nearest_codes(m[k] * inverse);
             uint32_t vc = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x06040200u);
-            if (!FAST) {      // (there roots are finite, and so are first moments but for NaN, which the conversion keeps)
+            if constexpr (kAny) {      // (of FAST roots are finite, and so are first moments but for NaN, which the conversion keeps)
                 mc |= not_finite(m[k]);
                 vc |= not_finite(r[k]);
             }
@@ -386,6 +435,24 @@ __device__ __forceinline__ bool adamw_share(const TensorEntry& d, size_t e0, int
         }
     }
     return true;
+}
+
+// A share with 8-bit states, block by block: rare, operands out of range, or a tensor's last one to three elements.  It reads for itself, keeps nothing in
+// registers up to here (nor through the loop: the lane is hidden from the compiler, which would form all its addresses in front of it), and
+// does with few.
+template <int G, int P, int C>
+__device__ __forceinline__ void adamw_blocks(const TensorEntry& d, size_t e0, int lane, int left, float factor, const AdamArgs& a)
+{
+    asm volatile("" ::: "memory");
+    int at = 0;
+#pragma unroll 1
+    for (; at + kRow <= left; at += kRow) {
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        adamw_share<G, P, C, 8, 1, kFull, false>(d, e0 + at, l, kRow, factor, a);
+    }
+    if (left - at >= 4) adamw_share<G, P, C, 8, 1, kCut, false>(d, e0 + at, lane, left - at, factor, a);
+    else if (left - at > 0) adamw_share<G, P, C, 8, 1, kFew, false>(d, e0 + at, lane, left - at, factor, a);
 }
 
 // The step (in the order and with the roundings of bagua_hip.h): m = beta1 m + (1 - beta1) g, v = beta2 v + (1 - beta2) g^2,
@@ -410,16 +477,16 @@ k_adamw(const TensorEntry* __restrict__ entries, const uint32_t* __restrict__ ti
     }
     const int lane = threadIdx.x;
     const size_t left = d.numel - e0;
-    if (left >= static_cast<size_t>(kElements)) {
-        if constexpr (BITS == 8) {
+    if constexpr (BITS == 8) {
+        if (left >= static_cast<size_t>(kElements)) {
             if (a.in_range && adamw_share<G, P, C, BITS, K, kFull, true>(d, e0, lane, kElements, factor, a)) return;
-            // rare: reads for itself, keeps nothing in registers up to here, and does with few
-            asm volatile("" ::: "memory");
-#pragma unroll 1
-            for (int k = 0; k < K; ++k) adamw_share<G, P, C, BITS, 1, kFull, false>(d, e0 + k * kRow, lane, kRow, factor, a);
+            adamw_blocks<G, P, C>(d, e0, lane, kElements, factor, a);
         } else {
-            adamw_share<G, P, C, BITS, K, kFull, false>(d, e0, lane, kElements, factor, a);
+            if (left >= 4 && a.in_range && adamw_share<G, P, C, BITS, K, kCut, true>(d, e0, lane, static_cast<int>(left), factor, a)) return;
+            adamw_blocks<G, P, C>(d, e0, lane, static_cast<int>(left), factor, a);
         }
+    } else if (left >= static_cast<size_t>(kElements)) {
+        adamw_share<G, P, C, BITS, K, kFull, false>(d, e0, lane, kElements, factor, a);
     } else if (left >= 4) {
         adamw_share<G, P, C, BITS, K, kCut, false>(d, e0, lane, static_cast<int>(left), factor, a);
     } else {
@@ -659,10 +726,10 @@ extern "C" int bagua_adamw_step(const bagua_tensor_plan_t* plan, uint64_t step, 
     const TensorPlanView view = tensor_plan_view(plan);
     const uint32_t groups = static_cast<uint32_t>(plan->tiles * (kTileRows / share_rows(plan->state_bits)));
     const double t = static_cast<double>(step);
-    const float root = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(beta2, t)));
-    const AdamArgs a{clip, static_cast<float>(beta1), static_cast<float>(1.0 - beta1), static_cast<float>(beta2), static_cast<float>(1.0 - beta2),
-                     root, static_cast<float>(eps),
-                     static_cast<float>(lr / (1.0 - std::pow(beta1, t))), static_cast<float>(lr * weight_decay), seed, in_range(root, static_cast<float>(eps))};
+    AdamArgs a{clip, static_cast<float>(beta1), static_cast<float>(1.0 - beta1), static_cast<float>(beta2), static_cast<float>(1.0 - beta2),
+               static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(beta2, t))), static_cast<float>(eps),
+               static_cast<float>(lr / (1.0 - std::pow(beta1, t))), static_cast<float>(lr * weight_decay), seed, false};
+    a.in_range = in_range(a.beta1, a.omb1, a.root, a.eps, a.rate);
     const AdamKernel kernel = plan->state_bits == 32 ? pick_adamw<32>(plan->grad_type, plan->param_type, plan->copy_type)
                                                      : pick_adamw<8>(plan->grad_type, plan->param_type, plan->copy_type);
     launch_kernel(kernel, dim3(groups), dim3(kWave), adamw_lds(plan->tiles, plan->param_type, plan->state_bits), static_cast<hipStream_t>(stream), view.entry,
