@@ -303,6 +303,14 @@ __device__ __forceinline__ bool last_to_arrive(uint32_t* counters, bool* flag)
 __device__ __forceinline__ bool last_of_cluster(uint32_t* counters, bool* flag) { return after_arrival(flag, [&] { return counted_last_of_cluster(counters); }); }
 __device__ __forceinline__ bool last_cluster(uint32_t* counters, bool* flag) { return after_arrival(flag, [&] { return counted_last(counters, clusters()); }); }
 
+// The lesser of `left`, which is the same in the whole wave, and `most`, by a comparison in 32 bits.  Written with 64-bit numbers next to a branch on
+// the same comparison, the compiler does that in the vector unit and then selects by the scalar unit's condition bit, which holds what
+// the arithmetic before it left there.
+__device__ __forceinline__ int at_most(size_t left, int most)
+{
+    return left >> 32 != 0 ? most : static_cast<int>(min(static_cast<uint32_t>(left), static_cast<uint32_t>(most)));
+}
+
 // Index of this wavefront in its workgroup, as a scalar.  The compiler cannot tell that threadIdx.x >> 6 is the same
 // in all 64 lanes and would carry every row offset and tail test derived from it through 64-bit vector arithmetic
 // and exec-mask branches; read from the first lane it lives in scalar registers.

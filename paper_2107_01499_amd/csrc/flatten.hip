@@ -213,7 +213,7 @@ k_decompress_unflatten(const TensorDesc* __restrict__ desc, const uint32_t* __re
         w[i] = 0;
         m0[i] = m1[i] = 0.0f;
         if (e0 >= n) continue;
-        const int remain = static_cast<int>((n - e0 < static_cast<size_t>(kRow)) ? (n - e0) : kRow);
+        const int remain = at_most(n - e0, kRow);
         const size_t c = e0 / chunk;                            // a row never straddles chunks
         if (CODEC == 0) {
             m0[i] = meta[2 * c];

@@ -22,6 +22,16 @@ def test_probe_read_tile_sums(bg):
     assert sums.cpu().tolist() == want
 
 
+@pytest.mark.parametrize("n", [1, 3, 100, 255, 256, 257, 1024 + 60, 4096 + 1024 + 7, 2 * 4096 + 3 * 1024 + 200])
+def test_probe_read_stops_at_the_last_element(bg, n):
+    """The first row of a wave, cut short: nothing behind it is read."""
+    x = torch.full((n + 1024,), float("nan"), device="cuda")
+    x[:n] = torch.arange(n, dtype=torch.float32, device="cuda") % 7 - 3.0
+    sums = torch.full(((n + 4095) // 4096,), float("nan"), device="cuda")
+    bg.bagua_probe_read(x[:n], sums)
+    assert sums.cpu().tolist() == [float(x[t * 4096:min((t + 1) * 4096, n)].double().sum()) for t in range(sums.numel())]
+
+
 def test_probe_streams_copies_rows(bg):
     n = 5 * 256
     a = torch.arange(n, dtype=torch.float32, device="cuda")
