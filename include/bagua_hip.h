@@ -435,7 +435,7 @@ int bagua_bucket_flatten_batched_run(const void* const* plans, const size_t* T, 
  *
  * bagua_grad_norm:  out[0] = N = grad_scale * sqrt(sum of g^2 over all tensors),  out[1] = grad_scale * min(1, max_norm / (N + 1e-6)).
  *   Summed in 64 bits in an order that depends on the sizes alone.  grad_scale: what the gradients have to be multiplied with
- *   (1 / loss scale; 1: nothing).  max_norm: INFINITY for no clipping.  N not finite: out[1] = 0.
+ *   (1 / loss scale; 1: nothing), not below 0.  max_norm: INFINITY for no clipping.  N not finite: out[1] = 0.
  *   out device fp32[2], written.  Calls on one plan must not overlap in time (it holds the partial sums).
  *
  * bagua_adamw_step:  step t >= 1, all operations in fp32 and rounded one by one, host factors formed in 64 bits:

@@ -685,7 +685,7 @@ static bool plan_ok(const bagua_tensor_plan_t* plan)
 
 extern "C" int bagua_grad_norm(const bagua_tensor_plan_t* plan, double grad_scale, double max_norm, float* out, void* stream)
 {
-    if (!plan_ok(plan) || !out || !(std::fabs(grad_scale) < INFINITY) || !(max_norm >= 0.0)) return BAGUA_ERR_INVALID_ARG;
+    if (!plan_ok(plan) || !out || !(grad_scale >= 0.0 && grad_scale < INFINITY) || !(max_norm >= 0.0)) return BAGUA_ERR_INVALID_ARG;
     if (!aligned4(out)) return BAGUA_ERR_ALIGNMENT;
     const unsigned waves = norm_waves(plan->grad_type);
     const dim3 grid(norm_groups(plan->tiles, waves)), block(kWave * waves);

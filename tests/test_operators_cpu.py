@@ -133,3 +133,10 @@ def test_calls_that_are_not_ordinary_are_declined(bg):
         bg.bagua_tensor_plan([x], torch.zeros(10, dtype=torch.uint8))
     with pytest.raises(ValueError, match="expected GPU tensors"):
         bg.bagua_balance_grad([x], None, p, None, [x])
+
+
+@pytest.mark.parametrize("scale", [-1.0, -1e-30, -math.inf])
+def test_norm_refuses_a_scale_below_zero(bg, scale):
+    """The norm would come out negative, and the factor would turn the gradients around."""
+    s = bg.binding._PlanStruct(workspace=W, tiles=1, tensors=1, state_bits=32)
+    assert bg.binding.raw().bagua_grad_norm(ctypes.addressof(s), scale, 1.0, C, None) == INVALID
