@@ -416,7 +416,8 @@ int bagua_bucket_flatten_batched_run(const void* const* plans, const size_t* T, 
  * tensors in one launch (bias correction, decoupled weight decay, gradients and parameters in 32 or 16 bits, moments in 32 or
  * in 8 bits), and in front of it the global norm of their gradients with the factor that clips it.  Both read a table of the
  * tensors that bagua_tensor_plan writes into the caller's workspace; the plan SYNCHRONISES `stream` (a set-up call, as
- * bagua_flatten_plan), the two calls only launch and can be recorded into a HIP graph.
+ * bagua_flatten_plan), the two calls only launch and can be recorded into a HIP graph (whose replays
+ * keep the number, the factors and the seed of the step that was recorded).
  *
  * bagua_tensor_plan: a tensor is contiguous, may be empty, and needs the alignment of its element type only.
  *   numel          host[T], elements; T >= 1

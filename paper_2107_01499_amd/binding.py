@@ -668,9 +668,12 @@ def bagua_grad_norm(plan, out, max_norm=float("inf"), grad_scale=1.0, stream=Non
     _check("bagua_grad_norm", _lib.bagua_grad_norm(plan._at, grad_scale, max_norm, _ptr(out, torch.float32, 8), _stream(stream)))
 
 
-def bagua_adamw_step(plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, clip=None, seed=0, stream=None):
+def bagua_adamw_step(plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, clip=None, seed=None, stream=None):
     """Step number `step` (from 1 on) of all tensors of the plan.  clip: what bagua_grad_norm has left; where the norm is not
-    finite nothing changes.  seed: a number of 32 bits, another one each step, for what is rounded stochastically."""
+    finite nothing changes.  seed: a number of 32 bits, another one each step, for what is rounded stochastically; None: the
+    step's number."""
+    if seed is None:
+        seed = step & 0xFFFFFFFF
     if _native.adamw_step(plan._at, step, lr, beta1, beta2, eps, weight_decay, clip, seed, stream):
         return
     _check("bagua_adamw_step", _lib.bagua_adamw_step(plan._at, step, lr, beta1, beta2, eps, weight_decay, _ptr(clip, torch.float32, 8), seed,
