@@ -21,12 +21,7 @@ constexpr int kTileRows = kTensorTile / kRow;
 // fastest: 1 | 2 | 4 rows, 335 M elements, bf16 gradients and copies, 1524 | 1639 | 1644 us, 25.6 M fp32 113 | 115 | 118.  8 bits: bound by the
 // vector ALU, of which a block's maximum and reciprocals take less where blocks share them (blocks_most): 335 M elements, bf16 parameters
 // 733 | 566 | 569 us, 109 M with fp32 parameters and bf16 copies 300 | 275 | 284, 49 small tensors 16.5 | 4.0 | 5.5.
-#ifndef BAGUA_ADAM8_ROWS
-#define BAGUA_ADAM8_ROWS 2
-#endif
-#ifndef BAGUA_ADAM32_ROWS
-#define BAGUA_ADAM32_ROWS 1
-#endif
+constexpr int share_rows(int bits) { return bits == 8 ? 2 : 1; }
 // Waves of a long launch with 32-bit states that share a CU (see lds_for_residency): more of them only spread what is in flight over more
 // pages.  0 (as many as fit) | 11 | 12 | 13 | 16 waves: 335 M elements, bf16 gradients and copies, 1480 .. 1523 | 1433 | 1429 .. 1437 | 1456 | 1440 ..
 // 1449 us, fp32 1479 | 1473 | 1467 | 1480 | 1497, bf16 parameters 1183 | 1200 | 1154 | 1138 | 1137; 109 M, bf16 gradients and copies, 477 | 466 | 472 |
@@ -37,8 +32,6 @@ inline size_t adamw_lds(size_t tiles, int param_type, int bits)
     if (bits != 32 || tiles < (static_cast<size_t>(1) << 24) / kTensorTile) return 0;
     return lds_for_residency(param_type == BAGUA_F32 ? 12 : 16);
 }
-static_assert((BAGUA_ADAM8_ROWS == 1 || BAGUA_ADAM8_ROWS == 2 || BAGUA_ADAM8_ROWS == 4) && (BAGUA_ADAM32_ROWS == 1 || BAGUA_ADAM32_ROWS == 2 || BAGUA_ADAM32_ROWS == 4),
-              "rows that divide a tile");
 // The norm: one workgroup on a CU, with the waves that keep 32 KB of loads in flight there.  More waves read no faster, and each group more
 // is one more that has to be counted at the end, 13 ns apiece: 335 M fp32 elements, 2048 groups of 4 waves 215 us, 512 of 8 197, 512 of
 // 4 191, 256 of 8 192; bf16, 256 groups of 8 142, of 16 100; 25.6 M bf16, 2048 groups of 4 32.3, 256 of 16 14.3.
@@ -77,9 +70,9 @@ inline TensorPlanView tensor_plan_view(const bagua_tensor_plan_t* p)
 }
 
 // ---------------------------------------------------------------- four elements of a row
-// Four elements of a lane, from element e on, as they are in memory.  FULL: all are there.  Otherwise a lane that reaches over the end makes
+// Four elements of a lane, from element e on, as they are in memory.  kFull: all are there.  kCut: a lane that reaches over the end makes
 // the last access that does not, and moves what it gets into place: no load stands behind a test, or each would be waited for before
-// the next.  What lanes beyond the end hold means nothing.  `left`: valid elements; ANY: fewer than four, one by one.
+// the next.  What lanes beyond the end hold means nothing.  `left`: valid elements; kFew: fewer than four, one by one.
 template <typename T>
 struct Four {
     typedef T v __attribute__((ext_vector_type(4)));
@@ -221,15 +214,14 @@ __device__ __forceinline__ uint32_t most_of_roots(f4 x)
 struct OpMaxU { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); } };
 
 // The largest of each of K blocks of 256 values, of which every lane holds one: that of block k in the 64 / K lanes from k * 64 / K on.
-// Blocks are put side by side on the way (two in the halves of a register, four in its rows of 16), so that four cost what one does.
+// Two blocks are put side by side, in the halves of a register, so that they cost what one does.
 template <int K>
 __device__ __forceinline__ uint32_t blocks_most(const uint32_t (&x)[K])
 {
-    static_assert(K == 1 || K == 2 || K == 4, "");
+    static_assert(K == 1 || K == 2, "");
     const OpMaxU op;
     auto halves = [&](uint32_t a, uint32_t b) { const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false); return op(r[0], r[1]); };
     auto rows = [&](uint32_t a, uint32_t b) { const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false); return op(r[0], r[1]); };
-    if constexpr (K == 4) return row16_reduce(rows(halves(x[0], x[2]), halves(x[1], x[3])), op);
     const uint32_t v = halves(x[0], x[K - 1]);
     return row16_reduce(rows(v, v), op);
 }
@@ -301,8 +293,6 @@ __device__ __forceinline__ f4 updates(f4 m, f4 b, float rate, uint32_t small)
     }
     return u;
 }
-
-constexpr int share_rows(int bits) { return bits == 8 ? BAGUA_ADAM8_ROWS : BAGUA_ADAM32_ROWS; }
 
 // K rows of 256 elements of a tile.  G, P, C: types of gradient, parameter and copy (C < 0: none).  e0: the first element
 // in its tensor; left: elements from there on.  FAST (8 bits): with the functions above; false, and nothing done, where a block does not
