@@ -282,7 +282,8 @@ __host__ __device__ constexpr int sum_rows(int waves, int experts)
 // and keeps its sums in registers, a group joins its waves' in LDS, and the group that ends last adds up the groups' in a fixed order and forms
 // the loss, so that one launch reads each logit and choice once and no sum depends on which group came first.  Bound by what comes before and
 // after the loop, not by memory: 8 workers' 32768 rows of 64, bf16, 20.0 us, where the 41 MB are read in 6: the launch, the wait for the first rows
-// and the meeting of 256 groups are 9 to 12.  Long ones by the vector ALU (524288 x 256, bf16, 64.7 us, 4.4 TB/s).
+// and the meeting of 256 groups are 9 to 12.  Long ones (524288 x 256, bf16, 65 to 67 us, 4.5 TB/s) use half of the vector ALU's slots and two thirds of
+// the memory's rate, with three waves on a SIMD: what bounds them is not shown.
 // Dynamic LDS: float sums[sum_rows][experts], then uint32 counters[(experts + 1) << lg]: 2^lg copies of each, one of
 // which a lane adds to, so that popular experts are not waited for.  Workspace: counters (last_to_arrive), then every workgroup's sums and counts.
 template <int TYPE, int VEC, int L, int NV, int UNROLL, int WAVES>
@@ -619,8 +620,8 @@ template <int VEC_, int L_, int NV_, int UNROLL_, int WAVES_ = 16>
 struct Layout {
     static constexpr int VEC = VEC_, L = L_, NV = NV_, UNROLL = UNROLL_, WAVES = WAVES_, GRAD_UNROLL = NV_ == 1 ? 2 : 1;   // WAVES: of a workgroup of the forward pass
 };
-// The forward pass of 16-bit rows beyond 128 elements is bound by the vector ALU: twice the elements in half the lanes take half the
-// exchanges (524288 x 256, bf16, 78 -> 67 us, 250 K x 512, fp16, 82 -> 72; 8 x 32768 x 64 loses, 21.8 -> 22.0).
+// The forward pass of 16-bit rows beyond 128 elements: twice the elements in half the lanes take half the exchanges (524288 x 256, bf16, 78 -> 67 us,
+// 250 K x 512, fp16, 82 -> 72; 8 x 32768 x 64 loses, 21.8 -> 22.0).
 template <int V, bool FORWARD, typename F>
 inline void with_vectors(int experts, const F& f)
 {
@@ -742,9 +743,9 @@ extern "C" int bagua_balance_stats(int dtype, const void* const* logits, size_t 
             return launch_status();
         };
         // Rows of a wave at a time, 64 / L, in short launches one after another in different waves rather than together in one.  Together | apart:
-        // 100 tokens of 8 experts 6.7 | 5.4 us, 1000 8.2 | 6.6, 32768 15.0 | 11.2; 1000 of 64 11.2 | 10.1, 4096 12.3 | 10.2, 2 x 8192 12.6 | 15.8; 1000 of 256
-        // 11.8 | 10.4, 4096 12.9 | 15.1.  Not where that would make more than one group of one: 100 of 256 7.7 | 9.9.
-        // (All of them before the groups' sums were put together in fewer instructions, which takes 0.4 to 1.8 us from both sides.)
+        // 100 tokens of 8 experts 5.9 | 4.4 us, 1000 6.5 | 5.7, 32768 13.1 | 10.1; 1000 of 64 11.1 | 9.3, 4096 11.4 | 10.0; 1000 of 256 11.5 | 10.5.  Not where that would
+        // make more than one group of one: 4096 of 8 8.6 | 9.8, 100 of 256 7.2 | 9.7.  The line of 512 units: 400 | 512 | 700 units gain (lose) 1.4 | 1.4 | 0.9 us with
+        // 64 experts, 1.4 | 1.4 | (0.1) with 128, (0.4) | (0.4) | 0.6 with 256, 0.8 | 1.0 | (3.5) with 512; 8 experts gain 2.5 beyond it as well, up to 2048.
         size_t units = 0, tiles = 0;
         for (int w = 0; w < k; ++w) {
             units += (tokens[w] + kWave / Lay::L - 1) / (kWave / Lay::L);

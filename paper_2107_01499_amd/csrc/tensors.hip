@@ -19,8 +19,9 @@ constexpr int kTensorTile = 1024;
 constexpr int kTileRows = kTensorTile / kRow;
 // Rows of 256 elements that a wave (the whole workgroup) takes of a tile.  32 bits: the step is bound by memory, and one row streams
 // fastest: 1 | 2 | 4 rows, 335 M elements, bf16 gradients and copies, 1524 | 1639 | 1644 us, 25.6 M fp32 113 | 115 | 118.  8 bits: bound by the
-// vector ALU, of which a block's maximum and reciprocals take less where blocks share them (blocks_most): 335 M elements, bf16 parameters
-// 733 | 566 | 569 us, 109 M with fp32 parameters and bf16 copies 300 | 275 | 284, 49 small tensors 16.5 | 4.0 | 5.5.
+// vector ALU, of which a block's maximum and reciprocals take less where blocks share them (blocks_most): 1 | 2 rows, 335 M elements, bf16
+// parameters 701 | 565 us, 5 M 26.6 | 12.2, 109 M with fp32 parameters and bf16 copies 298 | 278, 49 small tensors 16.8 | 3.7 (four rows
+// gained nothing on two in long launches and lost in small ones, 4.0 | 5.5).
 constexpr int share_rows(int bits) { return bits == 8 ? 2 : 1; }
 // Waves of a long launch with 32-bit states that share a CU (see lds_for_residency): more of them only spread what is in flight over more
 // pages.  0 (as many as fit) | 11 | 12 | 13 | 16 waves: 335 M elements, bf16 gradients and copies, 1480 .. 1523 | 1433 | 1429 .. 1437 | 1456 | 1440 ..
@@ -449,8 +450,9 @@ __device__ __forceinline__ void adamw_blocks(const TensorEntry& d, size_t e0, in
 // p = (1 - lr decay) p - rate m / (root sqrt(v) + eps), every element by itself, read and written once; with 8 bits a wave holds whole
 // blocks, so that the new scale of a block is an exchange among its lanes and the states are
 // not read again.  A workgroup is one wave, which ends as soon as its own rows are written.  32-bit states: bound by memory, 335 M elements with bf16
-// gradients and copies 1436 us, 6.5 TB/s, 25.6 M fp32 109 us, 6.6 TB/s.  8-bit states: bound by the vector ALU, bf16 parameters and gradients,
-// 335 M elements, 574 to 583 us, 5.8 TB/s; with fp32 parameters and bf16 copies, 109 M, 278 us, 6.3 TB/s.
+// gradients and copies 1436 us, 6.5 TB/s, 25.6 M fp32 109 us, 6.5 TB/s.  8-bit states with fp32 parameters and bf16 copies: near the memory's rate and the
+// vector ALU's, 109 M, 278 us, 6.3 TB/s.  With bf16 parameters and gradients: bound by the vector ALU, 335 M, 563 to 600 us, 5.6 to 6.0 TB/s, with
+// the clock that this load leaves (1.9 of 2.4 GHz; for some calls after it begins 1.3, and up to 880 us).
 template <int G, int P, int C, int BITS>
 __global__ void __launch_bounds__(kWave)
 k_adamw(const TensorEntry* __restrict__ entries, const uint32_t* __restrict__ tile_tensor, AdamArgs a)
