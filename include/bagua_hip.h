@@ -511,6 +511,48 @@ int bagua_balance_grad(int dtype, const void* const* logits, size_t ld, const si
                        void* stream);
 
 /*
+ * Routing of tokens to experts, which gives the balance loss its choices and a mixture its weights, for k data-parallel workers' tokens in one
+ * launch.  For a token with logits x over E experts:
+ *   s = softmax(x) (BAGUA_SCORE_SOFTMAX) or, each for itself, 1 / (1 + exp(-x)) (BAGUA_SCORE_SIGMOID);   c = s + bias
+ *   groups > 1: experts [g*E/groups, (g+1)*E/groups) are group g, which is as good as the sum of its `group_best` (1 or 2) largest c; experts
+ *     outside the top_groups best groups are not chosen.
+ *   The top_k experts of largest c, the largest first, are the choices; equal c and equally good groups: the lowest index.
+ *   weight_j = scale * s_j, where renormalised scale * s_j / (sum of the chosen s)      (the bias chooses, it does not weigh).
+ * What is chosen is what s, c and their sums give in 64 bits, where they can be told apart there (without bias and with group_best = 1, c rises with x
+ * and x is compared itself); weights are formed in fp32.
+ *
+ * bagua_route:
+ *   dtype     BAGUA_F32, BAGUA_BF16 or BAGUA_F16: of the logits
+ *   logits    host[k] of device [tokens[i]][experts], rows `ld` >= experts elements apart; the alignment of an element suffices
+ *   tokens    host[k], any may be 0 (its pointers may then be NULL)
+ *   mask      host[k] of device u8[tokens[i]], 0 = padding: its logits do not matter, its ids are -1, its weights 0; NULL: none
+ *   bias      device fp32[experts], NULL: none
+ *   ids       host[k] of device [tokens[i]][top_k], int32 (id_bytes 4) or int64 (8), rows `ids_ld` >= top_k apart, written
+ *   weights   host[k] of device fp32[tokens[i]][top_k], rows `weights_ld` >= top_k apart, written
+ *   limits    1 <= k <= BAGUA_MAX_WORKERS, experts <= BAGUA_MAX_EXPERTS, a multiple of groups <= BAGUA_MAX_EXPERT_GROUPS, top_k <= BAGUA_MAX_CHOICES and
+ *             <= top_groups * experts / groups, group_best <= experts / groups
+ * A NaN ranks above every number, among logits, scores and groups.  A row of softmax with a NaN or +infinity has weights NaN, one that is -infinity
+ * throughout has scores and weights 0; the ids of a token are distinct and in range whatever its logits are.
+ *
+ * bagua_route_grad: gradient of the logits from dweights, that of the weights.  The choices have no gradient.
+ *   ids       as bagua_route left them; an id outside [0, experts) is none (so padding's gradient is 0); one that comes twice counts twice
+ *   weights   as bagua_route left them: read where softmax scores were renormalised (which needs scale != 0), NULL elsewhere
+ *   logits    read elsewhere; NULL where softmax scores were renormalised
+ *   dweights  host[k] of device fp32[tokens[i]][top_k], rows dweights_ld apart; those of ids that are none are not used
+ *   dlogits   host[k] of device [tokens[i]][experts] of dtype, rows ld_out apart, written: every element.  A row without an id has gradient 0.
+ * With softmax renormalised the weights stand for the chosen softmax alone: they must be all of a row's, and add up to scale.
+ */
+#define BAGUA_MAX_EXPERT_GROUPS 32
+#define BAGUA_MAX_CHOICES 64
+enum { BAGUA_SCORE_SOFTMAX = 0, BAGUA_SCORE_SIGMOID = 1 };
+int bagua_route(int dtype, const void* const* logits, size_t ld, const size_t* tokens, int k, int experts, const uint8_t* const* mask,
+                const float* bias, int score, int groups, int top_groups, int group_best, int top_k, int renormalise, double scale,
+                void* const* ids, int id_bytes, size_t ids_ld, float* const* weights, size_t weights_ld, void* stream);
+int bagua_route_grad(int dtype, const void* const* logits, size_t ld, const size_t* tokens, int k, int experts, const void* const* ids, int id_bytes,
+                     size_t ids_ld, int top_k, const float* const* weights, size_t weights_ld, const float* const* dweights, size_t dweights_ld,
+                     int score, int renormalise, double scale, void* const* dlogits, size_t ld_out, void* stream);
+
+/*
  * Measurement utilities used by the benchmark to state what the memory system of the GPU at hand delivers for
  * plain access patterns (the ceilings printed next to the roofline fractions); no arithmetic of the method.
  * bagua_probe_read: a read-only reduction, tile_sums[t] = sum of x[4096 t .. 4096 t + 4095] (device fp32[ceil(n/4096)]).

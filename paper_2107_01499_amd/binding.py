@@ -26,10 +26,14 @@ LIB_PATH = os.path.join(_HERE, "lib", "libbagua_hip.so")
 
 CODEC_MINMAX_U8 = 0
 CODEC_SIGN1 = 1
+SCORE_SOFTMAX = 0
+SCORE_SIGMOID = 1
 AVG_FP = 0
 AVG_LP_MINMAX_U8 = 1
 MAX_WORKERS = 32
 MAX_EXPERTS = 2048
+MAX_EXPERT_GROUPS = 32
+MAX_CHOICES = 64
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # BAGUA_F32, BAGUA_BF16, BAGUA_F16
 
 EXPORTS = (
@@ -45,6 +49,7 @@ EXPORTS = (
     "bagua_probe_streams", "bagua_flatten_sign_compress_ef", "bagua_decompress_unflatten", "bagua_reduce_compress_sign_ef", "bagua_decompress_sgd_step_topk", "bagua_decompress_adam_step_topk",
     "bagua_tensor_plan_bytes", "bagua_tensor_plan", "bagua_grad_norm", "bagua_adamw_step",
     "bagua_balance_workspace_bytes", "bagua_balance_stats", "bagua_balance_loss", "bagua_balance_grad",
+    "bagua_route", "bagua_route_grad",
 )
 
 
@@ -111,6 +116,8 @@ def _load():
     lib.bagua_balance_stats.argtypes = [i32, vp, sz, vp, i32, i32, vp, i32, sz, i32, vp, vp, vp, cd, vp, vp, vp, sz, vp]
     lib.bagua_balance_loss.argtypes = [vp, vp, i32, i32, cd, vp, vp, vp]
     lib.bagua_balance_grad.argtypes = [i32, vp, sz, vp, i32, i32, vp, vp, vp, vp, sz, vp]
+    lib.bagua_route.argtypes = [i32, vp, sz, vp, i32, i32, vp, vp, i32, i32, i32, i32, i32, i32, cd, vp, i32, sz, vp, sz, vp]
+    lib.bagua_route_grad.argtypes = [i32, vp, sz, vp, i32, i32, vp, i32, sz, i32, vp, sz, vp, sz, i32, i32, cd, vp, sz, vp]
     for name in EXPORTS[2:]:
         getattr(lib, name).restype = i32
     for name in ("bagua_batch_workspace_bytes", "bagua_tensor_plan_bytes", "bagua_balance_workspace_bytes"):
@@ -759,6 +766,55 @@ def bagua_balance_grad(logits, mask, weight, upstream, dlogits, stream=None):
     _check("bagua_balance_grad", _lib.bagua_balance_grad(
         _TYPES[dtype], la, ld, _sizes(rows), k, experts, _mask_array(mask, rows), _ptr(weight, torch.float32, 4 * experts),
         _ptr(upstream, torch.float32, 4), oa, ld_out, _stream(stream)))
+
+
+# ---------------------------------------------------------------------------------------------- routing to experts
+def bagua_route(logits, mask, ids, weights, bias=None, score=SCORE_SOFTMAX, groups=1, top_groups=1, group_best=1, renormalise=True, scale=1.0, stream=None):
+    """The top_k experts of every token and their weights.  logits: k tensors [tokens, experts]; mask: k tensors [tokens] (0 = padding) or None; ids: k
+    tensors [tokens, top_k], int32 or int64, and weights: k tensors [tokens, top_k], fp32, written; bias: fp32[experts], added to the scores that
+    experts are chosen by, or None.  groups > 1: experts are chosen from the top_groups groups whose group_best best experts have the largest sum."""
+    if _native.route(logits, mask, ids, weights, bias, score, groups, top_groups, group_best, renormalise, scale, stream):
+        return
+    k = len(logits)
+    _same_len(k, mask=mask, ids=ids, weights=weights)
+    if k == 0 or logits[0].dim() != 2 or ids[0].dim() != 2:
+        raise ValueError("expected 2-D tensors of at least one worker")
+    rows = [x.shape[0] for x in logits]
+    experts, top = logits[0].shape[1], ids[0].shape[1]
+    dtype, ld, la = _matrices(logits, tuple(_TYPES), experts)
+    it, ids_ld, ia = _matrices(ids, (torch.int32, torch.int64), top, rows)
+    _, weights_ld, wa = _matrices(weights, (torch.float32,), top, rows)
+    _check("bagua_route", _lib.bagua_route(
+        _TYPES[dtype], la, ld, _sizes(rows), k, experts, _mask_array(mask, rows), _ptr(bias, torch.float32, 4 * experts), score, groups, top_groups, group_best,
+        top, int(bool(renormalise)), scale, ia, 4 if it is torch.int32 else 8, ids_ld, wa, weights_ld, _stream(stream)))
+
+
+def bagua_route_grad(logits, ids, weights, dweights, dlogits, score=SCORE_SOFTMAX, renormalise=True, scale=1.0, stream=None):
+    """Gradient of the logits from that of the weights.  ids and weights as bagua_route left them (an id outside the experts is none).  Of logits and weights
+    one is read: the weights where softmax scores were renormalised, the logits elsewhere; the other may be None."""
+    if _native.route_grad(logits, ids, weights, dweights, dlogits, score, renormalise, scale, stream):
+        return
+    k = len(dlogits)
+    of_weights = score == SCORE_SOFTMAX and bool(renormalise)
+    if (weights if of_weights else logits) is None:
+        raise ValueError("the gradient is formed of the %s" % ("weights" if of_weights else "logits"))
+    _same_len(k, logits=logits, ids=ids, weights=weights, dweights=dweights)
+    if k == 0 or dlogits[0].dim() != 2 or ids[0].dim() != 2:
+        raise ValueError("expected 2-D tensors of at least one worker")
+    rows = [x.shape[0] for x in dlogits]
+    experts, top = dlogits[0].shape[1], ids[0].shape[1]
+    dtype, ld_out, oa = _matrices(dlogits, tuple(_TYPES), experts)
+    it, ids_ld, ia = _matrices(ids, (torch.int32, torch.int64), top, rows)
+    _, up_ld, ua = _matrices(dweights, (torch.float32,), top, rows)
+    ld = weights_ld = 0
+    la = wa = None
+    if of_weights:
+        _, weights_ld, wa = _matrices(weights, (torch.float32,), top, rows)
+    else:
+        _, ld, la = _matrices(logits, (dtype,), experts, rows)
+    _check("bagua_route_grad", _lib.bagua_route_grad(
+        _TYPES[dtype], la, ld, _sizes(rows), k, experts, ia, 4 if it is torch.int32 else 8, ids_ld, top, wa, weights_ld, ua, up_ld, score, int(bool(renormalise)),
+        scale, oa, ld_out, _stream(stream)))
 
 
 # ---------------------------------------------------------------------------------------------- probes

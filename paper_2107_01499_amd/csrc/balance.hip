@@ -5,10 +5,8 @@
 // more (in bounds, whatever the length): these are left out of the sums by a factor of 0, and where they are stored both lanes
 // store the same bits.
 #include <cmath>
-#include <type_traits>
 
-#include "batch.hpp"
-#include "elements.hpp"
+#include "rows.hpp"
 
 #pragma clang fp contract(off)
 
@@ -27,163 +25,6 @@ struct Workers {
     uint32_t first_tile[BAGUA_MAX_WORKERS + 1];   // a tile: the rows, of one worker, that a wave has in flight together
     uint32_t k;
 };
-
-template <typename T, int N>
-struct Raw;   // N elements as they are in memory, with the alignment of one
-template <typename T>
-struct Raw<T, 1> {
-    typedef T v __attribute__((ext_vector_type(1), aligned(sizeof(T))));
-};
-template <typename T>
-struct Raw<T, 4> {
-    typedef T v __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-};
-template <typename T>
-struct Raw<T, 8> {
-    typedef T v __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-};
-
-// op over the L lanes of a row, in every one of them.
-template <int L, typename T, typename F>
-__device__ __forceinline__ T lanes_reduce(T v, const F& op)
-{
-    if (L >= 2) v = op(v, dpp<kXor1>(v));
-    if (L >= 4) v = op(v, dpp<kXor2>(v));
-    if (L >= 8) v = op(v, dpp<kHalfMirror>(v));
-    if (L >= 16) v = op(v, dpp<kMirror>(v));
-    if (L >= 32) {
-        const uint32_t b = __builtin_bit_cast(uint32_t, v);
-        const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
-        v = op(__builtin_bit_cast(T, static_cast<uint32_t>(r[0])), __builtin_bit_cast(T, static_cast<uint32_t>(r[1])));
-    }
-    if (L >= 64) {
-        const uint32_t b = __builtin_bit_cast(uint32_t, v);
-        const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-        v = op(__builtin_bit_cast(T, static_cast<uint32_t>(r[0])), __builtin_bit_cast(T, static_cast<uint32_t>(r[1])));
-    }
-    return v;
-}
-
-// The largest over the L lanes of a row.  Numbers are ordered as integers once those below zero have their other bits turned, and the
-// integer maximum takes another lane's value in the same instruction, where that of numbers takes three to make a NaN quiet.
-struct OpMaxI { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return static_cast<uint32_t>(max(static_cast<int32_t>(a), static_cast<int32_t>(b))); } };
-__device__ __forceinline__ uint32_t in_order(uint32_t bits) { return bits ^ (static_cast<uint32_t>(static_cast<int32_t>(bits) >> 31) & 0x7fffffffu); }
-template <int L>
-__device__ __forceinline__ float lanes_most(float x)
-{
-    if (L == 1) return x;
-    return __uint_as_float(in_order(lanes_reduce<L>(in_order(__float_as_uint(x)), OpMaxI())));
-}
-
-constexpr int kRor1 = 0x121, kRor2 = 0x122, kRor4 = 0x124, kRor8 = 0x128;   // lane l reads l + 1, ... of its row of 16, around its end
-// The sum over the lanes that hold the same elements of different rows: l, l + L, l + 2 L, ...
-template <int L>
-__device__ __forceinline__ float rows_sum(float v)
-{
-    if (L <= 8) v = v + dpp<kRor8>(v);
-    if (L <= 4) v = v + dpp<kRor4>(v);
-    if (L <= 2) v = v + dpp<kRor2>(v);
-    if (L <= 1) v = v + dpp<kRor1>(v);
-    if (L <= 16) {
-        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    }
-    if (L <= 32) {
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    }
-    return v;
-}
-
-// What a lane holds of a row.
-template <int TYPE, int VEC, int L, int NV>
-struct Row {
-    typedef typename Elem<TYPE>::one one;
-    typedef typename Raw<one, VEC>::v raw;
-    static constexpr int kRows = kWave / L;       // rows of a unit
-    raw q[NV];
-
-    // Elements of vector j of the lane: from at(j) on; slot(j): what it would be if the row filled the lanes.
-    static __device__ __forceinline__ int slot(int j) { return (j * L + static_cast<int>(threadIdx.x % L)) * VEC; }
-    static __device__ __forceinline__ int at(int j, int experts) { return min(slot(j), experts - VEC); }
-
-    __device__ __forceinline__ void load(const one* row, int experts, bool there)
-    {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            q[j] = raw(0);
-            if (there) q[j] = __builtin_nontemporal_load(reinterpret_cast<const raw*>(row + at(j, experts)));
-        }
-    }
-    __device__ __forceinline__ void keep_if(bool there)
-    {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) q[j] = there ? q[j] : raw(0);
-    }
-    // The lane's elements as fp32, and the row's largest.
-    __device__ __forceinline__ float largest(float (&x)[NV][VEC]) const
-    {
-        float most = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                x[j][i] = Elem<TYPE>::widen(q[j][i]);
-                most = fmaxf(most, x[j][i]);
-            }
-        return lanes_most<L>(most);
-    }
-    // x = exp(x - most).  Not HUGE: log2(e) times both, and then the difference, in one fused operation; the rounding of the product with `most`
-    // is the same factor on all of a row, which the sum takes out again as long as it is near 1.  HUGE: the difference first, which costs an
-    // operation more, and is right whatever the magnitude.
-    template <bool HUGE>
-    static __device__ __forceinline__ void exponentials(float (&x)[NV][VEC], float most)
-    {
-        constexpr float kLog2e = 1.44269504088896340736f;
-        const float top = most == -INFINITY ? 0.0f : most, shift = -top * kLog2e;   // (nothing but -infinity: all become 0)
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                x[j][i] = __builtin_amdgcn_exp2f(HUGE ? (x[j][i] - top) * kLog2e : __builtin_fmaf(x[j][i], kLog2e, shift));
-    }
-    static __device__ __forceinline__ float reciprocal_sum(const float (&own)[NV][VEC], const float (&e)[NV][VEC])
-    {
-        float sum = 0.0f;
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) sum = __builtin_fmaf(e[j][i], own[j][i], sum);
-        sum = lanes_reduce<L>(sum, OpAddF());
-        const float r = __builtin_amdgcn_rcpf(sum);
-        return sum == 0.0f ? 0.0f : __builtin_fmaf(__builtin_fmaf(-sum, r, 1.0f), r, r);
-    }
-    static __device__ __forceinline__ void owned(int experts, float (&own)[NV][VEC])
-    {
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) own[j][i] = j < NV / 2 || at(j, experts) + i >= slot(j) ? 1.0f : 0.0f;   // (rows are longer than half the lanes)
-    }
-};
-
-// exp(x - largest) of a wave's U times rows, without a branch between them that would keep their exchanges from filling each other's gaps.
-template <typename R, int U, int NV, int VEC>
-__device__ __forceinline__ void exponentials_of(float (&e)[U][NV][VEC], const float (&most)[U], bool may_be_huge)
-{
-    bool huge = false;
-#pragma unroll
-    for (int u = 0; u < U; ++u) huge |= fabsf(most[u]) > 0x1p20f;
-    // up to 2^20 the shift is off by 2^-4 at most, half a unit of its last place: 4 % on all of a row.  Beyond 2^31 it would be off by more than 128,
-    // and leave nothing but zeros or infinities of the row
-    if (may_be_huge && __any(huge)) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) R::template exponentials<true>(e[u], most[u]);
-    } else {
-#pragma unroll
-        for (int u = 0; u < U; ++u) R::template exponentials<false>(e[u], most[u]);
-    }
-}
 
 // The workers' table with worker i in lane i: which worker has a tile is one comparison and a count of bits, and what belongs to it
 // is read from its lane.  (From the arguments that is a chain of scalar loads, a new one for every worker that is passed over.)
@@ -615,41 +456,6 @@ k_balance_grad(Workers ws, size_t ld, size_t ld_out, uint32_t tiles, int experts
     }
 }
 
-// Calls f with the layout of a row of `experts` elements: VEC, L, NV, and units that a wave has in flight together.
-template <int VEC_, int L_, int NV_, int UNROLL_, int WAVES_ = 16>
-struct Layout {
-    static constexpr int VEC = VEC_, L = L_, NV = NV_, UNROLL = UNROLL_, WAVES = WAVES_, GRAD_UNROLL = NV_ == 1 ? 2 : 1;   // WAVES: of a workgroup of the forward pass
-};
-// The forward pass of 16-bit rows beyond 128 elements: twice the elements in half the lanes take half the exchanges (524288 x 256, bf16, 78 -> 67 us,
-// 250 K x 512, fp16, 82 -> 72; 8 x 32768 x 64 loses, 21.8 -> 22.0).
-template <int V, bool FORWARD, typename F>
-inline void with_vectors(int experts, const F& f)
-{
-    if (experts < V) {
-        if (experts <= 1) f(Layout<1, 1, 1, 4>());
-        else if (experts <= 2) f(Layout<1, 2, 1, 4>());
-        else if (experts <= 4) f(Layout<1, 4, 1, 4>());
-        else f(Layout<1, 8, 1, 4>());
-    } else if (experts <= V) f(Layout<V, 1, 1, 4>());
-    else if (experts <= 2 * V) f(Layout<V, 2, 1, 4>());
-    else if (experts <= 4 * V) f(Layout<V, 4, 1, 4>());
-    else if (experts <= 8 * V) f(Layout<V, 8, 1, 4>());
-    else if (experts <= 16 * V) f(Layout<V, 16, 1, 4>());
-    else if (experts <= 32 * V) f(std::conditional_t<FORWARD && V == 8, Layout<V, 16, 2, 2>, Layout<V, 32, 1, 4>>());
-    else if (experts <= 64 * V) f(std::conditional_t<FORWARD && V == 8, Layout<V, 32, 2, 2>, Layout<V, 64, 1, 4>>());
-    else if (experts <= 128 * V) f(Layout<V, 64, 2, 2>());
-    else if (experts <= 256 * V) f(Layout<V, 64, 4, 1, V == 8 ? 8 : 16>());
-    else if constexpr (V == 4) f(Layout<V, 64, 8, 1, 8>());
-}
-// 16 bytes of a row in a lane: a wider vector of fp32 is two accesses that each leave out every other 16 bytes, and a store of half a
-// line costs a whole one (gradient of 1 M rows of 64, fp32: eight elements 101.8 us, four 82).
-template <bool FORWARD, typename F>
-inline void with_layout(int dtype, int experts, const F& f)
-{
-    if (dtype == BAGUA_F32) with_vectors<4, FORWARD>(experts, [&](auto layout) { f(layout, std::integral_constant<int, BAGUA_F32>()); });
-    else if (dtype == BAGUA_BF16) with_vectors<8, FORWARD>(experts, [&](auto layout) { f(layout, std::integral_constant<int, BAGUA_BF16>()); });
-    else with_vectors<8, FORWARD>(experts, [&](auto layout) { f(layout, std::integral_constant<int, BAGUA_F16>()); });
-}
 // Arguments that both passes have, and the workers' table.
 inline int balance_check(int dtype, const void* const* logits, size_t ld, const size_t* tokens, int k, int experts, Workers& ws)
 {

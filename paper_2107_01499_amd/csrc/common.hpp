@@ -588,7 +588,7 @@ struct RangeCheck {
         uintptr_t lo, hi;  // [lo, hi)
         bool written;
     };
-    Item item[6 * BAGUA_MAX_WORKERS + 12];
+    Item item[8 * BAGUA_MAX_WORKERS + 12];
     int count = 0;
     void add(const void* p, size_t bytes, bool written)
     {

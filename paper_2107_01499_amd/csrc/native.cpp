@@ -29,8 +29,8 @@ namespace {
     X(bagua_decompress_adam_step) X(bagua_compress_topk_ef) X(bagua_decompress_reduce_recompress_topk) X(bagua_decompress_topk) \
     X(bagua_decompress_sgd_step_topk) X(bagua_decompress_adam_step_topk)
 
-// Those of the calls on a plan and of the balance loss; their functions here go by the second part of the name.
-#define BAGUA_NATIVE_STEPS(X) X(grad_norm) X(adamw_step) X(balance_stats) X(balance_grad)
+// Those of the calls on a plan and of rows of logits; their functions here go by the second part of the name.
+#define BAGUA_NATIVE_STEPS(X) X(grad_norm) X(adamw_step) X(balance_stats) X(balance_grad) X(route) X(route_grad)
 
 // The entry points, as binding.py's library has them: the address of each, so that both paths call one and the same library.
 #define X(name) decltype(&name) f_##name = nullptr;
@@ -598,6 +598,54 @@ PY(balance_grad, 6)   // logits, mask, weight, upstream, dlogits, stream
     return [=](void* s) {
         return f_bagua_balance_grad(type_of(x.type), p.x, x.stride(), p.rows, x.count, static_cast<int>(e), masked ? p.m : nullptr, weight, up,
                                     const_cast<void* const*>(p.o), o.stride(), s);
+    };
+PY_END
+
+PY(route, 12)   // logits, mask, ids, weights, bias, score, groups, top_groups, group_best, renormalise, scale, stream
+    struct {
+        const void *x[BAGUA_MAX_WORKERS], *i[BAGUA_MAX_WORKERS], *w[BAGUA_MAX_WORKERS];
+        const uint8_t* m[BAGUA_MAX_WORKERS];
+        size_t rows[BAGUA_MAX_WORKERS];
+    } p;
+    const auto x = v.matrices(0, p.x, p.rows, false, -1, -1);
+    const bool masked = v.masks(1, p.m, p.rows, x.count) != nullptr;
+    const auto i = v.matrices(2, p.i, p.rows, true, -1, x.count);
+    const auto w = v.matrices(3, p.w, p.rows, true, i.columns, x.count);
+    v.ok = v.ok && type_of(x.type) >= 0 && (i.type == at::kInt || i.type == at::kLong) && w.type == at::kFloat && x.columns <= BAGUA_MAX_EXPERTS && i.columns <= x.columns;
+    const size_t e = v.ok ? static_cast<size_t>(x.columns) : 0;
+    const float* bias = v.f32(4, e);
+    const int score = v.small(5), groups = v.small(6), top_groups = v.small(7), best = v.small(8);
+    const bool renormalise = v.flag(9);
+    const double scale = v.number(10);
+    return [=](void* s) {
+        return f_bagua_route(type_of(x.type), p.x, x.stride(), p.rows, x.count, static_cast<int>(e), masked ? p.m : nullptr, bias, score, groups, top_groups, best,
+                             static_cast<int>(i.columns), renormalise, scale, const_cast<void* const*>(p.i), i.type == at::kInt ? 4 : 8, i.stride(),
+                             reinterpret_cast<float* const*>(const_cast<void* const*>(p.w)), w.stride(), s);
+    };
+PY_END
+
+PY(route_grad, 9)   // logits, ids, weights, dweights, dlogits, score, renormalise, scale, stream
+    struct {
+        const void *x[BAGUA_MAX_WORKERS], *i[BAGUA_MAX_WORKERS], *u[BAGUA_MAX_WORKERS], *o[BAGUA_MAX_WORKERS];
+        size_t rows[BAGUA_MAX_WORKERS];
+    } p;
+    const int score = v.small(5);
+    const bool renormalise = v.flag(6), of_weights = renormalise && score == BAGUA_SCORE_SOFTMAX;
+    const double scale = v.number(7);
+    const auto o = v.matrices(4, p.o, p.rows, false, -1, -1);
+    const auto i = v.matrices(1, p.i, p.rows, true, -1, o.count);
+    const auto u = v.matrices(3, p.u, p.rows, true, i.columns, o.count);
+    const auto x = v.matrices(of_weights ? 2 : 0, p.x, p.rows, true, of_weights ? i.columns : o.columns, o.count);
+    v.ok = v.ok && type_of(o.type) >= 0 && (i.type == at::kInt || i.type == at::kLong) && u.type == at::kFloat && x.type == (of_weights ? at::kFloat : o.type) &&
+           o.columns <= BAGUA_MAX_EXPERTS && i.columns <= o.columns;
+    // (whether the list that is not read fits the others is the general path's to say)
+    const int other = of_weights ? 0 : 2;
+    v.ok = v.ok && (!v.given(other) || ((PyList_CheckExact(v.a[other]) || PyTuple_CheckExact(v.a[other])) && PySequence_Fast_GET_SIZE(v.a[other]) == o.count));
+    return [=](void* s) {
+        return f_bagua_route_grad(type_of(o.type), of_weights ? nullptr : p.x, of_weights ? 0 : x.stride(), p.rows, o.count, static_cast<int>(o.columns), p.i,
+                                  i.type == at::kInt ? 4 : 8, i.stride(), static_cast<int>(i.columns), of_weights ? reinterpret_cast<const float* const*>(p.x) : nullptr,
+                                  of_weights ? x.stride() : 0, reinterpret_cast<const float* const*>(p.u), u.stride(), score, renormalise, scale,
+                                  const_cast<void* const*>(p.o), o.stride(), s);
     };
 PY_END
 

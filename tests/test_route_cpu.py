@@ -1,0 +1,80 @@
+"""What routing to experts and its gradient refuse, from the host alone: no case here reaches a launch."""
+import ctypes
+import math
+
+import pytest
+
+OK, INVALID, ALIGN, UNSUPPORTED = 0, 1, 2, 4
+# far-apart, aligned addresses that nothing looks at
+X, I, W, U, B, M, O = (0x100000000 * i for i in range(1, 8))
+
+
+@pytest.fixture(scope="module")
+def bg():
+    import paper_2107_01499_amd as b
+    return b
+
+
+def ptrs(*a):
+    return (ctypes.c_void_p * len(a))(*a)
+
+
+def sizes(*n):
+    return (ctypes.c_size_t * len(n))(*n)
+
+
+ROUTE = dict(dtype=0, logits=ptrs(X), ld=8, tokens=sizes(10), k=1, experts=8, mask=None, bias=None, score=0, groups=1, top_groups=1, group_best=1, top=2,
+             renormalise=1, scale=1.0, ids=ptrs(I), id_bytes=8, ids_ld=2, weights=ptrs(W), weights_ld=2)
+GRAD = dict(dtype=0, logits=None, ld=0, tokens=sizes(10), k=1, experts=8, ids=ptrs(I), id_bytes=8, ids_ld=2, top=2, weights=ptrs(W), weights_ld=2, up=ptrs(U), up_ld=2,
+            score=0, renormalise=1, scale=1.0, out=ptrs(O), ld_out=8)
+OF_LOGITS = dict(logits=ptrs(X), ld=8, weights=None, weights_ld=0)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=3), INVALID), (dict(dtype=-1), INVALID), (dict(logits=None), INVALID), (dict(logits=ptrs(None)), INVALID), (dict(tokens=None), INVALID), (dict(k=0), INVALID),
+    (dict(k=33), INVALID), (dict(experts=0), INVALID), (dict(ld=7), INVALID), (dict(experts=2049, ld=2049), UNSUPPORTED), (dict(tokens=sizes(1 << 31)), UNSUPPORTED),
+    (dict(ids=None), INVALID), (dict(ids=ptrs(None)), INVALID), (dict(weights=None), INVALID), (dict(weights=ptrs(None)), INVALID), (dict(id_bytes=2), INVALID),
+    (dict(top=0), INVALID), (dict(top=9, ids_ld=9, weights_ld=9), INVALID), (dict(experts=100, ld=100, top=65, ids_ld=65, weights_ld=65), UNSUPPORTED),
+    (dict(ids_ld=1), INVALID), (dict(weights_ld=1), INVALID), (dict(ld=1 << 50), UNSUPPORTED), (dict(ids_ld=1 << 50), UNSUPPORTED), (dict(weights_ld=1 << 50), UNSUPPORTED),
+    (dict(score=2), INVALID), (dict(score=-1), INVALID), (dict(groups=0), INVALID), (dict(groups=3), INVALID), (dict(groups=4, top_groups=0), INVALID),
+    (dict(groups=4, top_groups=5), INVALID), (dict(groups=8, top_groups=1), INVALID), (dict(groups=8, top_groups=4, group_best=2), INVALID),
+    (dict(groups=4, top_groups=2, group_best=3), INVALID), (dict(groups=4, top_groups=2, group_best=0), INVALID),
+    (dict(experts=66, ld=66, groups=33, top_groups=3), UNSUPPORTED), (dict(scale=math.nan), INVALID), (dict(scale=math.inf), INVALID), (dict(mask=ptrs(None)), INVALID),
+    (dict(logits=ptrs(X + 2)), ALIGN), (dict(dtype=1, logits=ptrs(X + 1)), ALIGN), (dict(ids=ptrs(I + 4)), ALIGN), (dict(ids=ptrs(I + 2), id_bytes=4), ALIGN),
+    (dict(weights=ptrs(W + 2)), ALIGN), (dict(bias=B + 1), ALIGN), (dict(ids=ptrs(X)), INVALID), (dict(weights=ptrs(X + 316)), INVALID), (dict(weights=ptrs(I + 156)), INVALID),
+    (dict(bias=I), INVALID), (dict(mask=ptrs(W + 3)), INVALID), (dict(tokens=sizes(0), logits=ptrs(None), ids=ptrs(None), weights=ptrs(None)), OK)])
+def test_routing_refuses(bg, kw, status):
+    a = dict(ROUTE, **kw)
+    assert bg.binding.raw().bagua_route(*[a[k] for k in ROUTE], None) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=3), INVALID), (dict(tokens=None), INVALID), (dict(k=0), INVALID), (dict(k=33), INVALID), (dict(experts=0), INVALID), (dict(ids=None), INVALID),
+    (dict(ids=ptrs(None)), INVALID), (dict(up=None), INVALID), (dict(up=ptrs(None)), INVALID), (dict(out=None), INVALID), (dict(out=ptrs(None)), INVALID),
+    (dict(weights=None), INVALID), (dict(weights=ptrs(None)), INVALID), (dict(weights_ld=1), INVALID), (dict(scale=0.0), INVALID), (dict(scale=math.nan), INVALID),
+    (dict(score=1), INVALID), (dict(renormalise=0), INVALID), (dict(OF_LOGITS), INVALID), (dict(OF_LOGITS, score=1, ld=7), INVALID),
+    (dict(OF_LOGITS, score=1, logits=ptrs(None)), INVALID), (dict(OF_LOGITS, score=1, logits=ptrs(X + 2)), ALIGN), (dict(OF_LOGITS, score=1, out=ptrs(X)), INVALID),
+    (dict(OF_LOGITS, score=1, ld=1 << 50), UNSUPPORTED), (dict(weights_ld=1 << 50), UNSUPPORTED), (dict(up_ld=1 << 50), UNSUPPORTED), (dict(ids_ld=1 << 50), UNSUPPORTED),
+    (dict(ld_out=1 << 50), UNSUPPORTED), (dict(ld_out=7), INVALID), (dict(up_ld=1), INVALID), (dict(ids_ld=1), INVALID), (dict(id_bytes=3), INVALID), (dict(top=0), INVALID),
+    (dict(top=9, ids_ld=9), INVALID), (dict(experts=2049, ld_out=2049), UNSUPPORTED), (dict(weights=ptrs(W + 2)), ALIGN), (dict(up=ptrs(U + 1)), ALIGN),
+    (dict(ids=ptrs(I + 4)), ALIGN), (dict(out=ptrs(O + 2)), ALIGN), (dict(out=ptrs(I)), INVALID), (dict(out=ptrs(W + 76)), INVALID), (dict(up=ptrs(O + 300)), INVALID),
+    (dict(tokens=sizes(0), ids=ptrs(None), weights=ptrs(None), up=ptrs(None), out=ptrs(None)), OK)])
+def test_gradient_refuses(bg, kw, status):
+    a = dict(GRAD, **kw)
+    assert bg.binding.raw().bagua_route_grad(*[a[k] for k in GRAD], None) == status
+
+
+def test_calls_that_are_not_ordinary_are_declined(bg):
+    """The host extension's part of these calls leaves what it does not know to the general path, and does nothing."""
+    import torch
+    native = bg.binding._native
+    x, ids, w = torch.zeros(4, 8), torch.zeros(4, 2, dtype=torch.int64), torch.zeros(4, 2)
+    for f, count in ((native.route, 12), (native.route_grad, 9)):
+        for n in (0, count - 1, count, count + 1):
+            assert f(*[None] * n) is False
+    assert native.route([x], None, [ids], [w], None, 0, 1, 1, 1, True, 1.0, None) is False         # not on the GPU
+    assert native.route_grad([x], [ids], [w], [w], [x], 0, True, 1.0, None) is False
+    with pytest.raises(ValueError, match="expected GPU tensors"):
+        bg.bagua_route([x], None, [ids], [w])
+    with pytest.raises(ValueError, match="expected GPU tensors"):
+        bg.bagua_route_grad(None, [ids], [w], [w], [x])
