@@ -553,6 +553,46 @@ int bagua_route_grad(int dtype, const void* const* logits, size_t ld, const size
                      int score, int renormalise, double scale, void* const* dlogits, size_t ld_out, void* stream);
 
 /*
+ * Distillation from a teacher's top logits, for k data-parallel workers' rows in one launch: workers that exchange the top logits of their answers, or
+ * learn from a larger model's, need `top` numbers of a row and not the vocabulary's.  For a row x over the vocabulary, the teacher's logits y_j at
+ * ids i_j, and temperature T:
+ *   q = softmax(y / T) over the row's entries;   p = softmax(x / T);   the teacher's part = T^2 * sum_j q_j * (log q_j - log p[i_j])
+ *   the label's part = - log softmax(x)[label]
+ *   loss = teacher_weight * the teacher's part + label_weight * the label's part
+ *   d loss / d x_v = teacher_weight * T * (p_v - sum of q_j with i_j = v) + label_weight * (softmax(x)_v - [v = label])
+ * bagua_distill_loss:
+ *   dtype     BAGUA_F32, BAGUA_BF16 or BAGUA_F16: of the logits;  teacher_type: of the teacher's, any of them
+ *   logits    host[k] of device [rows[i]][vocab], rows `ld` >= vocab elements apart; the alignment of an element suffices
+ *   rows      host[k], any may be 0 (its pointers may then be NULL)
+ *   ids       host[k] of device [rows[i]][top], int32 (id_bytes 4) or int64 (8), rows `ids_ld` apart.  An id outside [0, vocab) is no entry; one that
+ *             comes twice counts twice.  A row without entries, or with none above -infinity, has no teacher's part.
+ *   teacher   host[k] of device [rows[i]][top], rows `teacher_ld` apart
+ *   labels    host[k] of device int32 or int64 (label_bytes) [rows[i]]; outside [0, vocab): the row has no label's part.  NULL: none has
+ *   mask      host[k] of device u8[rows[i]], 0 = padding: nothing of the row matters, its loss, statistics and gradient are 0; NULL: none
+ *   loss      host[k] of device fp32[rows[i]], written: of each row
+ *   stats     host[k] of device fp32[rows[i]][3], written: m = max x, sum of exp((x - m) / T), and with labels the sum of exp(x - m), else 0
+ *   workspace device, >= bagua_distill_workspace_bytes(sum of rows, vocab) bytes, 16-byte aligned.  Calls on one workspace must not overlap in time.
+ *   limits    1 <= k <= BAGUA_MAX_WORKERS, vocab <= BAGUA_MAX_VOCABULARY, 1 <= top <= BAGUA_MAX_TEACHER_ENTRIES, 2^-60 <= T <= 2^60
+ * bagua_distill_grad: backward, with the same arguments; stats as bagua_distill_loss left them.
+ *   upstream  host[k] of device fp32, the gradient of each row's loss (upstream_per_row: [rows[i]]) or of all of a worker's ([1]); NULL: 1
+ *   dlogits   host[k] of device [rows[i]][vocab] of dtype, rows ld_out apart, written: every element.  It may be the logits' own memory (dlogits[i] == logits[i],
+ *             ld_out == ld), and then takes their place; any other overlap is refused.
+ * A row with neither entries nor a label has gradient 0, whatever its logits are.  NaN and +infinity in a row that counts make its loss and gradient
+ * NaN; -infinity is a probability of 0: where the teacher or the label wants it, the loss is +infinity.  Sums are formed in fp32 in a fixed order.
+ */
+#define BAGUA_MAX_VOCABULARY 0x40000000
+#define BAGUA_MAX_TEACHER_ENTRIES 1024
+size_t bagua_distill_workspace_bytes(size_t rows, size_t vocab);
+int bagua_distill_loss(int dtype, const void* const* logits, size_t ld, const size_t* rows, int k, size_t vocab, const void* const* ids, int id_bytes,
+                       size_t ids_ld, int top, int teacher_type, const void* const* teacher, size_t teacher_ld, const void* const* labels,
+                       int label_bytes, const uint8_t* const* mask, double temperature, double teacher_weight, double label_weight,
+                       float* const* loss, float* const* stats, void* workspace, size_t workspace_bytes, void* stream);
+int bagua_distill_grad(int dtype, const void* const* logits, size_t ld, const size_t* rows, int k, size_t vocab, const void* const* ids, int id_bytes,
+                       size_t ids_ld, int top, int teacher_type, const void* const* teacher, size_t teacher_ld, const void* const* labels,
+                       int label_bytes, const uint8_t* const* mask, double temperature, double teacher_weight, double label_weight,
+                       const float* const* stats, const float* const* upstream, int upstream_per_row, void* const* dlogits, size_t ld_out, void* stream);
+
+/*
  * Measurement utilities used by the benchmark to state what the memory system of the GPU at hand delivers for
  * plain access patterns (the ceilings printed next to the roofline fractions); no arithmetic of the method.
  * bagua_probe_read: a read-only reduction, tile_sums[t] = sum of x[4096 t .. 4096 t + 4095] (device fp32[ceil(n/4096)]).

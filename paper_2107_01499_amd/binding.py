@@ -34,6 +34,8 @@ MAX_WORKERS = 32
 MAX_EXPERTS = 2048
 MAX_EXPERT_GROUPS = 32
 MAX_CHOICES = 64
+MAX_VOCABULARY = 1 << 30
+MAX_TEACHER_ENTRIES = 1024
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # BAGUA_F32, BAGUA_BF16, BAGUA_F16
 
 EXPORTS = (
@@ -49,7 +51,7 @@ EXPORTS = (
     "bagua_probe_streams", "bagua_flatten_sign_compress_ef", "bagua_decompress_unflatten", "bagua_reduce_compress_sign_ef", "bagua_decompress_sgd_step_topk", "bagua_decompress_adam_step_topk",
     "bagua_tensor_plan_bytes", "bagua_tensor_plan", "bagua_grad_norm", "bagua_adamw_step",
     "bagua_balance_workspace_bytes", "bagua_balance_stats", "bagua_balance_loss", "bagua_balance_grad",
-    "bagua_route", "bagua_route_grad",
+    "bagua_route", "bagua_route_grad", "bagua_distill_workspace_bytes", "bagua_distill_loss", "bagua_distill_grad",
 )
 
 
@@ -118,9 +120,12 @@ def _load():
     lib.bagua_balance_grad.argtypes = [i32, vp, sz, vp, i32, i32, vp, vp, vp, vp, sz, vp]
     lib.bagua_route.argtypes = [i32, vp, sz, vp, i32, i32, vp, vp, i32, i32, i32, i32, i32, i32, cd, vp, i32, sz, vp, sz, vp]
     lib.bagua_route_grad.argtypes = [i32, vp, sz, vp, i32, i32, vp, i32, sz, i32, vp, sz, vp, sz, i32, i32, cd, vp, sz, vp]
+    lib.bagua_distill_workspace_bytes.argtypes = [sz, sz]
+    lib.bagua_distill_loss.argtypes = [i32, vp, sz, vp, i32, sz, vp, i32, sz, i32, i32, vp, sz, vp, i32, vp, cd, cd, cd, vp, vp, vp, sz, vp]
+    lib.bagua_distill_grad.argtypes = [i32, vp, sz, vp, i32, sz, vp, i32, sz, i32, i32, vp, sz, vp, i32, vp, cd, cd, cd, vp, vp, i32, vp, sz, vp]
     for name in EXPORTS[2:]:
         getattr(lib, name).restype = i32
-    for name in ("bagua_batch_workspace_bytes", "bagua_tensor_plan_bytes", "bagua_balance_workspace_bytes"):
+    for name in ("bagua_batch_workspace_bytes", "bagua_tensor_plan_bytes", "bagua_balance_workspace_bytes", "bagua_distill_workspace_bytes"):
         getattr(lib, name).restype = sz
     return lib
 
@@ -815,6 +820,63 @@ def bagua_route_grad(logits, ids, weights, dweights, dlogits, score=SCORE_SOFTMA
     _check("bagua_route_grad", _lib.bagua_route_grad(
         _TYPES[dtype], la, ld, _sizes(rows), k, experts, ia, 4 if it is torch.int32 else 8, ids_ld, top, wa, weights_ld, ua, up_ld, score, int(bool(renormalise)),
         scale, oa, ld_out, _stream(stream)))
+
+
+# ---------------------------------------------------------------------------------------------- distillation
+def bagua_distill_workspace_bytes(rows, vocab):
+    """Bytes of workspace of bagua_distill_loss for so many rows of all workers together."""
+    return int(_lib.bagua_distill_workspace_bytes(rows, vocab))
+
+
+def _row_vectors(tensors, rows, dtypes, per=1):
+    """Type and addresses of a list of contiguous GPU tensors with `per` elements for every row of a worker."""
+    dtype = _type_of(tensors, "tensors with an element for every row", dtypes)
+    return dtype, (ctypes.c_void_p * len(tensors))(*[_ptr(t, dtype, per * n * t.element_size()) if n else None for t, n in zip(tensors, rows)])
+
+
+def _distill(logits, ids, teacher, labels, mask, **lists):
+    """What both passes have in common: rows, vocabulary, and the arguments from the type on up to the mask."""
+    k = len(logits)
+    _same_len(k, ids=ids, teacher=teacher, labels=labels, mask=mask, **lists)
+    if k == 0 or logits[0].dim() != 2 or ids[0].dim() != 2:
+        raise ValueError("expected 2-D tensors of at least one worker")
+    rows = [x.shape[0] for x in logits]
+    vocab, top = logits[0].shape[1], ids[0].shape[1]
+    dtype, ld, la = _matrices(logits, tuple(_TYPES), vocab)
+    it, ids_ld, ia = _matrices(ids, (torch.int32, torch.int64), top, rows)
+    tt, teacher_ld, ta = _matrices(teacher, tuple(_TYPES), top, rows)
+    bt, ba = (None, None) if labels is None else _row_vectors(labels, rows, (torch.int32, torch.int64))
+    return rows, vocab, dtype, (_TYPES[dtype], la, ld, _sizes(rows), k, vocab, ia, 4 if it is torch.int32 else 8, ids_ld, top, _TYPES[tt], ta, teacher_ld, ba,
+                                0 if bt is None else 4 if bt is torch.int32 else 8, _mask_array(mask, rows))
+
+
+def bagua_distill_loss(logits, ids, teacher, labels, mask, loss, stats, workspace, temperature=1.0, teacher_weight=1.0, label_weight=0.0, stream=None):
+    """Loss of every row of the k workers, and what the backward pass needs of it.  logits: k tensors [rows, vocab]; ids: k tensors [rows, top], int32 or
+    int64, and teacher: k tensors [rows, top], the teacher's logits there; labels: k tensors [rows], int32 or int64 (outside the vocabulary: none), or
+    None; mask: k tensors [rows] (0 = padding) or None; loss: k tensors fp32[rows] and stats: k tensors fp32[rows, 3], written."""
+    if _native.distill_loss(logits, ids, teacher, labels, mask, loss, stats, workspace, temperature, teacher_weight, label_weight, stream):
+        return
+    rows, _, _, args = _distill(logits, ids, teacher, labels, mask, loss=loss, stats=stats)
+    wp, wb = _ws(workspace)
+    _check("bagua_distill_loss", _lib.bagua_distill_loss(
+        *args, temperature, teacher_weight, label_weight, _row_vectors(loss, rows, (torch.float32,))[1], _row_vectors(stats, rows, (torch.float32,), 3)[1], wp, wb,
+        _stream(stream)))
+
+
+def bagua_distill_grad(logits, ids, teacher, labels, mask, stats, upstream, dlogits, temperature=1.0, teacher_weight=1.0, label_weight=0.0, stream=None):
+    """Gradient of the logits; stats as bagua_distill_loss left them with the same arguments.  upstream: the gradient that arrives at the losses, fp32[1] for
+    all rows or k tensors fp32[rows], or None.  dlogits may be logits themselves."""
+    if _native.distill_grad(logits, ids, teacher, labels, mask, stats, upstream, dlogits, temperature, teacher_weight, label_weight, stream):
+        return
+    per_row = isinstance(upstream, (list, tuple))
+    rows, vocab, dtype, args = _distill(logits, ids, teacher, labels, mask, stats=stats, dlogits=dlogits, **(dict(upstream=upstream) if per_row else {}))
+    _, ld_out, oa = _matrices(dlogits, (dtype,), vocab, rows)
+    if per_row:
+        ua = _row_vectors(upstream, rows, (torch.float32,))[1]
+    else:
+        ua = None if upstream is None else (ctypes.c_void_p * len(logits))(*[_ptr(upstream, torch.float32, 4)] * len(logits))
+    _check("bagua_distill_grad", _lib.bagua_distill_grad(
+        *args, temperature, teacher_weight, label_weight, _row_vectors(stats, rows, (torch.float32,), 3)[1], ua, int(per_row), oa, ld_out, _stream(stream)))
 
 
 # ---------------------------------------------------------------------------------------------- probes

@@ -30,7 +30,7 @@ namespace {
     X(bagua_decompress_sgd_step_topk) X(bagua_decompress_adam_step_topk)
 
 // Those of the calls on a plan and of rows of logits; their functions here go by the second part of the name.
-#define BAGUA_NATIVE_STEPS(X) X(grad_norm) X(adamw_step) X(balance_stats) X(balance_grad) X(route) X(route_grad)
+#define BAGUA_NATIVE_STEPS(X) X(grad_norm) X(adamw_step) X(balance_stats) X(balance_grad) X(route) X(route_grad) X(distill_loss) X(distill_grad)
 
 // The entry points, as binding.py's library has them: the address of each, so that both paths call one and the same library.
 #define X(name) decltype(&name) f_##name = nullptr;
@@ -190,6 +190,23 @@ struct Args {
             p[j] = rows[j] ? static_cast<const uint8_t*>(q) : nullptr;
         }
         return p;
+    }
+    // A list of workers' contiguous tensors of one type with `per` elements for every row: their type.
+    at::ScalarType row_vectors(int i, const void** p, const size_t* rows, int count, size_t per)
+    {
+        at::ScalarType type = at::kByte;
+        if (!ok || !(PyList_CheckExact(a[i]) || PyTuple_CheckExact(a[i])) || PySequence_Fast_GET_SIZE(a[i]) != count) { ok = false; return type; }
+        PyObject** items = PySequence_Fast_ITEMS(a[i]);
+        for (int j = 0; j < count && ok; ++j) {
+            void* q = nullptr;
+            ok = items[j] != Py_None && tensor_ptr(items[j], kAny, 0, &q);
+            if (!ok) break;
+            const at::Tensor& t = THPVariable_Unpack(items[j]);
+            if (j == 0) type = t.scalar_type();
+            ok = t.scalar_type() == type && static_cast<size_t>(t.numel()) / per >= rows[j];
+            p[j] = rows[j] ? q : nullptr;
+        }
+        return type;
     }
     size_t slots(size_t keep, size_t n, size_t chunk)
     {
@@ -646,6 +663,73 @@ PY(route_grad, 9)   // logits, ids, weights, dweights, dlogits, score, renormali
                                   i.type == at::kInt ? 4 : 8, i.stride(), static_cast<int>(i.columns), of_weights ? reinterpret_cast<const float* const*>(p.x) : nullptr,
                                   of_weights ? x.stride() : 0, reinterpret_cast<const float* const*>(p.u), u.stride(), score, renormalise, scale,
                                   const_cast<void* const*>(p.o), o.stride(), s);
+    };
+PY_END
+
+// What both passes of a distillation begin with: logits, ids, teacher, labels, mask.
+struct Distilled {
+    const void *x[BAGUA_MAX_WORKERS], *i[BAGUA_MAX_WORKERS], *t[BAGUA_MAX_WORKERS], *b[BAGUA_MAX_WORKERS];
+    const uint8_t* m[BAGUA_MAX_WORKERS];
+    size_t rows[BAGUA_MAX_WORKERS];
+    size_t ld, ids_ld, teacher_ld, vocab;
+    at::ScalarType dtype;
+    int type, teacher, k, top, id_bytes, label_bytes;
+    bool masked;
+    explicit Distilled(Args& v)
+    {
+        const auto mx = v.matrices(0, x, rows, false, -1, -1);
+        const auto mi = v.matrices(1, i, rows, true, -1, mx.count);
+        const auto mt = v.matrices(2, t, rows, true, mi.columns, mx.count);
+        const bool labelled = v.given(3);
+        const at::ScalarType label = labelled ? v.row_vectors(3, b, rows, mx.count, 1) : at::kLong;
+        masked = v.masks(4, m, rows, mx.count) != nullptr;
+        type = type_of(dtype = mx.type), teacher = type_of(mt.type), k = mx.count;
+        ld = mx.stride(), ids_ld = mi.stride(), teacher_ld = mt.stride(), vocab = static_cast<size_t>(mx.columns);
+        v.ok = v.ok && type >= 0 && teacher >= 0 && (mi.type == at::kInt || mi.type == at::kLong) && (label == at::kInt || label == at::kLong) &&
+               mx.columns <= BAGUA_MAX_VOCABULARY && mi.columns <= BAGUA_MAX_TEACHER_ENTRIES;
+        top = v.ok ? static_cast<int>(mi.columns) : 0, id_bytes = mi.type == at::kInt ? 4 : 8, label_bytes = !labelled ? 0 : label == at::kInt ? 4 : 8;
+    }
+};
+
+PY(distill_loss, 12)   // logits, ids, teacher, labels, mask, loss, stats, workspace, temperature, teacher_weight, label_weight, stream
+    const Distilled d(v);
+    struct {
+        const void *l[BAGUA_MAX_WORKERS], *s[BAGUA_MAX_WORKERS];
+    } p;
+    const bool fp32 = v.row_vectors(5, p.l, d.rows, d.k, 1) == at::kFloat && v.row_vectors(6, p.s, d.rows, d.k, 3) == at::kFloat;
+    v.ok = v.ok && fp32;
+    void* ws = v.ptr(7, kAny, 0);
+    const size_t bytes = v.ok && v.given(7) ? THPVariable_Unpack(v.a[7]).nbytes() : 0;
+    const double temperature = v.number(8), teach = v.number(9), tell = v.number(10);
+    return [=](void* s) {
+        return f_bagua_distill_loss(d.type, d.x, d.ld, d.rows, d.k, d.vocab, d.i, d.id_bytes, d.ids_ld, d.top, d.teacher, d.t, d.teacher_ld, d.label_bytes ? d.b : nullptr,
+                                    d.label_bytes, d.masked ? d.m : nullptr, temperature, teach, tell, reinterpret_cast<float* const*>(const_cast<void* const*>(p.l)),
+                                    reinterpret_cast<float* const*>(const_cast<void* const*>(p.s)), ws, bytes, s);
+    };
+PY_END
+
+PY(distill_grad, 12)   // logits, ids, teacher, labels, mask, stats, upstream, dlogits, temperature, teacher_weight, label_weight, stream
+    const Distilled d(v);
+    struct {
+        const void *s[BAGUA_MAX_WORKERS], *u[BAGUA_MAX_WORKERS], *o[BAGUA_MAX_WORKERS];
+        size_t rows[BAGUA_MAX_WORKERS];
+    } p;
+    for (int w = 0; w < d.k; ++w) p.rows[w] = d.rows[w];
+    bool fp32 = v.row_vectors(5, p.s, d.rows, d.k, 3) == at::kFloat;
+    const bool per_row = PyList_CheckExact(v.a[6]) || PyTuple_CheckExact(v.a[6]), up = v.given(6);
+    if (per_row) {
+        fp32 = v.row_vectors(6, p.u, d.rows, d.k, 1) == at::kFloat && fp32;
+    } else {
+        const float* one = v.f32(6, 1);
+        for (int w = 0; w < d.k; ++w) p.u[w] = one;
+    }
+    const auto o = v.matrices(7, p.o, p.rows, true, static_cast<int64_t>(d.vocab), d.k);
+    v.ok = v.ok && fp32 && o.type == d.dtype;
+    const double temperature = v.number(8), teach = v.number(9), tell = v.number(10);
+    return [=](void* s) {
+        return f_bagua_distill_grad(d.type, d.x, d.ld, d.rows, d.k, d.vocab, d.i, d.id_bytes, d.ids_ld, d.top, d.teacher, d.t, d.teacher_ld, d.label_bytes ? d.b : nullptr,
+                                    d.label_bytes, d.masked ? d.m : nullptr, temperature, teach, tell, reinterpret_cast<const float* const*>(p.s),
+                                    up ? reinterpret_cast<const float* const*>(p.u) : nullptr, per_row, const_cast<void* const*>(p.o), o.stride(), s);
     };
 PY_END
 

@@ -1,0 +1,82 @@
+"""What distillation and its gradient refuse, from the host alone: no case here reaches a launch."""
+import ctypes
+import math
+
+import pytest
+
+OK, INVALID, ALIGN, UNSUPPORTED = 0, 1, 2, 4
+# far-apart, aligned addresses that nothing looks at
+X, I, T, B, M, L, S, W, U, O = (0x100000000 * i for i in range(1, 11))
+
+
+@pytest.fixture(scope="module")
+def bg():
+    import paper_2107_01499_amd as b
+    return b
+
+
+def ptrs(*a):
+    return (ctypes.c_void_p * len(a))(*a)
+
+
+def sizes(*n):
+    return (ctypes.c_size_t * len(n))(*n)
+
+
+BOTH = dict(dtype=0, logits=ptrs(X), ld=100, rows=sizes(10), k=1, vocab=100, ids=ptrs(I), id_bytes=8, ids_ld=4, top=4, teacher_type=0, teacher=ptrs(T), teacher_ld=4,
+            labels=ptrs(B), label_bytes=8, mask=None, temperature=2.0, teach=1.0, tell=0.5)
+LOSS = dict(BOTH, loss=ptrs(L), stats=ptrs(S), ws=W, bytes=1 << 20)
+GRAD = dict(BOTH, stats=ptrs(S), up=None, per_row=0, out=ptrs(O), ld_out=100)
+
+BAD = [(dict(dtype=3), INVALID), (dict(logits=None), INVALID), (dict(logits=ptrs(None)), INVALID), (dict(rows=None), INVALID), (dict(k=0), INVALID), (dict(k=33), INVALID),
+       (dict(vocab=0), INVALID), (dict(ld=99), INVALID), (dict(vocab=(1 << 30) + 1, ld=1 << 31, ld_out=1 << 31), UNSUPPORTED), (dict(rows=sizes(1 << 31)), UNSUPPORTED), (dict(ids=None), INVALID),
+       (dict(ids=ptrs(None)), INVALID), (dict(id_bytes=2), INVALID), (dict(top=0), INVALID), (dict(ids_ld=3), INVALID), (dict(teacher_ld=3), INVALID),
+       (dict(top=1025, ids_ld=1025, teacher_ld=1025), UNSUPPORTED), (dict(teacher_type=3), INVALID), (dict(teacher=None), INVALID), (dict(teacher=ptrs(None)), INVALID),
+       (dict(label_bytes=1), INVALID), (dict(labels=ptrs(None)), INVALID), (dict(mask=ptrs(None)), INVALID), (dict(temperature=0.0), INVALID), (dict(temperature=-1.0), INVALID),
+       (dict(temperature=math.nan), INVALID), (dict(temperature=math.inf), INVALID), (dict(temperature=1e-30), UNSUPPORTED), (dict(temperature=1e30), UNSUPPORTED),
+       (dict(teach=math.nan), INVALID), (dict(tell=math.inf), INVALID), (dict(ld=1 << 50), UNSUPPORTED), (dict(ids_ld=1 << 50), UNSUPPORTED), (dict(teacher_ld=1 << 50), UNSUPPORTED),
+       (dict(logits=ptrs(X + 2)), ALIGN), (dict(dtype=1, logits=ptrs(X + 1)), ALIGN), (dict(ids=ptrs(I + 4)), ALIGN), (dict(teacher=ptrs(T + 2)), ALIGN),
+       (dict(teacher_type=2, teacher=ptrs(T + 1)), ALIGN), (dict(labels=ptrs(B + 4)), ALIGN), (dict(stats=None), INVALID), (dict(stats=ptrs(None)), INVALID), (dict(stats=ptrs(S + 2)), ALIGN)]
+
+
+@pytest.mark.parametrize("kw,status", BAD + [
+    (dict(loss=None), INVALID), (dict(loss=ptrs(None)), INVALID), (dict(ws=None), INVALID), (dict(bytes=8), INVALID), (dict(loss=ptrs(L + 1)), ALIGN), (dict(ws=W + 8), ALIGN),
+    (dict(loss=ptrs(X + 3996)), INVALID), (dict(stats=ptrs(L + 36)), INVALID), (dict(stats=ptrs(T)), INVALID), (dict(loss=ptrs(I)), INVALID), (dict(ws=B), INVALID),
+    (dict(mask=ptrs(S + 119)), INVALID), (dict(rows=sizes(0), logits=ptrs(None), ids=ptrs(None), teacher=ptrs(None), labels=ptrs(None), loss=ptrs(None), stats=ptrs(None)), OK)])
+def test_loss_refuses(bg, kw, status):
+    a = {k: v for k, v in dict(LOSS, **kw).items() if k in LOSS}
+    assert bg.binding.raw().bagua_distill_loss(*[a[k] for k in LOSS], None) == status
+
+
+@pytest.mark.parametrize("kw,status", BAD + [
+    (dict(out=None), INVALID), (dict(out=ptrs(None)), INVALID), (dict(ld_out=99), INVALID), (dict(ld_out=1 << 50), UNSUPPORTED), (dict(out=ptrs(O + 2)), ALIGN),
+    (dict(up=ptrs(None)), INVALID), (dict(up=ptrs(U + 2)), ALIGN), (dict(out=ptrs(X + 4)), INVALID), (dict(out=ptrs(X), ld_out=101), INVALID), (dict(out=ptrs(S)), INVALID),
+    (dict(up=ptrs(O + 3996)), INVALID), (dict(up=ptrs(O - 4), per_row=1), INVALID), (dict(out=ptrs(I)), INVALID), (dict(labels=ptrs(O + 3992)), INVALID),
+    (dict(rows=sizes(0), logits=ptrs(None), ids=ptrs(None), teacher=ptrs(None), labels=ptrs(None), stats=ptrs(None), out=ptrs(None)), OK)])
+def test_gradient_refuses(bg, kw, status):
+    a = {k: v for k, v in dict(GRAD, **kw).items() if k in GRAD}
+    assert bg.binding.raw().bagua_distill_grad(*[a[k] for k in GRAD], None) == status
+
+
+def test_workspace(bg):
+    size = bg.bagua_distill_workspace_bytes
+    assert size(10, 0) == 0 == size(10, (1 << 30) + 1) == size(1 << 31, 10)
+    assert 0 < size(0, 100) <= size(1, 100) and size(1, 1 << 20) > size(1, 100)
+    # few rows never take more than many parts of each: what a call has to hold stays small
+    assert max(size(r, v) for r in (1, 5, 100, 2047, 2048, 100000) for v in (1, 4096, 50000, 1 << 30)) < 1 << 20
+
+
+def test_calls_that_are_not_ordinary_are_declined(bg):
+    """The host extension's part of these calls leaves what it does not know to the general path, and does nothing."""
+    import torch
+    native = bg.binding._native
+    x, ids, y, l, s = torch.zeros(4, 50), torch.zeros(4, 3, dtype=torch.int64), torch.zeros(4, 3), torch.zeros(4), torch.zeros(4, 3)
+    for f in (native.distill_loss, native.distill_grad):
+        for n in (0, 11, 12, 13):
+            assert f(*[None] * n) is False
+    assert native.distill_loss([x], [ids], [y], None, None, [l], [s], l, 1.0, 1.0, 0.0, None) is False        # not on the GPU
+    assert native.distill_grad([x], [ids], [y], None, None, [s], None, [x], 1.0, 1.0, 0.0, None) is False
+    with pytest.raises(ValueError, match="expected GPU tensors"):
+        bg.bagua_distill_loss([x], [ids], [y], None, None, [l], [s], l)
+    with pytest.raises(ValueError, match="expected GPU tensors"):
+        bg.bagua_distill_grad([x], [ids], [y], None, None, [s], None, [x])

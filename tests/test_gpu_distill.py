@@ -1,0 +1,371 @@
+"""Distillation from a teacher's top logits: loss, statistics and gradient against the formulas in 64 bits, and the gradient against differences of the loss."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF_ULP = {"f32": U, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+LEAST = {"f32": 2.0 ** -149, "bf16": 2.0 ** -133, "f16": 2.0 ** -24}
+
+
+@pytest.fixture(scope="module")
+def bg():
+    import paper_2107_01499_amd as b
+    assert torch.cuda.is_available()
+    return b
+
+
+def matrix(rows, columns, dtype, pad=0, offset=0, fill=0.0):
+    """A matrix whose rows lie `pad` elements further apart than they are long, `offset` elements into its storage."""
+    store = torch.full((offset + rows * (columns + pad) + 8,), fill, device="cuda").to(dtype)
+    m = store[offset:offset + rows * (columns + pad)].view(rows, columns + pad)[:, :columns]
+    m.store, m.offset = store, offset
+    return m
+
+
+def untouched(m, fill):
+    """What lies between the rows, in front of the first and behind the last."""
+    rest = m.store.cpu().double().numpy()
+    keep = np.ones(rest.shape, bool)
+    rows, columns = m.shape
+    wide = m.stride(0) if rows > 1 else columns
+    for r in range(rows):
+        keep[m.offset + r * wide:m.offset + r * wide + columns] = False
+    return np.all(rest[keep] == fill)
+
+
+def inputs(rows, vocab, top, dtype, seed, teacher="f32", ids=torch.int64, labels=torch.int64, masked=None, pad=0, offset=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    s = dict(logits=[], ids=[], teacher=[], labels=None if labels is None else [], mask=None if masked is None else [])
+    for n in rows:
+        x = matrix(n, vocab, TYPES[dtype], pad, offset, math.nan)
+        x.copy_(torch.randn(n, vocab, device="cuda", generator=g) * 2)
+        s["logits"].append(x)
+        i = matrix(n, top, ids, pad, 0, -7)
+        # distinct where the vocabulary allows it
+        pick = torch.rand(n, vocab, device="cuda", generator=g).argsort(1)[:, :top] if vocab <= 5000 else torch.randint(0, vocab, (n, top), device="cuda", generator=g)
+        if top > vocab:
+            pick = torch.randint(0, vocab, (n, top), device="cuda", generator=g)
+        i.copy_(pick)
+        i[torch.rand(n, top, device="cuda", generator=g) < 0.1] = -1
+        s["ids"].append(i)
+        t = matrix(n, top, TYPES[teacher], pad, 0, math.nan)
+        t.copy_(torch.randn(n, top, device="cuda", generator=g) * 2)
+        s["teacher"].append(t)
+        if labels is not None:
+            b = torch.randint(0, vocab, (n,), device="cuda", generator=g).to(labels)
+            b[torch.rand(n, device="cuda", generator=g) < 0.2] = -100
+            s["labels"].append(b)
+        if masked is not None:
+            m = torch.rand(n, device="cuda", generator=g) >= masked
+            x[~m] = math.nan
+            s["mask"].append(m)
+    return s
+
+
+def truth(s, w, temperature, teach, tell, up=None):
+    """(loss, stats, gradient, size of what is added up for the loss and for the gradient) of worker w in 64 bits."""
+    x = s["logits"][w].double().cpu().numpy()
+    n, v = x.shape
+    ids, y = s["ids"][w].cpu().numpy(), s["teacher"][w].double().cpu().numpy() / temperature
+    labels = np.full(n, -1) if s["labels"] is None else s["labels"][w].cpu().numpy()
+    keep = np.ones(n, bool) if s["mask"] is None else s["mask"][w].cpu().numpy().astype(bool)
+    loss, stats, grad = np.zeros(n), np.zeros((n, 3)), np.zeros((n, v))
+    loss_size, grad_size = np.zeros(n), np.zeros((n, v))
+    for r in np.flatnonzero(keep):
+        m = x[r].max()
+        z = x[r] - m
+        e, e1 = np.exp(z / temperature), np.exp(z)
+        stats[r] = m, e.sum(), e1.sum() if s["labels"] is not None else 0.0
+        u = 1.0 if up is None else float(up[r])
+        there = (ids[r] >= 0) & (ids[r] < v) & (y[r] != -np.inf)       # an entry of probability 0 adds 0 * log 0 = 0
+        i, t = ids[r][there], y[r][there]
+        if i.size:
+            log_q = t - t.max()
+            log_q = log_q - np.log(np.exp(log_q).sum())
+            q, log_p = np.exp(log_q), z[i] / temperature - np.log(e.sum())
+            loss[r] += teach * temperature ** 2 * (q * (log_q - log_p)).sum()
+            loss_size[r] += abs(teach) * temperature ** 2 * (q * (np.abs(log_q) + np.abs(log_p))).sum()
+            p = e / e.sum()
+            grad[r] += u * teach * temperature * p
+            np.add.at(grad[r], i, -u * teach * temperature * q)
+            grad_size[r] += abs(u * teach * temperature) * p
+            np.add.at(grad_size[r], i, abs(u * teach * temperature) * q)
+        if 0 <= labels[r] < v:
+            loss[r] += tell * (np.log(e1.sum()) - z[labels[r]])
+            loss_size[r] += abs(tell) * (np.log(e1.sum()) - z[labels[r]])
+            grad[r] += u * tell * e1 / e1.sum()
+            grad[r, labels[r]] -= u * tell
+            grad_size[r] += abs(u * tell) * e1 / e1.sum()
+            grad_size[r, labels[r]] += abs(u * tell)
+    return loss, stats, grad, loss_size, grad_size
+
+
+def depth(s, vocab, top, temperature):
+    """Relative error of a sum and of an exponential: the argument of the latter, a difference times a factor, is off by 3 U of itself, and e^-a * a is
+    below 1/2 wherever it matters for a sum; a thread adds vocab / 64 of them in a chain, at most, then 14 exchanges and scalings."""
+    reach = max([float((x[torch.isfinite(x)].double().max() - x[torch.isfinite(x)].double().min()) / min(temperature, 1.0)) if torch.isfinite(x).any() else 0.0
+                 for x in s["logits"]])
+    return (vocab / 64 + 40 + top / 64) * U, (3 * reach + vocab / 64 + 60 + top / 64) * U
+
+
+def check(bg, s, temperature=1.0, teach=1.0, tell=0.5, up="one", pad=0, offset=0, in_place=False):
+    rows, vocab, top = [x.shape[0] for x in s["logits"]], s["logits"][0].shape[1], s["ids"][0].shape[1]
+    dtype = [k for k, v in TYPES.items() if v is s["logits"][0].dtype][0]
+    loss, stats = [torch.full((n + 2,), 7.0, device="cuda") for n in rows], [torch.full((n + 1, 3), 7.0, device="cuda") for n in rows]
+    need = bg.bagua_distill_workspace_bytes(sum(rows), vocab)
+    ws = torch.full((need + 32,), 91, dtype=torch.uint8, device="cuda")
+    bg.bagua_distill_loss(s["logits"], s["ids"], s["teacher"], s["labels"], s["mask"], loss, stats, ws[:need], temperature, teach, tell)
+    assert torch.all(ws[need:] == 91)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    ups = {"none": None, "one": torch.tensor([0.25], device="cuda"), "rows": [torch.randn(n, device="cuda", generator=g) for n in rows]}[up]
+    if in_place:
+        out = s["logits"]
+        before = dict(s, logits=[x.clone() for x in s["logits"]])
+    else:
+        out = [matrix(n, vocab, TYPES[dtype], pad, offset, 5.0) for n in rows]
+        before = s
+    bg.bagua_distill_grad(s["logits"], s["ids"], s["teacher"], s["labels"], s["mask"], stats, ups, out, temperature, teach, tell)
+    in_sum, in_exp = depth(before, vocab, top, temperature)
+    for w, n in enumerate(rows):
+        u = None if ups is None else (ups[w] if up == "rows" else ups.expand(n)).cpu()
+        want_loss, want_stats, want, loss_size, size = truth(before, w, temperature, teach, tell, u)
+        got = loss[w].double().cpu().numpy()
+        assert np.all(got[n:] == 7) and torch.all(stats[w][n:] == 7)
+        # beside the sums: logarithms to 2 U of themselves and what the sums' errors leave there, quotients, products; a dozen roundings
+        assert np.all(np.abs(got[:n] - want_loss) <= 24 * U * loss_size + 2 * in_sum * (abs(teach) * temperature ** 2 + abs(tell)) + 1e-38), np.max(np.abs(got[:n] - want_loss))
+        got = stats[w][:n].double().cpu().numpy()
+        assert np.array_equal(got[:, 0], want_stats[:, 0]) and np.all(np.abs(got[:, 1:] - want_stats[:, 1:]) <= in_sum * want_stats[:, 1:])
+        got = out[w].double().cpu().numpy()
+        allowed = 2 * in_exp * size + HALF_ULP[dtype] * np.abs(want) * 1.001 + LEAST[dtype]
+        assert np.all(np.abs(got - want) <= allowed), np.max(np.abs(got - want) / allowed)
+        if not in_place:
+            assert untouched(out[w], 5.0)
+    return loss, stats, out
+
+
+VOCABS = [1, 2, 3, 7, 8, 9, 63, 64, 65, 513, 1009, 4095, 4096, 4097, 8191, 16390, 30522, 40001]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("vocab", VOCABS)
+def test_every_vocabulary(bg, vocab, dtype):
+    print("distill vocab=%d %s" % (vocab, dtype), flush=True)
+    top = min(vocab, 9)
+    for temperature, labels, up in ((1.0, None, "none"), (1.0, torch.int64, "one"), (2.0, torch.int32, "rows"), (0.7, None, "one")):
+        s = inputs([5, 0, 1, 3], vocab, top, dtype, vocab, labels=labels, pad=vocab % 3, offset=vocab % 2)
+        check(bg, s, temperature, up=up, pad=(vocab + 1) % 4, offset=vocab % 5)
+
+
+@pytest.mark.parametrize("top", [1, 2, 63, 64, 65, 130, 1024])
+@pytest.mark.parametrize("teacher,ids", [("f32", torch.int64), ("bf16", torch.int32), ("f16", torch.int64)])
+def test_every_number_of_entries(bg, top, teacher, ids):
+    print("distill top=%d %s" % (top, teacher), flush=True)
+    for vocab in (50, 3000, 50001):
+        check(bg, inputs([3, 2], vocab, top, "bf16", top, teacher=teacher, ids=ids, pad=top % 2), 2.0, teach=0.7, tell=0.3, up="rows")
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,vocab", [([1], 200003), ([2, 1], 131072), ([40], 60000), ([300], 17000), ([70, 30], 1009), ([3000], 700), ([1], 1500007)])
+def test_few_and_many_rows(bg, rows, vocab, dtype):
+    """Rows that several workgroups share, and those that one has."""
+    print("distill rows=%s vocab=%d %s" % (rows, vocab, dtype), flush=True)
+    check(bg, inputs(rows, vocab, 20, dtype, vocab), 2.0)
+    check(bg, inputs(rows, vocab, 20, dtype, vocab + 1, masked=0.4), 1.0, up="rows")
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("vocab", [9, 1009, 30522, 100001])
+def test_padding(bg, vocab, dtype):
+    for masked in (0.0, 0.5, 1.0):
+        s = inputs([9, 0, 4], vocab, 5, dtype, 3, masked=masked)
+        loss, stats, out = check(bg, s, 2.0)
+        for m, l, t, o in zip(s["mask"], loss, stats, out):
+            n = m.shape[0]
+            assert torch.all(l[:n][~m] == 0) and torch.all(t[:n][~m] == 0) and torch.all(o[~m] == 0)
+        check(bg, dict(s, mask=[m.to(torch.uint8) * 3 for m in s["mask"]]), 2.0)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("vocab,rows", [(9, [3, 1]), (1009, [7]), (30522, [5, 3]), (100001, [2]), (8192, [4])])
+def test_gradient_in_place(bg, vocab, rows, dtype):
+    for pad, offset in ((0, 0), (3, 1)):
+        for labels in (None, torch.int64):
+            check(bg, inputs(rows, vocab, 8, dtype, vocab, labels=labels, pad=pad, offset=offset, masked=0.3), 2.0, in_place=True)
+
+
+def test_entries_that_are_none_or_come_twice(bg):
+    for vocab in (50, 20000):
+        s = inputs([12], vocab, 6, "f32", 4)
+        ids, x, y, labels = s["ids"][0], s["logits"][0], s["teacher"][0], s["labels"][0]
+        ids.copy_(torch.randint(0, 4, (12, 6), device="cuda"))       # with repetitions
+        ids[0] = -1                                                  # no entry
+        ids[1, 2:] = vocab
+        ids[2] = 3                                                   # one entry, six times
+        ids[3, 0] = 1 << 33 | 1                                      # its lower half would be an id
+        labels[0], labels[1], labels[2], labels[4] = 5, vocab, 3, -1
+        ids[5], labels[5], x[5] = -1, -1, math.nan                   # nothing to learn: the logits do not matter to the gradient
+        y[6] = -math.inf                                             # an entry that the teacher excludes, and a row of them
+        y[7, 1:] = -math.inf
+        loss, stats = [torch.zeros(12, device="cuda")], [torch.zeros(12, 3, device="cuda")]
+        ws, out = torch.zeros(bg.bagua_distill_workspace_bytes(12, vocab), dtype=torch.uint8, device="cuda"), [torch.full_like(x, 9.0)]
+        bg.bagua_distill_loss([x], [ids], [y], [labels], None, loss, stats, ws, 2.0, 1.0, 0.5)
+        bg.bagua_distill_grad([x], [ids], [y], [labels], None, stats, None, out, 2.0, 1.0, 0.5)
+        assert torch.all(out[0][5] == 0) and float(loss[0][5]) == 0
+        rest = [r for r in range(12) if r != 5]
+        part = dict(logits=[x[rest]], ids=[ids[rest]], teacher=[y[rest]], labels=[labels[rest]], mask=None)
+        want_loss, _, want, loss_size, size = truth(part, 0, 2.0, 1.0, 0.5)
+        in_sum, in_exp = depth(part, vocab, 6, 2.0)
+        assert np.all(np.abs(loss[0][rest].double().cpu().numpy() - want_loss) <= 24 * U * loss_size + 2 * in_sum * 4.5)
+        assert np.all(np.abs(out[0][rest].double().cpu().numpy() - want) <= 2 * in_exp * size + 2 * U * np.abs(want) + 2.0 ** -149)
+        again = [torch.empty_like(x)]
+        bg.bagua_distill_grad([x], [ids], [y], [labels], None, stats, None, again, 2.0, 1.0, 0.5)
+        assert torch.equal(again[0], out[0])
+
+
+@pytest.mark.parametrize("vocab", [33, 5000, 70001])
+def test_numbers_that_are_not_finite(bg, vocab):
+    for dtype in TYPES:
+        s = inputs([8], vocab, 4, dtype, 6)
+        x, ids = s["logits"][0], s["ids"][0]
+        ids.copy_(torch.arange(4, device="cuda").expand(8, 4) + 8)
+        s["labels"][0].fill_(20)
+        x[1, 0] = math.nan
+        x[2, vocab - 1] = math.inf
+        x[3, 12:20] = -math.inf                                      # neither wanted by the teacher nor by the label
+        x[4, 9] = -math.inf                                          # wanted by the teacher
+        x[5, 20] = -math.inf                                         # by the label
+        x[6] = -math.inf                                             # probabilities of 0 throughout
+        x[7] = 3e38 if dtype != "f16" else 6e4
+        loss, stats = [torch.zeros(8, device="cuda")], [torch.zeros(8, 3, device="cuda")]
+        ws, out = torch.zeros(bg.bagua_distill_workspace_bytes(8, vocab), dtype=torch.uint8, device="cuda"), [torch.full_like(x, 9.0)]
+        for temperature in (1.0, 2.0):
+            bg.bagua_distill_loss([x], [ids], s["teacher"], s["labels"], None, loss, stats, ws, temperature, 1.0, 0.5)
+            bg.bagua_distill_grad([x], [ids], s["teacher"], s["labels"], None, stats, None, out, temperature, 1.0, 0.5)
+            got = loss[0].cpu()
+            assert torch.isnan(got[1:3]).all() and torch.isinf(got[4:7]).all() and torch.all(got[4:7] > 0) and torch.isfinite(got[[0, 3, 7]]).all()
+            d = out[0].float().cpu()
+            assert torch.isnan(d[1:3]).all() and torch.isfinite(d[[0, 3, 4, 5, 6, 7]]).all()
+            assert torch.all(d[3, 12:20] == 0) and d[4, 9] < 0 and d[5, 20] < 0
+            assert torch.all(d[6, 21:] == 0) and torch.all(d[6, 8:12] < 0)
+
+
+def test_logits_of_great_magnitude(bg):
+    """The same differences around a large number: statistics are relative to the largest."""
+    for base in (0.0, 4096.0, -65536.0):
+        s = inputs([6], 3000, 5, "f32", 8)
+        s["logits"][0].mul_(8).round_().div_(8).add_(base)
+        check(bg, s, 2.0)
+
+
+def test_weights_of_zero_and_below(bg):
+    for teach, tell in ((0.0, 1.0), (1.0, 0.0), (-0.5, 2.0), (0.0, 0.0)):
+        check(bg, inputs([4], 700, 5, "f32", 9), 2.0, teach, tell)
+
+
+@pytest.mark.parametrize("temperature", [1.0, 2.0])
+def test_gradient_against_differences(bg, temperature):
+    """(L(x + h) - L(x - h)) / 2h of the rows' losses."""
+    rows, vocab, h = 6, 24, 2.0 ** -5
+    s = inputs([rows], vocab, 4, "f32", 10)
+    ws = torch.zeros(bg.bagua_distill_workspace_bytes(rows, vocab), dtype=torch.uint8, device="cuda")
+    loss, stats, d = [torch.zeros(rows, device="cuda")], [torch.zeros(rows, 3, device="cuda")], [torch.zeros(rows, vocab, device="cuda")]
+    args = lambda x: ([x], s["ids"], s["teacher"], s["labels"], None)  # noqa: E731
+    x = s["logits"][0].contiguous()
+    bg.bagua_distill_loss(*args(x), loss, stats, ws, temperature, 1.0, 0.5)
+    size = loss[0].abs().max().item()
+    bg.bagua_distill_grad(*args(x), stats, None, d, temperature, 1.0, 0.5)
+    for v in range(vocab):
+        sides = []
+        for sign in (1.0, -1.0):
+            y = x.clone()
+            y[:, v] += sign * h
+            bg.bagua_distill_loss(*args(y), loss, stats, ws, temperature, 1.0, 0.5)
+            sides.append(loss[0].double().clone())
+        # third derivative of a logarithm of a sum of exponentials: below 1/8 at T = 1 and / T^3; a loss is a sum of terms up to 20 times as large
+        allowed = h * h / 6 * 1.5 + 60 * U * max(20.0, size) * temperature ** 2 / h
+        assert torch.all(((sides[0] - sides[1]) / (2 * h) - d[0][:, v].double()).abs() <= allowed)
+
+
+def test_in_a_graph_and_on_streams(bg):
+    """Captured and replayed on other rows, two graphs with a workspace of their own each; and two streams at once."""
+    rows, vocab = [20, 0, 5], 70001
+    s = [inputs(rows, vocab, 20, "bf16", 11 + i, masked=0.2) for i in range(2)]
+    need = bg.bagua_distill_workspace_bytes(sum(rows), vocab)
+    bufs = [dict(ws=torch.zeros(need, dtype=torch.uint8, device="cuda"), loss=[torch.zeros(n, device="cuda") for n in rows],
+                 stats=[torch.zeros(n, 3, device="cuda") for n in rows], out=[torch.zeros_like(x) for x in s[0]["logits"]]) for _ in range(2)]
+
+    def step(i, stream=None):
+        a, b = s[i], bufs[i]
+        bg.bagua_distill_loss(a["logits"], a["ids"], a["teacher"], a["labels"], a["mask"], b["loss"], b["stats"], b["ws"], 2.0, 1.0, 0.5, stream)
+        bg.bagua_distill_grad(a["logits"], a["ids"], a["teacher"], a["labels"], a["mask"], b["stats"], None, b["out"], 2.0, 1.0, 0.5, stream)
+
+    flat = lambda i: bufs[i]["loss"] + bufs[i]["stats"] + bufs[i]["out"]  # noqa: E731
+    want = []
+    for i in range(2):
+        step(i)
+        want.append([t.clone() for t in flat(i)])
+    graphs = []
+    for i in range(2):
+        graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=stream):
+            step(i)
+        graphs.append(graph)
+    same = lambda i: all(torch.equal(a, b) for a, b in zip(flat(i), want[i]))  # noqa: E731
+    for seed in range(3):
+        for i in range(2):
+            for t in flat(i):
+                t.zero_()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        assert same(0) and same(1)
+        fresh = inputs(rows, vocab, 20, "bf16", 30 + seed, masked=0.2)
+        for i in range(2):
+            for key in ("logits", "ids", "teacher", "labels", "mask"):
+                for t, f in zip(s[i][key], fresh[key]):
+                    t.copy_(f)
+            step(i)
+            want[i] = [t.clone() for t in flat(i)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for t in flat(0) + flat(1):
+        t.zero_()
+    torch.cuda.synchronize()
+    for i, stream in enumerate(streams):
+        step(i, stream)
+    torch.cuda.synchronize()
+    assert same(0) and same(1)
+
+
+def test_refusals(bg):
+    x, ids, y = torch.zeros(4, 50, device="cuda"), torch.zeros(4, 3, dtype=torch.int64, device="cuda"), torch.zeros(4, 3, device="cuda")
+    labels, loss, stats = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, device="cuda"), torch.zeros(4, 3, device="cuda")
+    ws = torch.zeros(1024, dtype=torch.uint8, device="cuda")
+    forward = lambda x=x, ids=ids, y=y, labels=labels, mask=None, loss=loss, stats=stats, ws=ws, **kw: bg.bagua_distill_loss(  # noqa: E731
+        [x], [ids], [y], None if labels is None else [labels], mask, [loss], [stats], ws, **kw)
+    back = lambda x=x, out=None, up=None, stats=stats, **kw: bg.bagua_distill_grad(  # noqa: E731
+        [x], [ids], [y], [labels], None, [stats], up, [torch.zeros_like(x) if out is None else out], **kw)
+    for words, f in (("expected one of", lambda: forward(x=x.double())), ("expected one of", lambda: forward(ids=ids.short())), ("expected one of", lambda: forward(y=y.double())),
+                     ("rows", lambda: forward(ids=ids[:3])), ("columns", lambda: forward(y=y[:, :2])), ("too small", lambda: forward(labels=labels[:3])),
+                     ("element for every row", lambda: forward(labels=labels.float())), ("too small", lambda: forward(loss=loss[:3])), ("too small", lambda: forward(stats=stats[:3])),
+                     ("element for every row", lambda: forward(loss=loss.half())), ("mask must be", lambda: forward(mask=[loss])),
+                     ("equally far apart", lambda: forward(x=x[:1].expand(4, 50))), ("expected one of", lambda: back(out=x.bfloat16())),
+                     ("rows", lambda: back(out=torch.zeros(3, 50, device="cuda"))), ("too small", lambda: back(up=[loss[:2]])), ("names 2 tensors", lambda: back(up=[loss, loss])),
+                     ("too small", lambda: back(up=torch.zeros(0, device="cuda")))):
+        with pytest.raises(ValueError, match=words):
+            f()
+    for f in (lambda: forward(ws=ws[:8]), lambda: forward(temperature=0.0), lambda: forward(temperature=math.nan), lambda: forward(label_weight=math.inf),
+              lambda: forward(loss=stats.view(-1)), lambda: back(temperature=-1.0), lambda: back(out=x, stats=x.view(-1)[:12].view(4, 3))):
+        with pytest.raises(bg.BaguaError, match="INVALID"):
+            f()
+    big = torch.zeros(2, 200, device="cuda")
+    with pytest.raises(bg.BaguaError, match="INVALID"):              # the logits' memory, but not element upon element
+        bg.bagua_distill_grad([big[:, :50]], [ids[:2]], [y[:2]], None, None, [stats[:2]], None, [big.view(4, 100)[:2, :50]])
+    with pytest.raises(bg.BaguaError, match="UNSUPPORTED"):
+        forward(temperature=1e-30)
