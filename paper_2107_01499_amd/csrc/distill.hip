@@ -54,7 +54,7 @@ struct Taught {
                                               : static_cast<uint64_t>(static_cast<int64_t>(t.template ptr<const int32_t>(kLabels)[t.t0]));
         return v < a.vocab ? static_cast<int>(v) : -1;
     }
-    __device__ __forceinline__ bool counts() const { return t.at[kMask] == 0 || t.template ptr<const uint8_t>(kMask)[t.t0] != 0; }
+    __device__ __forceinline__ bool counts() const { return !t.has(kMask) || t.template ptr<const uint8_t>(kMask)[t.t0] != 0; }
 };
 
 // The teacher's softmax over its entries, by a wave that has entry j in lane j % 64: its largest logit and the sum relative to it; no entry: sum 0.
@@ -171,8 +171,7 @@ k_distill(Lists<kDistillLists> ls, DistillArgs a)
     __shared__ float of_wave[WAVES][1 + SUMS];
     const int lane = threadIdx.x & 63, wave = wave_index();
     const uint32_t unit = blockIdx.x / a.parts, part = blockIdx.x - unit * a.parts;
-    const LaneLists<kDistillLists> table(ls);
-    const ListTile<kDistillLists> t(table, unit, 1);
+    const ListTile<kDistillLists> t(ls, unit, 1);
     const Taught<kDistillLists> w{a, t};
     if (!w.counts()) {
         if (part == 0 && threadIdx.x < 3) {
@@ -255,8 +254,7 @@ k_distill_finish(Lists<kDistillLists> ls, DistillArgs a)
 {
     typedef typename Elem<TYPE>::one one;
     const int lane = threadIdx.x & 63;
-    const LaneLists<kDistillLists> table(ls);
-    const ListTile<kDistillLists> t(table, blockIdx.x, 1);
+    const ListTile<kDistillLists> t(ls, blockIdx.x, 1);
     const Taught<kDistillLists> w{a, t};
     if (!w.counts()) return;
     const one* row = t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0) * a.ld;
@@ -287,8 +285,7 @@ k_distill_grad(Lists<kDistillGradLists> ls, DistillArgs a)
     float *named_x = named + a.top + 1, *named_less = named + 2 * (a.top + 1);
     const int lane = threadIdx.x & 63;
     const uint32_t unit = blockIdx.x / a.parts, part = blockIdx.x - unit * a.parts;
-    const LaneLists<kDistillGradLists> table(ls);
-    const ListTile<kDistillGradLists> t(table, unit, 1);
+    const ListTile<kDistillGradLists> t(ls, unit, 1);
     const Taught<kDistillGradLists> w{a, t};
     const one* row = t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0) * a.ld;
     one* out = t.template ptr<one>(kOut) + static_cast<size_t>(t.t0) * a.out_ld;
@@ -304,7 +301,7 @@ k_distill_grad(Lists<kDistillGradLists> ls, DistillArgs a)
         return;
     }
     const float* stats = t.template ptr<const float>(kStats) + static_cast<size_t>(t.t0) * 3;
-    const float up = t.at[kUp] == 0 ? 1.0f : t.template ptr<const float>(kUp)[a.up_per_row ? t.t0 : 0];
+    const float up = !t.has(kUp) ? 1.0f : t.template ptr<const float>(kUp)[a.up_per_row ? t.t0 : 0];
     const float origin = stats[0] == -INFINITY ? 0.0f : stats[0];
     const float teach = teacher.sum == 0.0f ? 0.0f : up * (a.teacher_weight * a.temperature), tell = label < 0 ? 0.0f : up * a.label_weight;
     float factor = stats[1] == 0.0f ? 0.0f : teach / stats[1];

@@ -26,17 +26,19 @@ struct RouteArgs {
     int by_logit;              // the scores need not be formed: experts are chosen by their logits
     float scale;
     uint32_t index_mask;       // the bits of a key that tell the expert
-    uint32_t per_k, per_each, per_groups;     // reciprocals, 0 for a divisor of 1
+    uint32_t per_each, per_groups;     // reciprocals, 0 for a divisor of 1
     uint32_t wave_words;       // LDS of a wave
     uint32_t part;             // lanes that look through a group together, a power of two
 };
 
 // Integers that are ordered as the numbers are; NaN above all, both zeros the same.
-__device__ __forceinline__ uint32_t ordered(float x)
+__device__ __forceinline__ float one_nan(float x) { return x != x ? __builtin_nanf("") : x; }
+__device__ __forceinline__ uint32_t ordered_one_nan(float x)      // of a number that is no -0, and NaN without a sign
 {
-    const uint32_t b = __float_as_uint(x + 0.0f);
-    return x != x ? 0xffffffffu : b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
+    const uint32_t b = __float_as_uint(x);
+    return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
 }
+__device__ __forceinline__ uint32_t ordered(float x) { return ordered_one_nan(one_nan(x + 0.0f)); }
 __device__ __forceinline__ float number(uint32_t o) { return __uint_as_float(o ^ (static_cast<int32_t>(o) < 0 ? 0x80000000u : 0xffffffffu)); }
 __device__ __forceinline__ uint64_t ordered(double x)
 {
@@ -45,7 +47,20 @@ __device__ __forceinline__ uint64_t ordered(double x)
 }
 __device__ __forceinline__ double number(uint64_t o) { return __builtin_bit_cast(double, o ^ (static_cast<int64_t>(o) < 0 ? 1ull << 63 : ~0ull)); }
 
+// f(std::integral_constant<int, 0>()), ..., N - 1
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void unrolled_const(const F& f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        unrolled_const<N, I + 1>(f);
+    }
+}
 struct OpMaxU { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); } };
+
+constexpr float kLog2e = 1.44269504088896340736f;
+// To 2 units of its last place and as many as the size of x.
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
 
 // Lanes of a wave wait for what others of it have written to LDS.
 __device__ __forceinline__ void wave_sync()
@@ -128,244 +143,436 @@ __device__ __forceinline__ void choose_in_64(const typename Elem<TYPE>::one* row
     }
 }
 
-// EXACT: 16-bit logits are what experts are chosen by, and a key holds all of one.
-template <int TYPE, int VEC, int L, int NV, bool EXACT>
+// Sorts N keys, the largest first, by a fixed network (odd-even merging of sorted halves, Batcher 1968); what no one asks for afterwards is not computed.
+template <int P, int K, int I, typename T, int N>
+__device__ __forceinline__ void sort_step(T (&v)[N])     // exchanges at distance K on the way to sorted runs of 2 P
+{
+    if constexpr (I + K < N) {
+        if constexpr (I >= K % P && (I - K % P) / K % 2 == 0 && I / (2 * P) == (I + K) / (2 * P)) {
+            const T x = v[I], y = v[I + K];
+            v[I] = max(x, y);
+            v[I + K] = min(x, y);
+        }
+        sort_step<P, K, I + 1>(v);
+    } else if constexpr (K > 1) {
+        sort_step<P, K / 2, 0>(v);
+    } else if constexpr (2 * P < N) {
+        sort_step<2 * P, 2 * P, 0>(v);
+    }
+}
+template <typename T, int N>
+__device__ __forceinline__ void sort_keys(T (&v)[N])
+{
+    if constexpr (N > 1) sort_step<1, 1, 0>(v);
+}
+// The first AHEAD of the keys move up one place where `here` is true.
+template <int AHEAD, int I, typename T, int N>
+__device__ __forceinline__ void move_up(T (&v)[N], bool here, T none)
+{
+    if constexpr (I < AHEAD && I < N) {
+        if constexpr (I + 1 < N) v[I] = here ? v[I + 1] : v[I];
+        else v[I] = here ? none : v[I];
+        move_up<AHEAD, I + 1>(v, here, none);
+    }
+}
+// Takes the largest key of a row's lanes, whose keys are sorted.  AHEAD: how many more will be asked for.
+template <int L, int AHEAD, typename OP, typename T, int N>
+__device__ __forceinline__ T take(T (&key)[N], T none)
+{
+    const T best = static_cast<T>(lanes_reduce<L>(static_cast<uint32_t>(key[0]), OP()));
+    move_up<AHEAD, 0>(key, key[0] == best, none);
+    return best;
+}
+
+// exp(x) for x <= 0: the rounding of x * log2(e) and of log2(e) are made up for.
+__device__ __forceinline__ float exp_below(float x)
+{
+    const float t = x * kLog2e, off = __builtin_fmaf(x, 1.925963033500e-8f, __builtin_fmaf(x, kLog2e, -t)), e = __builtin_amdgcn_exp2f(t);
+    return t < -150.0f ? 0.0f : __builtin_fmaf(e, off * 0.693147180559945f, e);
+}
+// What a choice weighs before sums: most is what softmax is relative to, and for sigmoid at most 0 and not below the largest of the choices' logits or 0.
+__device__ __forceinline__ float weight_of(float x, float most, bool softmax)
+{
+    if (softmax) return exp_below(x - most);
+    const float far = exp_below(-fabsf(x)), s = x <= 0.0f ? exp_below(x - most) : 1.0f;
+    const float w = s / (1.0f + far);
+    return x != x ? x : w;
+}
+// The weights' common factor from their sum.
+__device__ __forceinline__ float weight_factor(const RouteArgs& a, float sum, float inverse)
+{
+    if (a.renormalise) return inverse != inverse ? inverse : sum == 0.0f ? 0.0f : a.scale / sum;
+    return a.score == BAGUA_SCORE_SOFTMAX ? inverse * a.scale : a.scale;
+}
+template <int L>
+__device__ __forceinline__ uint64_t lanes_of_row(int row) { return (L == 64 ? ~0ull : (1ull << (L & 63)) - 1) << (row * L & 63); }
+
+constexpr int kFewChoices = 8;
+
+// The forward pass for 16-bit logits that are themselves what experts are chosen by, and few choices.  A key is then the whole logit and the expert's
+// place in 32 bits.  Every lane sorts the keys of its part of a row, and the row's lanes take the largest of their first ones, one choice after another;
+// a choice stays in the lane that will write it.
+template <int TYPE, int VEC, int L, int NV>
+__global__ void __launch_bounds__(kWave * kRouteWaves)
+k_route_16(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
+{
+    typedef Row<TYPE, VEC, L, NV> R;
+    typedef typename R::one one;
+    constexpr int RW = R::kRows, PER = VEC * NV, MINE = (kFewChoices + L - 1) / L;
+    constexpr int32_t kNone = INT32_MIN;
+    constexpr uint32_t kInf = TYPE == BAGUA_BF16 ? 0x7f80 : 0x7c00;
+    const int lane = threadIdx.x & 63, row = lane / L, in_row = lane % L, experts = a.experts, top_k = a.top_k;
+    const uint32_t tile = blockIdx.x * (blockDim.x / kWave) + static_cast<uint32_t>(wave_index());
+    if (tile >= tiles) return;
+    const ListTile<kRouteLists> t(ls, tile, RW);
+    const uint32_t my_row = min(static_cast<uint32_t>(row), t.rows - 1);
+    R raw;
+    raw.load(t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0 + my_row) * a.ld, experts, true);
+    const bool counts = !t.has(kMask) || t.template ptr<const uint8_t>(kMask)[t.t0 + my_row] != 0, softmax = a.score == BAGUA_SCORE_SOFTMAX;
+    int32_t key[PER];
+    // Sign and magnitude to two's complement, two elements at a time: both zeros are 0 then, and NaN is the largest, if it has no sign.
+    typedef int16_t s2 __attribute__((ext_vector_type(2)));
+    typedef uint16_t u2 __attribute__((ext_vector_type(2)));
+    u2 most_bits = {0, 0};
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < VEC; i += 2) {
+            s2 q = {static_cast<int16_t>(raw.q[j][i]), static_cast<int16_t>(VEC > 1 ? raw.q[j][(i + 1) % VEC] : 0)};
+            const s2 sign = q >> 15, size = q & static_cast<int16_t>(0x7fff);
+            most_bits = __builtin_elementwise_max(most_bits, __builtin_bit_cast(u2, size));
+            const uint32_t both = __builtin_bit_cast(uint32_t, (size ^ sign) - sign), place = static_cast<uint32_t>(experts - R::at(j, experts) - i);
+            key[j * VEC + i] = static_cast<int32_t>(both << 16 | place);
+            if (VEC > 1) key[j * VEC + (i + 1) % VEC] = static_cast<int32_t>((both & 0xffff0000u) | (place - 1));
+        }
+    if (__any(max(most_bits[0], most_bits[1]) > kInf)) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if ((raw.q[j][i] & 0x7fff) > kInf) key[j * VEC + i] = 0x7fff0000 | (key[j * VEC + i] & 0xffff);
+    }
+    if (experts != L * PER) {                                   // the lanes behind a row's last element hold its last ones once more
+#pragma unroll
+        for (int j = NV / 2; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (R::at(j, experts) + i < R::slot(j)) key[j * VEC + i] = kNone;
+    }
+    sort_keys(key);
+    int32_t mine[MINE], first = 0;
+#pragma unroll
+    for (int m = 0; m < MINE; ++m) mine[m] = 0;
+    unrolled_const<kFewChoices>([&](auto j) {
+        constexpr int J = decltype(j)::value;
+        if (J < top_k) {
+            const int32_t best = take<L, kFewChoices - 1 - J, OpMaxI>(key, kNone);
+            if (J == 0) first = best;
+            mine[J / L] = in_row == J % L ? best : mine[J / L];
+        }
+    });
+    auto logit = [](int32_t k) {
+        const int32_t o = k >> 16;
+        return Elem<TYPE>::widen(static_cast<uint16_t>(o < 0 ? 0x8000 | -o : o));
+    };
+    float top = logit(first), inverse = 1.0f;                   // the row's largest, too; NaN if there is one
+    if (softmax && !a.renormalise) {
+        float e[1][NV][VEC], most[1], own[NV][VEC];
+        R::owned(experts, own);
+        most[0] = raw.largest(e[0]);
+        exponentials_of<R>(e, most, TYPE != BAGUA_F16);
+        inverse = R::reciprocal_sum(own, e[0]);
+    }
+    const float most = !softmax ? (a.renormalise ? fminf(top, 0.0f) : 0.0f) : top, from = most == -INFINITY ? INFINITY : most;
+    float w[MINE], sum = 0.0f;
+#pragma unroll
+    for (int m = 0; m < MINE; ++m) {
+        w[m] = weight_of(logit(mine[m]), from, softmax);
+        sum += m * L + in_row < top_k ? w[m] : 0.0f;
+    }
+    const float factor = weight_factor(a, lanes_reduce<L>(sum, OpAddF()), inverse);
+    if (static_cast<uint32_t>(row) >= t.rows) return;
+    const size_t token = t.t0 + static_cast<uint32_t>(row);
+#pragma unroll
+    for (int m = 0; m < MINE; ++m) {
+        const int j = m * L + in_row;
+        if (j >= top_k) continue;
+        const int32_t id = counts ? experts - (mine[m] & 0xffff) : -1;
+        if (a.id_bytes == 8) t.template ptr<int64_t>(kIds)[token * a.ids_ld + j] = id;
+        else t.template ptr<int32_t>(kIds)[token * a.ids_ld + j] = id;
+        t.template ptr<float>(kWeights)[token * a.weights_ld + j] = counts ? w[m] * factor : 0.0f;
+    }
+}
+
+// The forward pass of everything else.  As above, but a key has lost the last bits of its score to the expert's place: some runners-up are taken too, and
+// the candidates put in order by their scores in 32 bits where two keys are close.  FEW: at most kFewChoices.
+template <int TYPE, int VEC, int L, int NV, bool FEW>
 __global__ void __launch_bounds__(kWave * kRouteWaves)
 k_route(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
 {
     typedef Row<TYPE, VEC, L, NV> R;
     typedef typename R::one one;
-    constexpr int RW = R::kRows;
+    constexpr int RW = R::kRows, PER = VEC * NV;
     extern __shared__ uint64_t lds_of_waves[];
-    const int lane = threadIdx.x & 63, wave = wave_index(), row = lane / L, in_row = lane % L, experts = a.experts, top_k = a.top_k;
-    const int slots = EXACT ? top_k : top_k + kMoreChoices;
+    const int lane = threadIdx.x & 63, wave = wave_index(), row = lane / L, in_row = lane % L, experts = a.experts, top_k = a.top_k, slots = top_k + kMoreChoices;
     uint32_t* lds = reinterpret_cast<uint32_t*>(lds_of_waves) + static_cast<uint32_t>(wave) * a.wave_words;
-    uint32_t* keys = lds + row * slots;                                          // the choices, and the runners-up
+    uint32_t* keys = lds + row * slots;                                          // the candidates, as keys and then as experts - id
     float* logits = reinterpret_cast<float*>(lds + RW * slots) + row * slots;    // theirs; at last the weights
-    uint32_t* more = lds + ((2 * RW * slots + 1) & ~1);                          // choice scores for the groups, or the keys of 64 bits
-    const LaneLists<kRouteLists> table(ls);
-    const uint32_t waves = gridDim.x * (blockDim.x / kWave), index_mask = a.index_mask;
-    const bool softmax = a.score == BAGUA_SCORE_SOFTMAX, with_row = !EXACT ? !a.by_logit || (softmax && !a.renormalise) : softmax && !a.renormalise;
-    float own[NV][VEC];
-    R::owned(experts, own);
-
-    for (uint32_t tile = blockIdx.x * (blockDim.x / kWave) + wave; tile < tiles; tile += waves) {
-        const ListTile<kRouteLists> t(table, tile, RW);
-        const uint32_t my_row = min(static_cast<uint32_t>(row), t.rows - 1);
-        const one* x_row = t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0 + my_row) * a.ld;
-        R raw;
-        raw.load(x_row, experts, true);
-        const bool counts = t.at[kMask] == 0 || t.template ptr<const uint8_t>(kMask)[t.t0 + my_row] != 0;
-        float x[NV][VEC], top = -INFINITY, inverse = 1.0f, error = 0.0f;       // error: of a choice score, at most
-        uint32_t key[NV][VEC];
+    uint32_t* more = lds + 2 * RW * slots;                                       // for the groups, the candidates' order, or the keys of 64 bits
+    const uint32_t tile = blockIdx.x * (blockDim.x / kWave) + static_cast<uint32_t>(wave), index_mask = a.index_mask;
+    if (tile >= tiles) return;
+    const ListTile<kRouteLists> t(ls, tile, RW);
+    const bool softmax = a.score == BAGUA_SCORE_SOFTMAX;
+    const uint32_t my_row = min(static_cast<uint32_t>(row), t.rows - 1);
+    const one* x_row = t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0 + my_row) * a.ld;
+    R raw;
+    raw.load(x_row, experts, true);
+    const bool counts = !t.has(kMask) || t.template ptr<const uint8_t>(kMask)[t.t0 + my_row] != 0;
+    float c[PER], top = -INFINITY, inverse = 1.0f, error = 0.0f;                // choice scores; error: of one, at most
+    if (a.by_logit && !(softmax && !a.renormalise)) {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) x[j][i] = Elem<TYPE>::widen(raw.q[j][i]);
-        if (with_row) {
-            float e[1][NV][VEC], most[1];
-            most[0] = top = raw.largest(e[0]);
-            if (softmax) {
-                exponentials_of<R>(e, most, TYPE != BAGUA_F16);
-                inverse = R::reciprocal_sum(own, e[0]);
-                error = inverse * 0x1p-21f;
-            } else {
-                const float low = fminf(top, 0.0f);
-                error = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * low)) * __builtin_fmaf(-low, 0x1p-23f, 0x1p-21f);
-            }
-            if (!EXACT && !a.by_logit) {
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) {
-                        float c = softmax ? e[0][j][i] * inverse : __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * x[j][i]));
-                        if (a.bias) c = c + a.bias[R::at(j, experts) + i];
-                        key[j][i] = ordered(c);
-                    }
-            }
-        }
-        if (EXACT || a.by_logit) {
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) key[j][i] = ordered(x[j][i]);
-        }
-        bool again = false;                                                     // the row needs 64 bits
-        uint32_t allowed = 0xffffffffu;
-        if (a.groups > 1) {
-            uint32_t* score_of = more;
-            float* good = reinterpret_cast<float*>(more + RW * experts);
-            uint32_t* state = more + RW * experts + RW * a.groups;              // of every row: the groups that stay; whether that is not certain
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) score_of[row * experts + R::at(j, experts) + i] = key[j][i];
-            if (in_row == 0) state[row] = 0, state[RW + row] = 0;
-            float* errors = reinterpret_cast<float*>(state + 2 * RW);
-            if (in_row == 0) errors[row] = error;
-            wave_sync();
-            const uint32_t pairs = static_cast<uint32_t>(RW * a.groups), at_once = kWave / a.part, sub = static_cast<uint32_t>(lane) & (a.part - 1);
-            for (uint32_t p0 = 0; p0 < pairs; p0 += at_once) {
-                const uint32_t pair = p0 + static_cast<uint32_t>(lane) / a.part, r = quotient(min(pair, pairs - 1), a.per_groups), g = min(pair, pairs - 1) - r * a.groups;
-                uint32_t first = 0, second = 0;
-                for (uint32_t i = sub; i < static_cast<uint32_t>(a.each); i += a.part) {
-                    const uint32_t v = score_of[r * experts + g * a.each + i];
-                    second = max(second, min(first, v));
-                    first = max(first, v);
-                }
-                for (uint32_t d = 1; d < a.part; d *= 2) {
-                    const uint32_t f = __shfl_xor(first, d), s = __shfl_xor(second, d);
-                    second = max(min(first, f), max(second, s));
-                    first = max(first, f);
-                }
-                if (pair < pairs && sub == 0) good[pair] = a.group_best == 2 ? number(first) + number(second) : number(first);
-            }
-            wave_sync();
-            for (uint32_t pair = lane; pair < pairs; pair += kWave) {
-                const uint32_t r = quotient(pair, a.per_groups), g = pair - r * a.groups;
-                const float mine = good[pair];
-                int before = 0, perhaps = 0;
-                if (EXACT || a.by_logit) {
-                    const uint32_t o = ordered(mine);
-                    for (uint32_t h = 0; h < static_cast<uint32_t>(a.groups); ++h) {
-                        const uint32_t other = ordered(good[r * a.groups + h]);
-                        before += other > o || (other == o && h < g);
-                    }
-                    perhaps = before;
-                } else {
-                    for (uint32_t h = 0; h < static_cast<uint32_t>(a.groups); ++h) {
-                        const float other = good[r * a.groups + h], apart = 4.0f * errors[r] + fmaxf(fabsf(mine), fabsf(other)) * 0x1p-21f;
-                        before += h != g && other > mine + apart;
-                        perhaps += h != g && !(other < mine - apart);
-                    }
-                }
-                if (perhaps < a.top_groups) atomicOr(state + r, 1u << g);
-                else if (before < a.top_groups) atomicOr(state + RW + r, 1u);
-            }
-            wave_sync();
-            allowed = state[row];
-            again = state[RW + row] != 0;
-        }
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const uint32_t e = static_cast<uint32_t>(R::at(j, experts) + i);
-                key[j][i] = (key[j][i] & ~index_mask) | (static_cast<uint32_t>(experts) - e);
-                if (a.groups > 1) key[j][i] = allowed >> quotient(e, a.per_each) & 1u ? key[j][i] : 0u;
-            }
-        // Scores of two keys, the better one first, are too close to tell in 32 bits.
-        auto close = [&](uint32_t better, uint32_t worse) {
-            if (worse == 0) return false;                                       // there is none
-            if (a.by_logit) return (better & ~index_mask) == (worse & ~index_mask);
-            const float b = number(better & ~index_mask), w = number(worse & ~index_mask);
-            return !(b - w > 2.0f * error + fmaxf(fabsf(b), fabsf(w)) * (static_cast<float>(index_mask) * 0x1p-22f + 0x1p-21f));
-        };
-        uint32_t last = 0;
-        int taken = 0;
-        auto take = [&] {
-            uint32_t best = 0;
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) best = max(best, key[j][i]);
-            best = lanes_reduce<L>(best, OpMaxU());
-            float its = 0.0f;
-            bool here = false;
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    const bool is = key[j][i] == best;
-                    key[j][i] = is ? 0u : key[j][i];
-                    if (!EXACT) {
-                        its = is ? x[j][i] : its;
-                        here |= is;
-                    }
-                }
-            if (in_row == 0) keys[taken] = best;
-            if (!EXACT && here) logits[taken] = its;
-            ++taken;
-            return best;
-        };
-        for (int j = 0; j < top_k; ++j) last = take();
-        if (!EXACT) {
-            for (int j = 0; j < kMoreChoices; ++j) {
-                const uint32_t next = take();
-                if (!__any(close(last, next))) break;
-            }
-        }
-        wave_sync();
-        if (!EXACT) {
-            auto same = [&](int j) {      // not only close: the same logit with the same bias, which the expert's place decides
-                if (logits[j] != logits[j + 1]) return false;
-                return !a.bias || a.bias[experts - (keys[j] & index_mask)] == a.bias[experts - (keys[j + 1] & index_mask)];
-            };
-            for (int j = in_row; j + 1 < top_k; j += L) again |= close(keys[j], keys[j + 1]) && !same(j);
-            bool ends = false;
-            for (int j = top_k - 1; j + 1 < taken; ++j) {
-                if (ends) break;
-                if (!close(keys[j], keys[j + 1])) ends = true;
-                else if (!same(j)) break;
-            }
-            again = (again || !ends) && counts && static_cast<uint32_t>(row) < t.rows;
-            const uint64_t rows_again = __ballot(again);
-            for (uint64_t left = rows_again; left != 0;) {
-                const int r = (__ffsll(static_cast<unsigned long long>(left)) - 1) / L;
-                const uint64_t of_row = (L == 64 ? ~0ull : (1ull << (L & 63)) - 1) << (r * L & 63);
-                left &= ~of_row;
-                choose_in_64<TYPE>(t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0 + static_cast<uint32_t>(r)) * a.ld, a,
-                                   reinterpret_cast<uint64_t*>(more), lds + r * slots, reinterpret_cast<float*>(lds + RW * slots) + r * slots);
-            }
-            wave_sync();
-        }
-        // The weights, formed of the chosen logits.
-        auto logit = [&](int j) {      // (16-bit numbers as fp32 ones have zeros in a key's last bits, turned to ones below 0)
-            const uint32_t o = keys[j] & ~index_mask;
-            return EXACT ? number(static_cast<int32_t>(o) < 0 ? o : o | index_mask) : logits[j];
-        };
-        float most = -INFINITY;
-        if (a.renormalise) {
-            for (int j = in_row; j < top_k; j += L) most = fmaxf(most, logit(j));
-            most = lanes_most<L>(most);
-            if (!softmax) most = fminf(most, 0.0f);
+            for (int i = 0; i < VEC; ++i) c[j * VEC + i] = Elem<TYPE>::widen(raw.q[j][i]) + 0.0f;
+    } else {
+        float e[1][NV][VEC], most[1];
+        most[0] = top = raw.largest(e[0]);
+        if (softmax) {
+            float own[NV][VEC];
+            R::owned(experts, own);
+            exponentials_of<R>(e, most, TYPE != BAGUA_F16);
+            inverse = R::reciprocal_sum(own, e[0]);
+            error = inverse * 0x1p-21f;
         } else {
-            most = softmax ? top : 0.0f;
+            const float low = fminf(top, 0.0f);
+            error = sigmoid(low) * __builtin_fmaf(-low, 0x1p-23f, 0x1p-21f);
         }
-        if (most == -INFINITY) most = INFINITY;                                 // nothing but -infinity: weights of 0
-        float sum = 0.0f;
-        for (int j = in_row; j < top_k; j += L) {
-            const float v = logit(j), s = expf((softmax || v <= 0.0f ? v : 0.0f) - most);
-            float w = softmax ? s : s / (1.0f + expf(v <= 0.0f ? v : -v));
-            if (v != v) w = v;
-            sum += w;
-            logits[j] = w;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float bias[VEC] = {};
+            if (a.bias) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) bias[i] = a.bias[R::at(j, experts) + i];
+            }
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                c[j * VEC + i] = a.by_logit ? Elem<TYPE>::widen(raw.q[j][i]) + 0.0f : (softmax ? e[0][j][i] * inverse : sigmoid(e[0][j][i])) + bias[i];
         }
-        float factor = a.scale;
-        if (a.renormalise) {
-            sum = lanes_reduce<L>(sum, OpAddF());
-            factor = sum == 0.0f ? 0.0f : a.scale / sum;
-            if (inverse != inverse) factor = inverse;
-        } else if (softmax) {
-            factor = inverse * a.scale;
-        }
-        for (int j = in_row; j < top_k; j += L) {
-            const float w = logits[j];
-            logits[j] = counts ? w * factor : 0.0f;
-            keys[j] = counts ? static_cast<uint32_t>(experts) - (keys[j] & index_mask) : 0xffffffffu;
+    }
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < PER; i += 2) nan |= __builtin_isunordered(c[i], c[(i + 1) % PER]);
+    if (__any(nan)) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c[i] = one_nan(c[i]);
+    }
+    uint32_t key[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) key[i] = ordered_one_nan(c[i]);
+    bool again = false;                                                         // the row needs 64 bits
+    uint32_t allowed = 0xffffffffu;
+    if (a.groups > 1) {
+        uint32_t* score_of = more;
+        float* good = reinterpret_cast<float*>(more + RW * experts);
+        uint32_t* state = more + RW * experts + RW * a.groups;                  // of every row: the groups that stay; whether that is not certain
+        float* errors = reinterpret_cast<float*>(state + 2 * RW);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) score_of[row * experts + R::at(j, experts) + i] = key[j * VEC + i];
+        if (in_row == 0) state[row] = 0, state[RW + row] = 0, errors[row] = error;
+        wave_sync();
+        const uint32_t pairs = static_cast<uint32_t>(RW * a.groups), at_once = kWave / a.part, sub = static_cast<uint32_t>(lane) & (a.part - 1);
+        for (uint32_t p0 = 0; p0 < pairs; p0 += at_once) {
+            const uint32_t pair = p0 + static_cast<uint32_t>(lane) / a.part, r = quotient(min(pair, pairs - 1), a.per_groups), g = min(pair, pairs - 1) - r * a.groups;
+            uint32_t first = 0, second = 0;
+#pragma unroll 8
+            for (uint32_t i = sub; i < static_cast<uint32_t>(a.each); i += a.part) {
+                const uint32_t v = score_of[r * experts + g * a.each + i];
+                second = max(second, min(first, v));
+                first = max(first, v);
+            }
+            for (uint32_t d = 1; d < a.part; d *= 2) {
+                const uint32_t f = __shfl_xor(first, d), s = __shfl_xor(second, d);
+                second = max(min(first, f), max(second, s));
+                first = max(first, f);
+            }
+            if (pair < pairs && sub == 0) good[pair] = a.group_best == 2 ? number(first) + number(second) : number(first);
         }
         wave_sync();
-        const uint32_t items = t.rows * static_cast<uint32_t>(top_k);
-        float* weights = t.template ptr<float>(kWeights);
-        for (uint32_t i = static_cast<uint32_t>(lane); i < items; i += kWave) {
-            const uint32_t r = quotient(i, a.per_k), j = i - r * top_k;
-            const size_t token = t.t0 + r;
-            const int32_t id = static_cast<int32_t>(lds[r * slots + j]);
-            if (a.id_bytes == 8) t.template ptr<int64_t>(kIds)[token * a.ids_ld + j] = id;
-            else t.template ptr<int32_t>(kIds)[token * a.ids_ld + j] = id;
-            weights[token * a.weights_ld + j] = reinterpret_cast<const float*>(lds)[RW * slots + r * slots + j];
+        for (uint32_t pair = lane; pair < pairs; pair += kWave) {
+            const uint32_t r = quotient(pair, a.per_groups), g = pair - r * a.groups;
+            const float mine = good[pair];
+            int before = 0, perhaps = 0;
+            if (a.by_logit) {
+                const uint32_t o = ordered(mine);
+                for (uint32_t h = 0; h < static_cast<uint32_t>(a.groups); ++h) {
+                    const uint32_t other = ordered(good[r * a.groups + h]);
+                    before += other > o || (other == o && h < g);
+                }
+                perhaps = before;
+            } else {
+                // (a group as close as that is of nearly this size)
+                const float apart = __builtin_fmaf(fabsf(mine), 0x1p-20f, 4.0f * errors[r]), above = mine + apart, below = mine - apart;
+                perhaps = -1;                                                   // itself
+#pragma unroll 8
+                for (uint32_t h = 0; h < static_cast<uint32_t>(a.groups); ++h) {
+                    const float other = good[r * a.groups + h];
+                    before += other > above;
+                    perhaps += !(other < below);
+                }
+            }
+            if (perhaps < a.top_groups) atomicOr(state + r, 1u << g);
+            else if (before < a.top_groups) atomicOr(state + RW + r, 1u);
         }
         wave_sync();
+        allowed = state[row];
+        again = state[RW + row] != 0;
+        wave_sync();
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int at = R::at(j, experts);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) key[j * VEC + i] = (key[j * VEC + i] & ~index_mask) | static_cast<uint32_t>(experts - at - i);
+        if (a.groups > 1) {
+            if (a.each % VEC == 0 && experts % VEC == 0) {                      // a vector is of one group
+                const uint32_t stays = 0u - (allowed >> quotient(static_cast<uint32_t>(at), a.per_each) & 1u);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) key[j * VEC + i] &= stays;
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) key[j * VEC + i] &= 0u - (allowed >> quotient(static_cast<uint32_t>(at + i), a.per_each) & 1u);
+            }
+        }
+    }
+    if (experts != L * PER) {                                                   // the lanes behind a row's last element hold its last ones once more
+#pragma unroll
+        for (int j = NV / 2; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (R::at(j, experts) + i < R::slot(j)) key[j * VEC + i] = 0;
+    }
+    sort_keys(key);
+    // Scores of two keys, the better one first, cannot be told apart by the keys.
+    auto close = [&](uint32_t better, uint32_t worse) {
+        if (worse == 0) return false;                                           // there is none
+        if (a.by_logit) return (better & ~index_mask) == (worse & ~index_mask);
+        const float b = number(better & ~index_mask), w = number(worse & ~index_mask);
+        return !(b - w > __builtin_fmaf(fmaxf(fabsf(b), fabsf(w)), __builtin_fmaf(static_cast<float>(index_mask), 0x1p-22f, 0x1p-21f), 2.0f * error));
+    };
+    uint32_t last = 0;
+    int taken = top_k;
+    if (FEW) {
+        unrolled_const<kFewChoices>([&](auto j) {
+            constexpr int J = decltype(j)::value;
+            if (J < top_k) {
+                last = take<L, kFewChoices - 1 - J + kMoreChoices, OpMaxU>(key, 0u);
+                if (in_row == 0) keys[J] = last;
+            }
+        });
+    } else {
+        for (int j = 0; j < top_k; ++j) {
+            last = take<L, PER, OpMaxU>(key, 0u);
+            if (in_row == 0) keys[j] = last;
+        }
+    }
+    // Runners-up, until one is so far behind that what the keys left out cannot matter.
+    bool ends = false;
+    for (int j = 0; j < kMoreChoices; ++j) {
+        const uint32_t next = take<L, PER, OpMaxU>(key, 0u);
+        if (in_row == 0) keys[taken] = next;
+        ++taken;
+        ends = ends || !close(last, next);
+        if (__all(ends)) break;
+    }
+    again = again || !ends;
+    wave_sync();
+    bool order = false;
+    for (int j = in_row; j < taken; j += L) {
+        const uint32_t k = keys[j];
+        order |= j + 1 < taken && close(k, keys[j + 1]);
+        logits[j] = k != 0 ? Elem<TYPE>::widen(x_row[static_cast<uint32_t>(experts) - (k & index_mask)]) : 0.0f;
+    }
+    wave_sync();
+    for (int j = in_row; j < taken; j += L) keys[j] &= index_mask;
+    wave_sync();
+    if (__any(order)) {
+        // By the scores themselves, each candidate by how many are before it.  (Into another place: what a row's lanes have not come to is not moved.)
+        float* score_of = reinterpret_cast<float*>(more) + row * slots;
+        uint32_t *new_keys = more + RW * slots + row * slots, *new_logits = more + 2 * RW * slots + row * slots;
+        const float shift = -(top == -INFINITY ? 0.0f : top);
+        for (int j = in_row; j < taken; j += L) {
+            const uint32_t k = keys[j];
+            const float x = logits[j];
+            float s = x;
+            if (!a.by_logit) {
+                s = softmax ? __builtin_amdgcn_exp2f((x + shift) * kLog2e) * inverse : sigmoid(x);
+                if (a.bias && k != 0) s = s + a.bias[static_cast<uint32_t>(experts) - k];
+            }
+            score_of[j] = s;
+        }
+        wave_sync();
+        for (int j = in_row; j < taken; j += L) {
+            const uint32_t mine = keys[j];
+            if (mine == 0) continue;
+            const float x = logits[j], s = score_of[j];
+            const uint32_t o = ordered(s);
+            int before = 0;
+            bool near = false;
+            for (int i = 0; i < taken; ++i) {
+                const uint32_t other = keys[i];
+                if (other == 0) break;
+                const float d = score_of[i];
+                const uint32_t p = ordered(d);
+                before += p > o || (p == o && other > mine);
+                // too close to tell in 32 bits, and not the same logit with the same bias, which the expert's place decides
+                if (!a.by_logit && i != j && !(fabsf(s - d) > __builtin_fmaf(fmaxf(fabsf(s), fabsf(d)), 0x1p-22f, 2.0f * error)) &&
+                    !(logits[i] == x && (!a.bias || a.bias[static_cast<uint32_t>(experts) - mine] == a.bias[static_cast<uint32_t>(experts) - other])))
+                    near = true;
+            }
+            again |= near && before < top_k;
+            new_keys[before] = mine;
+            new_logits[before] = __float_as_uint(x);
+        }
+        wave_sync();
+        for (int j = in_row; j < top_k; j += L) {
+            keys[j] = new_keys[j];
+            logits[j] = __uint_as_float(new_logits[j]);
+        }
+        wave_sync();
+    }
+    again = again && counts && static_cast<uint32_t>(row) < t.rows;
+    for (uint64_t left = __ballot(again); left != 0;) {
+        const int r = (__ffsll(static_cast<unsigned long long>(left)) - 1) / L;
+        left &= ~lanes_of_row<L>(r);
+        choose_in_64<TYPE>(t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0 + static_cast<uint32_t>(r)) * a.ld, a, reinterpret_cast<uint64_t*>(more),
+                           lds + r * slots, reinterpret_cast<float*>(lds + RW * slots) + r * slots);
+    }
+    wave_sync();
+    // The weights, formed of the chosen logits.
+    float most = softmax ? top : 0.0f;
+    if (a.renormalise) {
+        most = -INFINITY;
+        for (int j = in_row; j < top_k; j += L) most = fmaxf(most, logits[j]);
+        most = lanes_most<L>(most);
+        if (!softmax) most = fminf(most, 0.0f);
+    }
+    if (most == -INFINITY) most = INFINITY;                                     // nothing but -infinity: weights of 0
+    float sum = 0.0f;
+    for (int j = in_row; j < top_k; j += L) {
+        const float w = weight_of(logits[j], most, softmax);
+        sum += w;
+        logits[j] = w;
+    }
+    const float factor = weight_factor(a, lanes_reduce<L>(sum, OpAddF()), inverse);
+    if (static_cast<uint32_t>(row) >= t.rows) return;
+    const size_t token = t.t0 + static_cast<uint32_t>(row);
+    for (int j = in_row; j < top_k; j += L) {
+        const int32_t id = counts ? experts - static_cast<int32_t>(keys[j]) : -1;
+        if (a.id_bytes == 8) t.template ptr<int64_t>(kIds)[token * a.ids_ld + j] = id;
+        else t.template ptr<int32_t>(kIds)[token * a.ids_ld + j] = id;
+        t.template ptr<float>(kWeights)[token * a.weights_ld + j] = counts ? logits[j] * factor : 0.0f;
     }
 }
 
@@ -391,14 +598,13 @@ k_route_grad(Lists<kRouteGradLists> ls, RouteGradArgs a, uint32_t tiles)
     extern __shared__ uint64_t lds_of_waves[];
     const int lane = threadIdx.x & 63, wave = wave_index(), row = lane / L, in_row = lane % L, experts = a.experts, top_k = a.top_k;
     float* spread = reinterpret_cast<float*>(lds_of_waves) + static_cast<uint32_t>(wave) * a.wave_words + row * experts;
-    const LaneLists<kRouteGradLists> table(ls);
     const uint32_t waves = gridDim.x * (blockDim.x / kWave);
     float own[NV][VEC];
     R::owned(experts, own);
     for (int e = in_row; e < experts; e += L) spread[e] = 0.0f;
     wave_sync();
     for (uint32_t tile = blockIdx.x * (blockDim.x / kWave) + wave; tile < tiles; tile += waves) {
-        const ListTile<kRouteGradLists> t(table, tile, RW);
+        const ListTile<kRouteGradLists> t(ls, tile, RW);
         const bool there = static_cast<uint32_t>(row) < t.rows;
         const size_t token = t.t0 + min(static_cast<uint32_t>(row), t.rows - 1);
         const one* x_row = t.template ptr<const one>(kGradLogits) + token * a.ld;
@@ -523,6 +729,40 @@ k_route_grad(Lists<kRouteGradLists> ls, RouteGradArgs a, uint32_t tiles)
 
 inline uint32_t reciprocal_of(int d) { return d == 1 ? 0 : static_cast<uint32_t>((0x100000000ull + static_cast<uint64_t>(d) - 1) / static_cast<uint64_t>(d)); }
 
+// Calls f with the layout of a row of `experts` logits: as many lanes as leave each some 16 of them, so that a choice, an exchange over the row's
+// lanes, is one for many rows.
+template <int VEC_, int L_, int NV_>
+struct RouteLayout {
+    static constexpr int VEC = VEC_, L = L_, NV = NV_;
+};
+template <int V, typename F>
+inline void with_lanes(int experts, const F& f)
+{
+    constexpr int N = 16 / V;                            // vectors of a lane
+    if (experts < V) {
+        if (experts <= 1) f(RouteLayout<1, 1, 1>());
+        else if (experts <= 2) f(RouteLayout<1, 2, 1>());
+        else if (experts <= 4) f(RouteLayout<1, 4, 1>());
+        else f(RouteLayout<1, 8, 1>());
+    } else if (experts <= V) f(RouteLayout<V, 1, 1>());
+    else if (experts <= 8 && V == 4) f(RouteLayout<V, 1, 2>());
+    else if (experts <= 16) f(RouteLayout<V, 1, N>());
+    else if (experts <= 32) f(RouteLayout<V, 2, N>());
+    else if (experts <= 64) f(RouteLayout<V, 4, N>());
+    else if (experts <= 128) f(RouteLayout<V, 8, N>());
+    else if (experts <= 256) f(RouteLayout<V, 16, N>());
+    else if (experts <= 512) f(RouteLayout<V, 32, N>());
+    else if (experts <= 1024) f(RouteLayout<V, 64, N>());
+    else f(RouteLayout<V, 64, 2 * N>());
+}
+template <typename F>
+inline void with_route_layout(int dtype, int experts, const F& f)
+{
+    if (dtype == BAGUA_F32) with_lanes<4>(experts, [&](auto layout) { f(layout, std::integral_constant<int, BAGUA_F32>()); });
+    else if (dtype == BAGUA_BF16) with_lanes<8>(experts, [&](auto layout) { f(layout, std::integral_constant<int, BAGUA_BF16>()); });
+    else with_lanes<8>(experts, [&](auto layout) { f(layout, std::integral_constant<int, BAGUA_F16>()); });
+}
+
 // Waves of a workgroup whose LDS fits, and the grid.
 inline int route_waves(size_t wave_bytes)
 {
@@ -586,10 +826,9 @@ extern "C" int bagua_route(int dtype, const void* const* logits, size_t ld, cons
     int bits = 1;
     while (1 << bits <= experts) ++bits;
     a.index_mask = (1u << bits) - 1;
-    a.per_k = reciprocal_of(top_k), a.per_each = reciprocal_of(a.each), a.per_groups = reciprocal_of(groups);
-    const bool exact = a.by_logit && dtype != BAGUA_F32;
+    a.per_each = reciprocal_of(a.each), a.per_groups = reciprocal_of(groups);
     int status = BAGUA_OK;
-    with_layout<false>(dtype, experts, [&](auto layout, auto type) {
+    with_route_layout(dtype, experts, [&](auto layout, auto type) {
         typedef decltype(layout) Lay;
         constexpr int TYPE = decltype(type)::value;
         constexpr uint32_t RW = kWave / Lay::L;
@@ -601,20 +840,23 @@ extern "C" int bagua_route(int dtype, const void* const* logits, size_t ld, cons
         if (tiles == 0) return;
         a.part = 1;
         while (a.part < 16 && 2 * a.part * RW * static_cast<uint32_t>(groups) <= kWave && 2 * a.part <= static_cast<uint32_t>(a.each)) a.part *= 2;
-        const uint32_t chosen = (2 * RW * static_cast<uint32_t>(top_k + (exact ? 0 : kMoreChoices)) + 1) & ~1u;
-        const uint32_t for_groups = groups > 1 ? RW * (static_cast<uint32_t>(experts) + static_cast<uint32_t>(groups) + 3) : 0, for_64 = exact ? 0 : 2 * static_cast<uint32_t>(experts);
-        a.wave_words = (chosen + std::max(for_groups, for_64) + 1) & ~1u;
-        const size_t wave_bytes = a.wave_words * sizeof(uint32_t);
-        const int waves = route_waves(wave_bytes);
-        const dim3 grid = route_grid(tiles, waves), block(static_cast<uint32_t>(kWave * waves));
-        auto launch = [&](auto kernel) {
-            launch_kernel(kernel, grid, block, wave_bytes * static_cast<size_t>(waves), static_cast<hipStream_t>(stream), ls, a, static_cast<uint32_t>(tiles));
+        auto launch = [&](auto kernel, size_t wave_bytes) {
+            const int waves = route_waves(wave_bytes);
+            launch_kernel(kernel, dim3(static_cast<uint32_t>((tiles + static_cast<uint64_t>(waves) - 1) / static_cast<uint64_t>(waves))), dim3(static_cast<uint32_t>(kWave * waves)),
+                          wave_bytes * static_cast<size_t>(waves), static_cast<hipStream_t>(stream), ls, a, static_cast<uint32_t>(tiles));
+            status = launch_status();
         };
         if constexpr (TYPE != BAGUA_F32) {
-            if (exact) launch(k_route<TYPE, Lay::VEC, Lay::L, Lay::NV, true>);
+            if (a.by_logit && groups == 1 && top_k <= kFewChoices) {
+                launch(k_route_16<TYPE, Lay::VEC, Lay::L, Lay::NV>, 0);
+                return;
+            }
         }
-        if (!exact) launch(k_route<TYPE, Lay::VEC, Lay::L, Lay::NV, false>);
-        status = launch_status();
+        const uint32_t slots = RW * static_cast<uint32_t>(top_k + kMoreChoices), columns = static_cast<uint32_t>(experts);
+        const uint32_t for_groups = groups > 1 ? RW * (columns + static_cast<uint32_t>(groups) + 3) : 0;
+        a.wave_words = (2 * slots + std::max({for_groups, 2 * columns, 3 * slots}) + 1) & ~1u;
+        if (top_k <= kFewChoices) launch(k_route<TYPE, Lay::VEC, Lay::L, Lay::NV, true>, a.wave_words * sizeof(uint32_t));
+        else if constexpr (Lay::VEC * Lay::NV * Lay::L > kFewChoices) launch(k_route<TYPE, Lay::VEC, Lay::L, Lay::NV, false>, a.wave_words * sizeof(uint32_t));
     });
     return status;
 }
