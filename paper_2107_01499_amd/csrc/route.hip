@@ -14,7 +14,6 @@
 namespace bagua {
 
 constexpr int kRouteWaves = 4;
-constexpr uint32_t kRouteMostWaves = 65536;   // of a launch
 constexpr int kMoreChoices = 4;               // rounds beyond the last choice that look for the end of a run of equal scores
 
 enum { kLogits = 0, kMask, kIds, kWeights, kRouteLists };
@@ -584,146 +583,146 @@ struct RouteGradArgs {
     int experts, top_k, score, renormalise, id_bytes;
     float scale;
     uint32_t wave_words;
+    int row_held;              // elements of a row in LDS: a multiple of a vector
 };
 
-// A row's choices are spread over a row of fp32 numbers in LDS, which is zero before and after, and read from there as it is written to memory.
-// FULL: softmax that was not renormalised, whose gradient reaches every logit; elsewhere the chosen ones alone.
+// One gradient of a weight goes to one logit, but where the scores are a whole row's softmax: a row's choices are written to a row in LDS that is zero
+// elsewhere, and it is read from there as it goes to memory.  FULL: softmax that was not renormalised, whose gradient reaches every logit; the row in
+// LDS then holds the weights' gradients, in fp32, elsewhere the logits' as they will be stored.
 template <int TYPE, int VEC, int L, int NV, bool FULL>
 __global__ void __launch_bounds__(kWave * kRouteWaves)
 k_route_grad(Lists<kRouteGradLists> ls, RouteGradArgs a, uint32_t tiles)
 {
     typedef Row<TYPE, VEC, L, NV> R;
     typedef typename R::one one;
+    typedef std::conditional_t<FULL, float, one> held;
+    typedef held held_vector __attribute__((ext_vector_type(VEC), aligned(sizeof(held) * VEC < 16 ? sizeof(held) * VEC : 16)));
     constexpr int RW = R::kRows;
     extern __shared__ uint64_t lds_of_waves[];
     const int lane = threadIdx.x & 63, wave = wave_index(), row = lane / L, in_row = lane % L, experts = a.experts, top_k = a.top_k;
-    float* spread = reinterpret_cast<float*>(lds_of_waves) + static_cast<uint32_t>(wave) * a.wave_words + row * experts;
-    const uint32_t waves = gridDim.x * (blockDim.x / kWave);
-    float own[NV][VEC];
-    R::owned(experts, own);
-    for (int e = in_row; e < experts; e += L) spread[e] = 0.0f;
-    wave_sync();
-    for (uint32_t tile = blockIdx.x * (blockDim.x / kWave) + wave; tile < tiles; tile += waves) {
-        const ListTile<kRouteGradLists> t(ls, tile, RW);
-        const bool there = static_cast<uint32_t>(row) < t.rows;
-        const size_t token = t.t0 + min(static_cast<uint32_t>(row), t.rows - 1);
-        const one* x_row = t.template ptr<const one>(kGradLogits) + token * a.ld;
-        R raw;
-        if (FULL) raw.load(x_row, experts, true);
-        auto id = [&](int j) {
-            const int64_t v = a.id_bytes == 8 ? t.template ptr<const int64_t>(kGradIds)[token * a.ids_ld + j]
-                                              : static_cast<int64_t>(t.template ptr<const int32_t>(kGradIds)[token * a.ids_ld + j]);
-            return static_cast<uint64_t>(v) < static_cast<uint64_t>(experts) ? static_cast<int>(v) : -1;
-        };
-        auto up = [&](int j) { return t.template ptr<const float>(kGradUp)[token * a.up_ld + j]; };
-        const bool shares = !FULL && a.renormalise, softmax = FULL || a.score == BAGUA_SCORE_SOFTMAX;
-        // a choice's part of the sum that the weights were divided by, and their mean gradient
-        const float* weights = t.template ptr<const float>(kGradWeights);
-        float most = -INFINITY, sum = 0.0f, mean = 0.0f;
-        bool any = false;
-        auto share = [&](int j, int e) {
-            if (softmax) return weights[token * a.weights_ld + j] / a.scale;
-            const float v = Elem<TYPE>::widen(x_row[e]);
-            return expf((v <= 0.0f ? v : 0.0f) - most) / (1.0f + expf(v <= 0.0f ? v : -v));
-        };
-        if (shares && !softmax) {
-            for (int j = in_row; j < top_k; j += L) {
-                const int e = id(j);
-                if (e >= 0) most = fmaxf(most, Elem<TYPE>::widen(x_row[e]));
-            }
+    const uint32_t tile = blockIdx.x * (blockDim.x / kWave) + static_cast<uint32_t>(wave);
+    if (tile >= tiles) return;
+    const ListTile<kRouteGradLists> t(ls, tile, RW);
+    const bool there = static_cast<uint32_t>(row) < t.rows, shares = !FULL && a.renormalise, softmax = FULL || a.score == BAGUA_SCORE_SOFTMAX;
+    const size_t token = t.t0 + min(static_cast<uint32_t>(row), t.rows - 1);
+    const one* x_row = shares && softmax ? nullptr : t.template ptr<const one>(kGradLogits) + token * a.ld;
+    R raw;
+    if (FULL) raw.load(x_row, experts, true);
+    // Choice j of the lane's row: the expert, or -1; the gradient of its weight; its weight, or its logit.
+    struct Choice {
+        int expert;
+        float up, value;
+    };
+    auto load = [&](int j) {
+        Choice c;
+        const size_t at = token * a.ids_ld + static_cast<size_t>(j);
+        const uint64_t id = a.id_bytes == 8 ? t.template ptr<const uint64_t>(kGradIds)[at] : static_cast<uint64_t>(static_cast<int64_t>(t.template ptr<const int32_t>(kGradIds)[at]));
+        c.expert = there && id < static_cast<uint64_t>(experts) ? static_cast<int>(id) : -1;
+        c.up = t.template ptr<const float>(kGradUp)[token * a.up_ld + static_cast<size_t>(j)];
+        c.value = 0.0f;
+        if (shares && softmax) c.value = t.template ptr<const float>(kGradWeights)[token * a.weights_ld + static_cast<size_t>(j)];
+        else if (!FULL && c.expert >= 0) c.value = Elem<TYPE>::widen(x_row[c.expert]);
+        return c;
+    };
+    // The lane's choices: the first one is kept, and read once.
+    Choice own_choice{-1, 0.0f, 0.0f};
+    if (in_row < top_k) own_choice = load(in_row);
+    auto choices = [&](auto&& f) {
+        if (own_choice.expert >= 0) f(in_row, own_choice);
+        for (int j = in_row + L; j < top_k; j += L) {
+            const Choice c = load(j);
+            if (c.expert >= 0) f(j, c);
+        }
+    };
+    held* spread = reinterpret_cast<held*>(reinterpret_cast<uint32_t*>(lds_of_waves) + static_cast<uint32_t>(wave) * a.wave_words) + row * a.row_held;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (R::slot(j) < a.row_held) *reinterpret_cast<held_vector*>(spread + R::slot(j)) = held_vector(0);
+    // a choice's part of the sum that the weights were divided by, and the mean gradient of the weights
+    float most = -INFINITY, sum = 0.0f, mean = 0.0f;
+    bool any = false;
+    if (shares) {
+        if (!softmax) {
+            choices([&](int, const Choice& c) { most = fmaxf(most, c.value); });
             most = fminf(lanes_most<L>(most), 0.0f);
             if (most == -INFINITY) most = INFINITY;
         }
-        for (int j = in_row; j < top_k; j += L) {
-            const int e = id(j);
-            any |= e >= 0;
-            if (shares && e >= 0) {
-                const float r = share(j, e);
-                sum += r;
-                mean = __builtin_fmaf(r, up(j), mean);
+    }
+    const float per_scale = 1.0f / a.scale;
+    auto share = [&](const Choice& c) { return softmax ? c.value * per_scale : weight_of(c.value, most, false); };
+    if (shares) {
+        choices([&](int, const Choice& c) {
+            const float r = share(c);
+            sum += r;
+            mean = __builtin_fmaf(r, c.up, mean);
+        });
+        sum = softmax ? 1.0f : lanes_reduce<L>(sum, OpAddF());
+        mean = lanes_reduce<L>(mean, OpAddF());
+        mean = sum == 0.0f ? 0.0f : mean / sum;
+    } else if (FULL) {
+        choices([&](int, const Choice&) { any = true; });
+    }
+    // what a choice adds to its logit, in FULL to its score
+    auto part = [&](const Choice& c) {
+        if (FULL) return c.up;
+        if (shares && softmax) return c.value * (c.up - mean);
+        const float far = exp_below(-fabsf(c.value)), q = 1.0f / (1.0f + far);     // 1 - sigmoid is 1 / (1 + exp(x))
+        if (!shares) return a.scale * c.up * (far * q * q);
+        const float rest = c.value <= 0.0f ? q : far * q;
+        return sum == 0.0f ? 0.0f : a.scale * (share(c) / sum) * (c.up - mean) * rest;
+    };
+    // An expert that a row names twice gets both.  The rows that have one are found by writing the choices' places first.
+    wave_sync();
+    auto place = [](int j) { return FULL ? __builtin_bit_cast(held, static_cast<std::conditional_t<FULL || TYPE == BAGUA_F32, uint32_t, uint16_t>>(j)) : held(j); };
+    choices([&](int j, const Choice& c) { spread[c.expert] = place(j); });
+    wave_sync();
+    bool twice = false;
+    choices([&](int j, const Choice& c) { twice |= spread[c.expert] != place(j); });
+    wave_sync();
+    auto narrow = [](float v) {
+        if constexpr (FULL) return v;
+        else return Elem<TYPE>::narrow(v);
+    };
+    if (!__any(twice)) {
+        choices([&](int, const Choice& c) { spread[c.expert] = narrow(part(c)); });
+    } else {
+        choices([&](int, const Choice& c) {
+            float all = 0.0f;
+            for (int i = 0; i < top_k; ++i) {
+                const Choice d = load(i);
+                if (d.expert == c.expert) all += part(d);
             }
-        }
-        if (shares) {
-            sum = softmax ? 1.0f : lanes_reduce<L>(sum, OpAddF());
-            mean = lanes_reduce<L>(mean, OpAddF());
-            mean = sum == 0.0f ? 0.0f : mean / sum;
-        }
-        // what a choice adds to its logit
-        auto part = [&](int j, int e) {
-            if (FULL) return up(j);
-            if (shares) {
-                const float r = sum == 0.0f ? 0.0f : share(j, e) / sum, d = a.scale * r * (up(j) - mean);
-                if (softmax) return d;
-                const float v = Elem<TYPE>::widen(x_row[e]), far = expf(v <= 0.0f ? v : -v);
-                return d * ((v <= 0.0f ? 1.0f : far) / (1.0f + far));
-            }
-            const float v = Elem<TYPE>::widen(x_row[e]), far = expf(v <= 0.0f ? v : -v);
-            return a.scale * up(j) * (far / ((1.0f + far) * (1.0f + far)));
-        };
-        // An expert that a row names twice gets both, one after the other in every call; the rows that have one are found by writing the
-        // choices' places first.
-        bool twice = false;
-        for (int j = in_row; j < top_k && there; j += L) {
-            const int e = id(j);
-            if (e >= 0) reinterpret_cast<uint32_t*>(spread)[e] = static_cast<uint32_t>(j);
-        }
-        wave_sync();
-        for (int j = in_row; j < top_k && there; j += L) {
-            const int e = id(j);
-            twice |= e >= 0 && reinterpret_cast<uint32_t*>(spread)[e] != static_cast<uint32_t>(j);
-        }
-        wave_sync();
-        if (!__any(twice)) {
-            for (int j = in_row; j < top_k && there; j += L) {
-                const int e = id(j);
-                if (e >= 0) spread[e] = part(j, e);
-            }
-        } else {
-            for (int j = in_row; j < top_k && there; j += L) {
-                const int e = id(j);
-                if (e >= 0) spread[e] = 0.0f;
-            }
-            wave_sync();
-            for (int j = 0; j < top_k; ++j) {
-                const int e = there && j % L == in_row ? id(j) : -1;
-                if (e >= 0) spread[e] += part(j, e);
-                wave_sync();
-            }
-        }
-        wave_sync();
-        float e[1][NV][VEC], factor = 0.0f, shift = 0.0f, most_of[1];
-        if (FULL) {
-            float dot = 0.0f;
-            most_of[0] = raw.largest(e[0]);
-            exponentials_of<R>(e, most_of, TYPE != BAGUA_F16);
-            const float inverse = R::reciprocal_sum(own, e[0]);
+            spread[c.expert] = narrow(all);
+        });
+    }
+    wave_sync();
+    float e[1][NV][VEC], factor = 0.0f, shift = 0.0f, most_of[1], own[NV][VEC];
+    if (FULL) {
+        float dot = 0.0f;
+        R::owned(experts, own);
+        most_of[0] = raw.largest(e[0]);
+        exponentials_of<R>(e, most_of, TYPE != BAGUA_F16);
+        const float inverse = R::reciprocal_sum(own, e[0]);
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) dot = __builtin_fmaf(e[0][j][i], spread[R::at(j, experts) + i] * own[j][i], dot);
-            shift = lanes_reduce<L>(dot, OpAddF()) * inverse;
-            factor = a.scale * inverse;
-            // a row without a choice (padding) has no gradient, whatever its logits are
-            const uint64_t chosen = __ballot(any), of_row = (L == 64 ? ~0ull : (1ull << (L & 63)) - 1) << (row * L & 63);
-            any = (chosen & of_row) != 0;
-        }
-        one* out = t.template ptr<one>(kGradOut) + token * a.out_ld;
+            for (int i = 0; i < VEC; ++i) dot = __builtin_fmaf(e[0][j][i], static_cast<float>(spread[R::at(j, experts) + i]) * own[j][i], dot);
+        shift = lanes_reduce<L>(dot, OpAddF()) * inverse;
+        factor = a.scale * inverse;
+        any = (__ballot(any) & lanes_of_row<L>(row)) != 0;      // a row without a choice (padding) has no gradient, whatever its logits are
+    }
+    if (!there) return;
+    one* out = t.template ptr<one>(kGradOut) + token * a.out_ld;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            typename R::raw q;
+    for (int j = 0; j < NV; ++j) {
+        typename R::raw q;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float s = spread[R::at(j, experts) + i];
-                q[i] = Elem<TYPE>::narrow(FULL ? (any ? e[0][j][i] * (factor * (s - shift)) : 0.0f) : s);
-            }
-            if (there) __builtin_nontemporal_store(q, reinterpret_cast<typename R::raw*>(out + R::at(j, experts)));
+        for (int i = 0; i < VEC; ++i) {
+            const held s = spread[R::at(j, experts) + i];
+            if constexpr (FULL) q[i] = Elem<TYPE>::narrow(any ? e[0][j][i] * (factor * (s - shift)) : 0.0f);
+            else q[i] = s;
         }
-        wave_sync();
-        for (int j = in_row; j < top_k && there; j += L) {
-            const int at = id(j);
-            if (at >= 0) spread[at] = 0.0f;
-        }
-        wave_sync();
+        __builtin_nontemporal_store(q, reinterpret_cast<typename R::raw*>(out + R::at(j, experts)));
     }
 }
 
@@ -770,7 +769,6 @@ inline int route_waves(size_t wave_bytes)
     while (waves > 1 && waves * wave_bytes > 64 * 1024) waves /= 2;
     return waves;
 }
-inline dim3 route_grid(uint64_t tiles, int waves) { return dim3(static_cast<uint32_t>((std::min<uint64_t>(tiles, kRouteMostWaves) + waves - 1) / waves)); }
 
 inline int route_check(int dtype, const size_t* tokens, int k, int experts, int score, int top_k, int id_bytes, double scale)
 {
@@ -897,7 +895,7 @@ extern "C" int bagua_route_grad(int dtype, const void* const* logits, size_t ld,
     a.ld = ld, a.ids_ld = ids_ld, a.weights_ld = weights_ld, a.up_ld = dweights_ld, a.out_ld = ld_out;
     a.experts = experts, a.top_k = top_k, a.score = score, a.renormalise = renormalise != 0, a.id_bytes = id_bytes, a.scale = static_cast<float>(scale);
     int status = BAGUA_OK;
-    with_layout<false>(dtype, experts, [&](auto layout, auto type) {
+    with_route_layout(dtype, experts, [&](auto layout, auto type) {
         typedef decltype(layout) Lay;
         constexpr int TYPE = decltype(type)::value;
         constexpr uint32_t RW = kWave / Lay::L;
@@ -907,14 +905,16 @@ extern "C" int bagua_route_grad(int dtype, const void* const* logits, size_t ld,
             return;
         }
         if (tiles == 0) return;
-        a.wave_words = (RW * static_cast<uint32_t>(experts) + 1) & ~1u;
-        const size_t wave_bytes = a.wave_words * sizeof(uint32_t);
+        const bool full = score == BAGUA_SCORE_SOFTMAX && !renormalise;
+        a.row_held = (experts + Lay::VEC - 1) / Lay::VEC * Lay::VEC;
+        const size_t wave_bytes = (RW * static_cast<size_t>(a.row_held) * (full ? sizeof(float) : element) + 15) / 16 * 16;
+        a.wave_words = static_cast<uint32_t>(wave_bytes / sizeof(uint32_t));
         const int waves = route_waves(wave_bytes);
-        const dim3 grid = route_grid(tiles, waves), block(static_cast<uint32_t>(kWave * waves));
+        const dim3 grid(static_cast<uint32_t>((tiles + static_cast<uint64_t>(waves) - 1) / static_cast<uint64_t>(waves))), block(static_cast<uint32_t>(kWave * waves));
         auto launch = [&](auto kernel) {
             launch_kernel(kernel, grid, block, wave_bytes * static_cast<size_t>(waves), static_cast<hipStream_t>(stream), ls, a, static_cast<uint32_t>(tiles));
         };
-        if (score == BAGUA_SCORE_SOFTMAX && !renormalise) launch(k_route_grad<TYPE, Lay::VEC, Lay::L, Lay::NV, true>);
+        if (full) launch(k_route_grad<TYPE, Lay::VEC, Lay::L, Lay::NV, true>);
         else launch(k_route_grad<TYPE, Lay::VEC, Lay::L, Lay::NV, false>);
         status = launch_status();
     });
