@@ -15,6 +15,8 @@ namespace bagua {
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr uint32_t kMostParts = kWave;        // of a row: a lane for each where they are put together
 
+constexpr uint32_t kLessonFloats = 5;         // of a row, beside its parts
+
 enum { kLogits = 0, kIds, kTeacher, kLabels, kMask, kLoss, kStats, kDistillLists };
 enum { kUp = kLoss, kOut = kStats + 1, kDistillGradLists };      // of the backward pass; the others are the same
 
@@ -24,7 +26,7 @@ struct DistillArgs {
     int top, id_bytes, teacher_type, label_bytes;    // label_bytes: 0 for no labels
     int up_per_row;
     float temperature, to_log2, teacher_weight, label_weight;    // to_log2: log2(e) / temperature
-    float* partial;                                  // [row][part][3], where a row has several
+    float* partial;                                  // [row][3 * parts + kLessonFloats], where a row has several parts
 };
 
 // What a row is taught: the teacher's entries, and the label.
@@ -101,74 +103,108 @@ struct Span {
     }
 };
 
-// The largest logit and the sums relative to it.
-template <int SUMS>
+// exp(d) from e = exp(d / T), where T is the whole number POWER: its square, third or fourth power, an operation or two instead of an exponential, which takes
+// as long as four.  POWER 0: T is another number.
+template <int POWER>
+__device__ __forceinline__ float power_of(float e, float d)
+{
+    if (POWER == 1) return e;
+    if (POWER == 2) return e * e;
+    if (POWER == 3) return e * e * e;
+    if (POWER == 4) return (e * e) * (e * e);
+    return __builtin_amdgcn_exp2f(d * kLog2e);
+}
+
+// The largest logit and the sums relative to it, at the teacher's temperature and, unless POWER is 1, at temperature 1.
+template <int POWER>
 struct Running {
-    float most = -INFINITY, sum[SUMS] = {};
+    static constexpr bool TWO = POWER != 1;
+    float most = -INFINITY, sum = 0.0f, sum_1 = 0.0f;
     __device__ __forceinline__ void rise(float m, const DistillArgs& a)
     {
         const float up = fmaxf(most, m), d = most == up ? 0.0f : most - up;     // (both -infinity: stays)
-        sum[0] *= __builtin_amdgcn_exp2f(d * a.to_log2);
-        if (SUMS == 2) sum[SUMS - 1] *= __builtin_amdgcn_exp2f(d * kLog2e);
+        const float e = __builtin_amdgcn_exp2f(d * a.to_log2);
+        sum *= e;
+        if (TWO) sum_1 *= power_of<POWER>(e, d);
         most = up;
     }
     __device__ __forceinline__ void add(float x, float from, const DistillArgs& a)
     {
-        const float d = x - from;
-        sum[0] += __builtin_amdgcn_exp2f(d * a.to_log2);
-        if (SUMS == 2) sum[SUMS - 1] += __builtin_amdgcn_exp2f(d * kLog2e);
+        const float d = x - from, e = __builtin_amdgcn_exp2f(d * a.to_log2);
+        sum += e;
+        if (POWER == 2) sum_1 = __builtin_fmaf(e, e, sum_1);
+        else if (TWO) sum_1 += power_of<POWER>(e, d);
     }
     __device__ __forceinline__ float origin() const { return most == -INFINITY ? 0.0f : most; }
+    // Put together over a wave, in every lane.
+    __device__ __forceinline__ void together(const DistillArgs& a)
+    {
+        rise(lanes_most<kWave>(most), a);
+        sum = lanes_reduce<kWave>(sum, OpAddF());
+        sum_1 = TWO ? lanes_reduce<kWave>(sum_1, OpAddF()) : sum;
+    }
 };
 
-// Loss and statistics of a row from what `parts` lanes of a wave hold of it.  first_id, first: the lane's teacher entry.
-template <int SUMS, int TYPE, int P>
-__device__ __forceinline__ void finish(const Taught<P>& w, const typename Elem<TYPE>::one* row, Running<SUMS> r, int lane, int first_id, float first_teacher, float first_x)
+// What a wave knows of the row's entries and label before it knows the row's sums.
+//   the teacher's part / T^2 = sum q log q - sum q (x - origin) / T + (most - origin) / T + log(sum)     with the row's largest logit and sum,
+// relative to the largest of the entries' own logits, so that nothing is rounded where it is large.
+struct Lesson {
+    float known, origin, at_label;      // the first two sums; NaN in at_label: no label
+    bool entries;
+};
+template <int TYPE, int P>
+__device__ __forceinline__ Lesson lesson_of(const Taught<P>& w, const typename Elem<TYPE>::one* row, int lane, int first_id, float first_teacher, float first_x, int label, float at_label)
 {
     const DistillArgs& a = w.a;
-    const float all = lanes_most<kWave>(r.most);
-    r.rise(all, a);
-    const float s = lanes_reduce<kWave>(r.sum[0], OpAddF()), s1 = SUMS == 2 ? lanes_reduce<kWave>(r.sum[SUMS - 1], OpAddF()) : s;
     const TeacherSum teacher(w, first_teacher, lane);
-    const float log_s = logf(s), log_q = logf(teacher.sum);
-    float part = 0.0f;
+    Lesson l{0.0f, -INFINITY, label >= 0 ? at_label : 0.0f, teacher.sum != 0.0f};
+    const float log_sum = logf(teacher.sum);
+    if (first_id >= 0 && first_teacher != -INFINITY) l.origin = first_x;
+    for (int j = lane + kWave; j < a.top; j += kWave) {
+        const int id = w.id(j);
+        if (id >= 0) l.origin = fmaxf(l.origin, Elem<TYPE>::widen(row[id]));
+    }
+    l.origin = lanes_most<kWave>(l.origin);
+    if (l.origin == -INFINITY) l.origin = 0.0f;
     auto entry = [&](int id, float y, float x) {
         const float term = TeacherSum::term(y, teacher.most, a);
         if (id < 0 || term == 0.0f) return;
-        const float q = term / teacher.sum;
-        const float log_p = x == -INFINITY ? x : (x - all) / a.temperature - log_s;
-        part += q * (((y - teacher.most) / a.temperature - log_q) - log_p);
+        l.known += term / teacher.sum * (((y - teacher.most) / a.temperature - log_sum) - (x - l.origin) / a.temperature);
     };
     entry(first_id, first_teacher, first_x);
     for (int j = lane + kWave; j < a.top; j += kWave) {
         const int id = w.id(j);
         if (id >= 0) entry(id, w.logit(j, id), Elem<TYPE>::widen(row[id]));
     }
-    part = lanes_reduce<kWave>(part, OpAddF());
-    const int label = w.label();
-    float loss = a.teacher_weight * (a.temperature * a.temperature) * part;
-    if (label >= 0) {
-        const float x = Elem<TYPE>::widen(row[label]);
-        loss += a.label_weight * (x == -INFINITY ? INFINITY : logf(s1) - (x - all));
-    }
-    if (lane == 0) {
-        w.t.template ptr<float>(kLoss)[w.t.t0] = loss;
-        float* stats = w.t.template ptr<float>(kStats) + static_cast<size_t>(w.t.t0) * 3;
-        stats[0] = all;
-        stats[1] = s;
-        stats[2] = a.label_bytes ? s1 : 0.0f;
-    }
+    l.known = lanes_reduce<kWave>(l.known, OpAddF());
+    return l;
+}
+// Loss and statistics of a row, by one lane.
+template <int POWER, int P>
+__device__ __forceinline__ void finish(const Taught<P>& w, const Lesson& l, const Running<POWER>& r, bool label)
+{
+    const DistillArgs& a = w.a;
+    float loss = 0.0f;
+    // (a part of weight 0 adds nothing where it is infinite either)
+    if (l.entries && a.teacher_weight != 0.0f)
+        loss = a.teacher_weight * (a.temperature * a.temperature) * (r.most == -INFINITY ? INFINITY : l.known + ((r.most - l.origin) / a.temperature + logf(r.sum)));
+    if (label && a.label_weight != 0.0f) loss += a.label_weight * (l.at_label == -INFINITY ? INFINITY : logf(r.sum_1) - (l.at_label - r.most));
+    w.t.template ptr<float>(kLoss)[w.t.t0] = loss;
+    float* stats = w.t.template ptr<float>(kStats) + static_cast<size_t>(w.t.t0) * 3;
+    stats[0] = r.most;
+    stats[1] = r.sum;
+    stats[2] = a.label_bytes ? r.sum_1 : 0.0f;
 }
 
-// One workgroup for a row, or a part of one.  SUMS: 2 where a label needs the sum at temperature 1 beside the one at the teacher's.
-template <int TYPE, int SUMS, int THREADS>
+// One workgroup for a row, or a part of one.
+template <int TYPE, int POWER, int THREADS>
 __global__ void __launch_bounds__(THREADS)
 k_distill(Lists<kDistillLists> ls, DistillArgs a)
 {
     typedef typename Elem<TYPE>::one one;
     typedef Span<TYPE> S;
     constexpr int VEC = S::VEC, UNROLL = 4, WAVES = THREADS / kWave;
-    __shared__ float of_wave[WAVES][1 + SUMS];
+    __shared__ float of_wave[3][WAVES];
     const int lane = threadIdx.x & 63, wave = wave_index();
     const uint32_t unit = blockIdx.x / a.parts, part = blockIdx.x - unit * a.parts;
     const ListTile<kDistillLists> t(ls, unit, 1);
@@ -182,14 +218,19 @@ k_distill(Lists<kDistillLists> ls, DistillArgs a)
     }
     const one* row = t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0) * a.ld;
     const S span(row, a.vocab, part, a.parts);
-    int id = -1;
-    float teacher = -INFINITY, at_id = 0.0f;
-    if (a.parts == 1 && wave == 0 && lane < a.top) {              // on their way while the row is read
-        id = w.id(lane);
-        teacher = w.logit(lane, id);
-        if (id >= 0) at_id = Elem<TYPE>::widen(row[id]);
+    const bool teaches = part == 0 && wave == 0;
+    int id = -1, label = -1;
+    float teacher = -INFINITY, at_id = 0.0f, at_label = 0.0f;
+    if (teaches) {                                                // on their way while the row is read
+        label = w.label();
+        if (lane < a.top) {
+            id = w.id(lane);
+            teacher = w.logit(lane, id);
+            if (id >= 0) at_id = Elem<TYPE>::widen(row[id]);
+        }
+        if (label >= 0) at_label = Elem<TYPE>::widen(row[label]);
     }
-    Running<SUMS> r;
+    Running<POWER> r;
     const uint32_t alone = span.single(threadIdx.x, a.vocab);
     if (alone < a.vocab) {
         const float x = Elem<TYPE>::widen(row[alone]);
@@ -197,18 +238,17 @@ k_distill(Lists<kDistillLists> ls, DistillArgs a)
         r.add(x, r.origin(), a);
     }
     const typename S::v* from = reinterpret_cast<const typename S::v*>(row + span.head);
-    for (uint32_t i = span.first + threadIdx.x; i < span.last; i += THREADS * UNROLL) {
+    // A wave's vectors: UNROLL at a time as long as all of them are there, then what is left.
+    uint32_t base = span.first + static_cast<uint32_t>(wave) * kWave;
+    for (; base + (UNROLL - 1) * THREADS + kWave <= span.last; base += UNROLL * THREADS) {
         typename S::v q[UNROLL];
         float x[UNROLL][VEC], most = -INFINITY;
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) q[u] = __builtin_nontemporal_load(from + min(i + u * THREADS, span.last - 1));
+        for (int u = 0; u < UNROLL; ++u) q[u] = __builtin_nontemporal_load(from + base + u * THREADS + lane);
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                x[u][e] = i + u * THREADS < span.last ? Elem<TYPE>::widen(q[u][e]) : -INFINITY;
-                most = fmaxf(most, x[u][e]);
-            }
+            for (int e = 0; e < VEC; ++e) most = fmaxf(most, x[u][e] = Elem<TYPE>::widen(q[u][e]));
         r.rise(most, a);
         const float origin = r.origin();
 #pragma unroll
@@ -216,64 +256,69 @@ k_distill(Lists<kDistillLists> ls, DistillArgs a)
 #pragma unroll
             for (int e = 0; e < VEC; ++e) r.add(x[u][e], origin, a);
     }
-    // the lanes of a wave, then the waves
-    const float all = lanes_most<kWave>(r.most);
-    r.rise(all, a);
+    if (base < span.last) {
+        typename S::v q[UNROLL];
 #pragma unroll
-    for (int s = 0; s < SUMS; ++s) r.sum[s] = lanes_reduce<kWave>(r.sum[s], OpAddF());
-    if (WAVES > 1) {
-        if (lane == 0) {
-            of_wave[wave][0] = r.most;
+        for (int u = 0; u < UNROLL; ++u) q[u] = __builtin_nontemporal_load(from + min(base + u * THREADS + lane, span.last - 1));
 #pragma unroll
-            for (int s = 0; s < SUMS; ++s) of_wave[wave][1 + s] = r.sum[s];
+        for (int u = 0; u < UNROLL; ++u) {
+            if (base + u * THREADS >= span.last) break;
+            const bool there = base + u * THREADS + lane < span.last;
+            float x[VEC], most = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) most = fmaxf(most, x[e] = there ? Elem<TYPE>::widen(q[u][e]) : -INFINITY);
+            r.rise(most, a);
+            const float origin = r.origin();
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) r.add(x[e], origin, a);
         }
+    }
+    r.together(a);
+    if (WAVES > 1) {
+        if (lane == 0) of_wave[0][wave] = r.most, of_wave[1][wave] = r.sum, of_wave[2][wave] = r.sum_1;
         __syncthreads();
         if (wave != 0) return;
+        r = Running<POWER>();
+        if (lane < WAVES) r.most = of_wave[0][lane], r.sum = of_wave[1][lane], r.sum_1 = of_wave[2][lane];
+        r.together(a);
     }
-    Running<SUMS> mine;
-    if (WAVES == 1 ? lane == 0 : lane < WAVES) {
-        mine.most = WAVES == 1 ? r.most : of_wave[lane % WAVES][0];
-#pragma unroll
-        for (int s = 0; s < SUMS; ++s) mine.sum[s] = WAVES == 1 ? r.sum[s] : of_wave[lane % WAVES][1 + s];
-    }
+    Lesson l{};
+    if (teaches) l = lesson_of<TYPE>(w, row, lane, id, teacher, at_id, label, at_label);
+    if (lane != 0) return;
     if (a.parts == 1) {
-        finish<SUMS, TYPE>(w, row, mine, lane, id, teacher, at_id);
+        finish(w, l, r, label >= 0);
         return;
     }
-    const float most = lanes_most<kWave>(mine.most);
-    mine.rise(most, a);
-    float* out = a.partial + (static_cast<size_t>(unit) * a.parts + part) * 3;
-    const float s = lanes_reduce<kWave>(mine.sum[0], OpAddF()), s1 = SUMS == 2 ? lanes_reduce<kWave>(mine.sum[SUMS - 1], OpAddF()) : 0.0f;
-    if (lane == 0) out[0] = most, out[1] = s, out[2] = s1;
+    float* out = a.partial + static_cast<size_t>(unit) * (3 * a.parts + kLessonFloats);
+    out[part] = r.most, out[a.parts + part] = r.sum, out[2 * a.parts + part] = r.sum_1;
+    if (teaches) {
+        out += 3 * a.parts;
+        out[0] = l.known, out[1] = l.origin, out[2] = l.at_label, out[3] = l.entries ? 1.0f : 0.0f, out[4] = label >= 0 ? 1.0f : 0.0f;
+    }
 }
 
 // Puts the parts of a row together: one wave for each row.
-template <int TYPE, int SUMS>
+template <int POWER>
 __global__ void __launch_bounds__(kWave)
 k_distill_finish(Lists<kDistillLists> ls, DistillArgs a)
 {
-    typedef typename Elem<TYPE>::one one;
     const int lane = threadIdx.x & 63;
     const ListTile<kDistillLists> t(ls, blockIdx.x, 1);
     const Taught<kDistillLists> w{a, t};
     if (!w.counts()) return;
-    const one* row = t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0) * a.ld;
-    Running<SUMS> r;
-    if (lane < static_cast<int>(a.parts)) {
-        const float* p = a.partial + (static_cast<size_t>(blockIdx.x) * a.parts + static_cast<uint32_t>(lane)) * 3;
-        r.most = p[0];
-#pragma unroll
-        for (int s = 0; s < SUMS; ++s) r.sum[s] = p[1 + s];
-    }
-    const int id = lane < a.top ? w.id(lane) : -1;
-    const float teacher = lane < a.top ? w.logit(lane, id) : -INFINITY;
-    finish<SUMS, TYPE>(w, row, r, lane, id, teacher, id >= 0 ? Elem<TYPE>::widen(row[id]) : 0.0f);
+    const float *p = a.partial + static_cast<size_t>(blockIdx.x) * (3 * a.parts + kLessonFloats), *q = p + 3 * a.parts;
+    const Lesson l{q[0], q[1], q[2], q[3] != 0.0f};
+    const bool label = q[4] != 0.0f;
+    Running<POWER> r;
+    if (lane < static_cast<int>(a.parts)) r.most = p[lane], r.sum = p[a.parts + lane], r.sum_1 = p[2 * a.parts + lane];
+    r.together(a);
+    if (lane == 0) finish(w, l, r, label);
 }
 
 // The backward pass, one workgroup for a part of a row: factor * exp((x - largest) / temperature), and with labels the same at temperature 1, for every
 // logit; the few that the teacher or the label names are written over when the others are out, each with all that its entries take from it.
 // The gradient may lie where the logits are: a workgroup reads those of its part that are named before it writes any.
-template <int TYPE, int SUMS, int THREADS>
+template <int TYPE, int POWER, int THREADS>
 __global__ void __launch_bounds__(THREADS)
 k_distill_grad(Lists<kDistillGradLists> ls, DistillArgs a)
 {
@@ -306,7 +351,7 @@ k_distill_grad(Lists<kDistillGradLists> ls, DistillArgs a)
     const float teach = teacher.sum == 0.0f ? 0.0f : up * (a.teacher_weight * a.temperature), tell = label < 0 ? 0.0f : up * a.label_weight;
     float factor = stats[1] == 0.0f ? 0.0f : teach / stats[1];
     const float factor_1 = stats[1] == 0.0f || a.label_bytes == 0 ? 0.0f : tell / stats[2];
-    if (SUMS == 1) factor += factor_1;                                    // both at temperature 1, or no labels
+    if (POWER == 1) factor += factor_1;                                   // both at temperature 1, or no labels
     for (int j = static_cast<int>(threadIdx.x); j <= a.top; j += THREADS) {
         const int id = j < a.top ? w.id(j) : label;
         const bool here = id >= 0 && static_cast<uint32_t>(id) >= span.from && static_cast<uint32_t>(id) < span.to;
@@ -316,23 +361,31 @@ k_distill_grad(Lists<kDistillGradLists> ls, DistillArgs a)
     }
     __syncthreads();
     auto value = [&](float x) {
-        const float d = x - origin;
-        float v = factor * __builtin_amdgcn_exp2f(d * a.to_log2);
-        if (SUMS == 2) v = __builtin_fmaf(factor_1, __builtin_amdgcn_exp2f(d * kLog2e), v);
-        return v;
+        const float d = x - origin, e = __builtin_amdgcn_exp2f(d * a.to_log2);
+        return POWER == 1 ? factor * e : __builtin_fmaf(factor_1, power_of<POWER>(e, d), factor * e);
     };
     const typename S::v* from = reinterpret_cast<const typename S::v*>(row + span.head);
-    for (uint32_t i = span.first + threadIdx.x; i < span.last; i += THREADS * UNROLL) {
+    uint32_t base = span.first + static_cast<uint32_t>(wave_index()) * kWave;
+    auto put = [&](uint32_t i, const typename S::v& q) {
+        typename S::v o;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) o[e] = Elem<TYPE>::narrow(value(Elem<TYPE>::widen(q[e])));
+        __builtin_nontemporal_store(o, to + i);
+    };
+    for (; base + (UNROLL - 1) * THREADS + kWave <= span.last; base += UNROLL * THREADS) {
         typename S::v q[UNROLL];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) q[u] = __builtin_nontemporal_load(from + min(i + u * THREADS, span.last - 1));
+        for (int u = 0; u < UNROLL; ++u) q[u] = __builtin_nontemporal_load(from + base + u * THREADS + lane);
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            typename S::v o;
+        for (int u = 0; u < UNROLL; ++u) put(base + u * THREADS + lane, q[u]);
+    }
+    if (base < span.last) {
+        typename S::v q[UNROLL];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) o[e] = Elem<TYPE>::narrow(value(Elem<TYPE>::widen(q[u][e])));
-            if (i + u * THREADS < span.last) __builtin_nontemporal_store(o, to + i + u * THREADS);
-        }
+        for (int u = 0; u < UNROLL; ++u) q[u] = __builtin_nontemporal_load(from + min(base + u * THREADS + lane, span.last - 1));
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+            if (base + u * THREADS + lane < span.last) put(base + u * THREADS + lane, q[u]);
     }
     if (alone < a.vocab) out[alone] = Elem<TYPE>::narrow(value(Elem<TYPE>::widen(row[alone])));
     pace_loads();                                                         // what is out cannot overtake what is written over it
@@ -422,21 +475,24 @@ inline int distill_check(const DistillCall& c, Lists<P>& ls, DistillArgs& a, Ran
     return BAGUA_OK;
 }
 
-// f with the type, the number of sums, and the threads of a workgroup.
+// f with the type, what power of an exponential at the teacher's temperature is one at 1, and the threads of a workgroup.
 template <typename F>
-inline void with_distill(int dtype, bool two, size_t vocab, const F& f)
+inline void with_distill(int dtype, bool labels, double temperature, size_t vocab, const F& f)
 {
-    auto sums = [&](auto type) {
-        auto threads = [&](auto n) {
-            if (vocab <= kShortVocab) f(type, n, std::integral_constant<int, kWave>());
-            else f(type, n, std::integral_constant<int, kDistillThreads>());
+    auto of_type = [&](auto type) {
+        auto of_power = [&](auto power) {
+            if (vocab <= kShortVocab) f(type, power, std::integral_constant<int, kWave>());
+            else f(type, power, std::integral_constant<int, kDistillThreads>());
         };
-        if (two) threads(std::integral_constant<int, 2>());
-        else threads(std::integral_constant<int, 1>());
+        if (!labels || temperature == 1.0) of_power(std::integral_constant<int, 1>());
+        else if (temperature == 2.0) of_power(std::integral_constant<int, 2>());
+        else if (temperature == 3.0) of_power(std::integral_constant<int, 3>());
+        else if (temperature == 4.0) of_power(std::integral_constant<int, 4>());
+        else of_power(std::integral_constant<int, 0>());
     };
-    if (dtype == BAGUA_F32) sums(std::integral_constant<int, BAGUA_F32>());
-    else if (dtype == BAGUA_BF16) sums(std::integral_constant<int, BAGUA_BF16>());
-    else sums(std::integral_constant<int, BAGUA_F16>());
+    if (dtype == BAGUA_F32) of_type(std::integral_constant<int, BAGUA_F32>());
+    else if (dtype == BAGUA_BF16) of_type(std::integral_constant<int, BAGUA_BF16>());
+    else of_type(std::integral_constant<int, BAGUA_F16>());
 }
 
 }  // namespace bagua
@@ -447,7 +503,7 @@ extern "C" size_t bagua_distill_workspace_bytes(size_t rows, size_t vocab)
 {
     if (vocab < 1 || vocab > BAGUA_MAX_VOCABULARY || rows > kMaxGrid) return 0;
     const size_t parts = loss_parts(rows, vocab);
-    return 16 + (parts > 1 ? (rows * parts * 3 * sizeof(float) + 15) / 16 * 16 : 0);
+    return 16 + (parts > 1 ? (rows * (parts * 3 + kLessonFloats) * sizeof(float) + 15) / 16 * 16 : 0);
 }
 
 extern "C" int bagua_distill_loss(int dtype, const void* const* logits, size_t ld, const size_t* rows, int k, size_t vocab, const void* const* ids, int id_bytes,
@@ -483,12 +539,12 @@ extern "C" int bagua_distill_loss(int dtype, const void* const* logits, size_t l
     if (total * a.parts > kMaxGrid) return BAGUA_ERR_UNSUPPORTED;
     hipStream_t s = static_cast<hipStream_t>(stream);
     int status = BAGUA_OK;
-    with_distill(dtype, labels && temperature != 1.0, vocab, [&](auto type, auto sums, auto threads) {
-        constexpr int TYPE = decltype(type)::value, SUMS = decltype(sums)::value, THREADS = decltype(threads)::value;
-        launch_kernel(k_distill<TYPE, SUMS, THREADS>, dim3(static_cast<uint32_t>(total) * a.parts), dim3(THREADS), 0, s, ls, a);
+    with_distill(dtype, labels != nullptr, temperature, vocab, [&](auto type, auto power, auto threads) {
+        constexpr int TYPE = decltype(type)::value, POWER = decltype(power)::value, THREADS = decltype(threads)::value;
+        launch_kernel(k_distill<TYPE, POWER, THREADS>, dim3(static_cast<uint32_t>(total) * a.parts), dim3(THREADS), 0, s, ls, a);
         status = launch_status();
         if (status != BAGUA_OK || a.parts == 1) return;
-        launch_kernel(k_distill_finish<TYPE, SUMS>, dim3(static_cast<uint32_t>(total)), dim3(kWave), 0, s, ls, a);
+        launch_kernel(k_distill_finish<POWER>, dim3(static_cast<uint32_t>(total)), dim3(kWave), 0, s, ls, a);
         status = launch_status();
     });
     return status;
@@ -529,9 +585,9 @@ extern "C" int bagua_distill_grad(int dtype, const void* const* logits, size_t l
     a.parts = grad_parts(total, vocab);
     if (total * a.parts > kMaxGrid) return BAGUA_ERR_UNSUPPORTED;
     int status = BAGUA_OK;
-    with_distill(dtype, labels && temperature != 1.0, vocab, [&](auto type, auto sums, auto threads) {
-        constexpr int TYPE = decltype(type)::value, SUMS = decltype(sums)::value, THREADS = decltype(threads)::value;
-        launch_kernel(k_distill_grad<TYPE, SUMS, THREADS>, dim3(static_cast<uint32_t>(total) * a.parts), dim3(THREADS), static_cast<size_t>(top + 1) * 3 * sizeof(float),
+    with_distill(dtype, labels != nullptr, temperature, vocab, [&](auto type, auto power, auto threads) {
+        constexpr int TYPE = decltype(type)::value, POWER = decltype(power)::value, THREADS = decltype(threads)::value;
+        launch_kernel(k_distill_grad<TYPE, POWER, THREADS>, dim3(static_cast<uint32_t>(total) * a.parts), dim3(THREADS), static_cast<size_t>(top + 1) * 3 * sizeof(float),
                       static_cast<hipStream_t>(stream), ls, a);
         status = launch_status();
     });
