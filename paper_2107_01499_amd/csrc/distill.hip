@@ -12,7 +12,6 @@
 
 namespace bagua {
 
-constexpr float kLog2e = 1.44269504088896340736f;
 constexpr uint32_t kMostParts = kWave;        // of a row: a lane for each where they are put together
 
 constexpr uint32_t kLessonFloats = 5;         // of a row, beside its parts
@@ -25,7 +24,7 @@ struct DistillArgs {
     uint32_t vocab, parts;
     int top, id_bytes, teacher_type, label_bytes;    // label_bytes: 0 for no labels
     int up_per_row;
-    float temperature, to_log2, teacher_weight, label_weight;    // to_log2: log2(e) / temperature
+    float temperature, per_temperature, to_log2, teacher_weight, label_weight;    // to_log2: log2(e) / temperature
     float* partial;                                  // [row][3 * parts + kLessonFloats], where a row has several parts
 };
 
@@ -59,47 +58,86 @@ struct Taught {
     __device__ __forceinline__ bool counts() const { return !t.has(kMask) || t.template ptr<const uint8_t>(kMask)[t.t0] != 0; }
 };
 
-// The teacher's softmax over its entries, by a wave that has entry j in lane j % 64: its largest logit and the sum relative to it; no entry: sum 0.
+// A wave's entries, j in lane j % 64: the first kHeld of every lane are asked for together, and kept; the others are read again by whoever needs them.
+constexpr int kHeld = 2;
+struct Entries {
+    int id[kHeld], top;
+    float y[kHeld];                    // -infinity: none
+    template <int P>
+    __device__ __forceinline__ void load(const Taught<P>& w, int lane)
+    {
+        top = w.a.top;
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) {
+            id[h] = -1;
+            if (h * kWave < top && lane + h * kWave < top) id[h] = w.id(lane + h * kWave);
+        }
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) {
+            y[h] = -INFINITY;
+            if (h * kWave < top) y[h] = w.logit(min(lane + h * kWave, top - 1), id[h]);
+        }
+    }
+    // f(place, id, logit, whether it is kept, which of those)
+    template <int P, typename F>
+    __device__ __forceinline__ void each(const Taught<P>& w, int lane, const F& f) const
+    {
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h)
+            if (h * kWave < top && id[h] >= 0) f(lane + h * kWave, id[h], y[h], std::integral_constant<bool, true>(), h);
+        for (int j = lane + kHeld * kWave; j < top; j += kWave) {
+            const int i = w.id(j);
+            if (i >= 0) f(j, i, w.logit(j, i), std::integral_constant<bool, false>(), 0);
+        }
+    }
+};
+// The teacher's softmax over its entries: its largest logit and the sum relative to it; no entry above -infinity: sum 0.
 struct TeacherSum {
     float most, sum;
     // exp((logit - most) / temperature), 0 for an entry that is none
-    static __device__ __forceinline__ float term(float logit, float most, const DistillArgs& a) { return logit == -INFINITY ? 0.0f : expf((logit - most) / a.temperature); }
+    static __device__ __forceinline__ float term(float logit, float most, const DistillArgs& a) { return logit == -INFINITY ? 0.0f : exp_below((logit - most) * a.per_temperature); }
     template <int P>
-    __device__ __forceinline__ TeacherSum(const Taught<P>& w, float first, int lane)
+    __device__ __forceinline__ TeacherSum(const Taught<P>& w, const Entries& entries, int lane)
     {
-        most = first;
-        for (int j = lane + kWave; j < w.a.top; j += kWave) most = fmaxf(most, w.logit(j, w.id(j)));
-        most = lanes_most<kWave>(most);
-        sum = term(first, most, w.a);
-        for (int j = lane + kWave; j < w.a.top; j += kWave) sum += term(w.logit(j, w.id(j)), most, w.a);
-        sum = lanes_reduce<kWave>(sum, OpAddF());
+        float m = -INFINITY, s = 0.0f;
+        entries.each(w, lane, [&](int, int, float y, auto, int) { m = fmaxf(m, y); });
+        most = lanes_most<kWave>(m);
+        entries.each(w, lane, [&](int, int, float y, auto, int) { s += term(y, most, w.a); });
+        sum = lanes_reduce<kWave>(s, OpAddF());
     }
 };
 
-// The logits of a row as the kernels go through them: some that lie before the first aligned vector, vectors, and some behind the last.
-template <int TYPE>
+// The logits of a row as the kernels go through them: some that lie before the first line of memory, vectors, and some behind the last vector.  A wave's 64
+// vectors are then whole lines, which stores want: with vectors that are aligned to themselves alone 8 x 512 rows of 30522, bf16, took 8 % longer.
+// (Rows that one wave has are short enough that its time goes into what lies in no vector: their vectors are aligned to themselves.)
+template <int TYPE, int THREADS>
 struct Span {
     typedef typename Elem<TYPE>::one one;
     static constexpr int VEC = TYPE == BAGUA_F32 ? 4 : 8;
+    static constexpr uint32_t LINE = (THREADS == kWave ? 16 : 128) / sizeof(one);
     typedef one v __attribute__((ext_vector_type(VEC), aligned(sizeof(one))));
     uint32_t head, vectors, first, last;       // first, last: vectors of this part
-    uint32_t from, to;                         // elements of this part
-    __device__ __forceinline__ Span(const one* aligned_row, uint32_t vocab, uint32_t part, uint32_t parts)
+    bool begins, ends;                         // whether the elements before and behind the vectors are of this part
+    __device__ __forceinline__ Span(const one* row, uint32_t vocab, uint32_t part, uint32_t parts)
     {
-        head = min(vocab, (0u - static_cast<uint32_t>(reinterpret_cast<uintptr_t>(aligned_row) / sizeof(one))) & (VEC - 1));
+        head = min(vocab, (0u - static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row) / sizeof(one))) & (LINE - 1));
         vectors = (vocab - head) / VEC;
-        const uint32_t each = (vectors + parts - 1) / parts;
+        const uint32_t each = part_vectors(vectors, parts);
         first = min(part * each, vectors);
         last = min(first + each, vectors);
-        from = part == 0 ? 0 : head + first * VEC;
-        to = part + 1 == parts ? vocab : head + last * VEC;
+        begins = part == 0;
+        ends = part + 1 == parts;
     }
-    // The elements that lie in no vector: `thread` has one of them, or none (vocab)
-    __device__ __forceinline__ uint32_t single(uint32_t thread, uint32_t vocab) const
+    static __host__ __device__ uint32_t part_vectors(uint32_t vectors, uint32_t parts) { return parts == 1 ? vectors : ((vectors + parts - 1) / parts + kWave - 1) / kWave * kWave; }
+    static constexpr uint32_t SINGLES = LINE + VEC;      // elements that lie in no vector, at most
+    // The elements of this part that lie in no vector, `step` threads one each: f(element, which of them).
+    template <typename F>
+    __device__ __forceinline__ void singles(uint32_t thread, uint32_t step, uint32_t vocab, const F& f) const
     {
-        if (thread < VEC) return thread < head && from == 0 ? thread : vocab;
-        const uint32_t e = head + vectors * VEC + thread - VEC;
-        return to == vocab && thread < 2 * VEC ? min(e, vocab) : vocab;
+        if (begins)
+            for (uint32_t e = thread; e < head; e += step) f(e, e);
+        const uint32_t tail = head + vectors * VEC;
+        if (ends && tail + thread < vocab) f(tail + thread, LINE + thread);
     }
 };
 
@@ -153,29 +191,20 @@ struct Lesson {
     bool entries;
 };
 template <int TYPE, int P>
-__device__ __forceinline__ Lesson lesson_of(const Taught<P>& w, const typename Elem<TYPE>::one* row, int lane, int first_id, float first_teacher, float first_x, int label, float at_label)
+__device__ __forceinline__ Lesson lesson_of(const Taught<P>& w, const typename Elem<TYPE>::one* row, int lane, const Entries& entries, const float (&held_x)[kHeld], int label, float at_label)
 {
     const DistillArgs& a = w.a;
-    const TeacherSum teacher(w, first_teacher, lane);
+    const TeacherSum teacher(w, entries, lane);
     Lesson l{0.0f, -INFINITY, label >= 0 ? at_label : 0.0f, teacher.sum != 0.0f};
     const float log_sum = logf(teacher.sum);
-    if (first_id >= 0 && first_teacher != -INFINITY) l.origin = first_x;
-    for (int j = lane + kWave; j < a.top; j += kWave) {
-        const int id = w.id(j);
-        if (id >= 0) l.origin = fmaxf(l.origin, Elem<TYPE>::widen(row[id]));
-    }
+    auto x_of = [&](int id, auto held, int h) { return decltype(held)::value ? held_x[h] : Elem<TYPE>::widen(row[id]); };
+    entries.each(w, lane, [&](int, int id, float, auto held, int h) { l.origin = fmaxf(l.origin, x_of(id, held, h)); });
     l.origin = lanes_most<kWave>(l.origin);
     if (l.origin == -INFINITY) l.origin = 0.0f;
-    auto entry = [&](int id, float y, float x) {
+    entries.each(w, lane, [&](int, int id, float y, auto held, int h) {
         const float term = TeacherSum::term(y, teacher.most, a);
-        if (id < 0 || term == 0.0f) return;
-        l.known += term / teacher.sum * (((y - teacher.most) / a.temperature - log_sum) - (x - l.origin) / a.temperature);
-    };
-    entry(first_id, first_teacher, first_x);
-    for (int j = lane + kWave; j < a.top; j += kWave) {
-        const int id = w.id(j);
-        if (id >= 0) entry(id, w.logit(j, id), Elem<TYPE>::widen(row[id]));
-    }
+        if (term != 0.0f) l.known += term / teacher.sum * (((y - teacher.most) * a.per_temperature - log_sum) - (x_of(id, held, h) - l.origin) * a.per_temperature);
+    });
     l.known = lanes_reduce<kWave>(l.known, OpAddF());
     return l;
 }
@@ -187,7 +216,7 @@ __device__ __forceinline__ void finish(const Taught<P>& w, const Lesson& l, cons
     float loss = 0.0f;
     // (a part of weight 0 adds nothing where it is infinite either)
     if (l.entries && a.teacher_weight != 0.0f)
-        loss = a.teacher_weight * (a.temperature * a.temperature) * (r.most == -INFINITY ? INFINITY : l.known + ((r.most - l.origin) / a.temperature + logf(r.sum)));
+        loss = a.teacher_weight * (a.temperature * a.temperature) * (r.most == -INFINITY ? INFINITY : l.known + ((r.most - l.origin) * a.per_temperature + logf(r.sum)));
     if (label && a.label_weight != 0.0f) loss += a.label_weight * (l.at_label == -INFINITY ? INFINITY : logf(r.sum_1) - (l.at_label - r.most));
     w.t.template ptr<float>(kLoss)[w.t.t0] = loss;
     float* stats = w.t.template ptr<float>(kStats) + static_cast<size_t>(w.t.t0) * 3;
@@ -202,7 +231,7 @@ __global__ void __launch_bounds__(THREADS)
 k_distill(Lists<kDistillLists> ls, DistillArgs a)
 {
     typedef typename Elem<TYPE>::one one;
-    typedef Span<TYPE> S;
+    typedef Span<TYPE, THREADS> S;
     constexpr int VEC = S::VEC, UNROLL = 4, WAVES = THREADS / kWave;
     __shared__ float of_wave[3][WAVES];
     const int lane = threadIdx.x & 63, wave = wave_index();
@@ -219,24 +248,22 @@ k_distill(Lists<kDistillLists> ls, DistillArgs a)
     const one* row = t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0) * a.ld;
     const S span(row, a.vocab, part, a.parts);
     const bool teaches = part == 0 && wave == 0;
-    int id = -1, label = -1;
-    float teacher = -INFINITY, at_id = 0.0f, at_label = 0.0f;
+    int label = -1;
+    Entries entries;
+    float held_x[kHeld], at_label = 0.0f;
     if (teaches) {                                                // on their way while the row is read
         label = w.label();
-        if (lane < a.top) {
-            id = w.id(lane);
-            teacher = w.logit(lane, id);
-            if (id >= 0) at_id = Elem<TYPE>::widen(row[id]);
-        }
+        entries.load(w, lane);
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) held_x[h] = h * kWave < a.top && entries.id[h] >= 0 ? Elem<TYPE>::widen(row[entries.id[h]]) : 0.0f;
         if (label >= 0) at_label = Elem<TYPE>::widen(row[label]);
     }
     Running<POWER> r;
-    const uint32_t alone = span.single(threadIdx.x, a.vocab);
-    if (alone < a.vocab) {
-        const float x = Elem<TYPE>::widen(row[alone]);
+    span.singles(threadIdx.x, THREADS, a.vocab, [&](uint32_t e, uint32_t) {
+        const float x = Elem<TYPE>::widen(row[e]);
         r.rise(x, a);
         r.add(x, r.origin(), a);
-    }
+    });
     const typename S::v* from = reinterpret_cast<const typename S::v*>(row + span.head);
     // A wave's vectors: UNROLL at a time as long as all of them are there, then what is left.
     uint32_t base = span.first + static_cast<uint32_t>(wave) * kWave;
@@ -283,7 +310,7 @@ k_distill(Lists<kDistillLists> ls, DistillArgs a)
         r.together(a);
     }
     Lesson l{};
-    if (teaches) l = lesson_of<TYPE>(w, row, lane, id, teacher, at_id, label, at_label);
+    if (teaches) l = lesson_of<TYPE>(w, row, lane, entries, held_x, label, at_label);
     if (lane != 0) return;
     if (a.parts == 1) {
         finish(w, l, r, label >= 0);
@@ -316,102 +343,163 @@ k_distill_finish(Lists<kDistillLists> ls, DistillArgs a)
 }
 
 // The backward pass, one workgroup for a part of a row: factor * exp((x - largest) / temperature), and with labels the same at temperature 1, for every
-// logit; the few that the teacher or the label names are written over when the others are out, each with all that its entries take from it.
-// The gradient may lie where the logits are: a workgroup reads those of its part that are named before it writes any.
+// logit, less what the teacher's entries and the label take from a few of them.  The entries of a part hang in lists, one for each vector, that the first
+// wave lays out in LDS: who writes a vector looks whether there is one.  So every element is written once, by whoever read it, and the gradient may
+// lie where the logits are.
+struct Named {
+    float less;                          // of the teacher's entries and, behind them, the label
+    int id;
+    uint32_t next;                       // of the same vector
+};
+constexpr uint32_t kNoEntry = 0xffffffffu;
 template <int TYPE, int POWER, int THREADS>
 __global__ void __launch_bounds__(THREADS)
 k_distill_grad(Lists<kDistillGradLists> ls, DistillArgs a)
 {
     typedef typename Elem<TYPE>::one one;
-    typedef Span<TYPE> S;
+    typedef Span<TYPE, THREADS> S;
     constexpr int VEC = S::VEC, UNROLL = 4;
-    extern __shared__ float named[];
-    int* named_id = reinterpret_cast<int*>(named);                       // [top + 1]: the teacher's entries and the label
-    float *named_x = named + a.top + 1, *named_less = named + 2 * (a.top + 1);
-    const int lane = threadIdx.x & 63;
+    extern __shared__ uint32_t first_of[];                               // of every vector of the part, and of the elements that lie in none
+    const int lane = threadIdx.x & 63, wave = wave_index();
     const uint32_t unit = blockIdx.x / a.parts, part = blockIdx.x - unit * a.parts;
     const ListTile<kDistillGradLists> t(ls, unit, 1);
     const Taught<kDistillGradLists> w{a, t};
     const one* row = t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0) * a.ld;
     one* out = t.template ptr<one>(kOut) + static_cast<size_t>(t.t0) * a.out_ld;
     const S span(out, a.vocab, part, a.parts);
-    const bool counts = w.counts();
-    const int first_id = counts && lane < a.top ? w.id(lane) : -1, label = counts ? w.label() : -1;
-    TeacherSum teacher(w, counts && lane < a.top ? w.logit(lane, first_id) : -INFINITY, counts ? lane : a.top);
-    typename S::v* to = reinterpret_cast<typename S::v*>(out + span.head);
-    const uint32_t alone = span.single(threadIdx.x, a.vocab);
-    if (!counts || (teacher.sum == 0.0f && label < 0)) {                  // nothing to learn: the logits do not matter
-        for (uint32_t i = span.first + threadIdx.x; i < span.last; i += THREADS) __builtin_nontemporal_store(typename S::v(0), to + i);
-        if (alone < a.vocab) out[alone] = 0;
+    const uint32_t vectors = span.last - span.first, firsts = (vectors + S::SINGLES + 3) / 4 * 4;
+    Named* named = reinterpret_cast<Named*>(first_of + firsts);
+    __shared__ float teacher_sum;
+    const typename S::v* from = reinterpret_cast<const typename S::v*>(row + span.head) + span.first;
+    typename S::v* to = reinterpret_cast<typename S::v*>(out + span.head) + span.first;
+    if (!w.counts()) {
+        for (uint32_t i = threadIdx.x; i < vectors; i += THREADS) __builtin_nontemporal_store(typename S::v(0), to + i);
+        span.singles(threadIdx.x, THREADS, a.vocab, [&](uint32_t e, uint32_t) { out[e] = 0; });
         return;
     }
+    const int label = w.label();
     const float* stats = t.template ptr<const float>(kStats) + static_cast<size_t>(t.t0) * 3;
     const float up = !t.has(kUp) ? 1.0f : t.template ptr<const float>(kUp)[a.up_per_row ? t.t0 : 0];
-    const float origin = stats[0] == -INFINITY ? 0.0f : stats[0];
-    const float teach = teacher.sum == 0.0f ? 0.0f : up * (a.teacher_weight * a.temperature), tell = label < 0 ? 0.0f : up * a.label_weight;
-    float factor = stats[1] == 0.0f ? 0.0f : teach / stats[1];
-    const float factor_1 = stats[1] == 0.0f || a.label_bytes == 0 ? 0.0f : tell / stats[2];
-    if (POWER == 1) factor += factor_1;                                   // both at temperature 1, or no labels
-    for (int j = static_cast<int>(threadIdx.x); j <= a.top; j += THREADS) {
-        const int id = j < a.top ? w.id(j) : label;
-        const bool here = id >= 0 && static_cast<uint32_t>(id) >= span.from && static_cast<uint32_t>(id) < span.to;
-        named_id[j] = here ? id : -1;
-        named_x[j] = here ? Elem<TYPE>::widen(row[id]) : 0.0f;
-        named_less[j] = j == a.top ? tell : teach == 0.0f ? 0.0f : teach * (TeacherSum::term(w.logit(j, id), teacher.most, a) / teacher.sum);
+    const float teach = up * (a.teacher_weight * a.temperature), tell = label < 0 ? 0.0f : up * a.label_weight;
+    if (wave == 0) {
+        Entries entries;
+        entries.load(w, lane);
+        typedef uint32_t w4 __attribute__((ext_vector_type(4)));
+        for (uint32_t i = 4 * static_cast<uint32_t>(lane); i < firsts; i += 4 * kWave) *reinterpret_cast<w4*>(first_of + i) = w4(kNoEntry);
+        const TeacherSum teacher(w, entries, lane);
+        const float share = teach / teacher.sum;
+        auto note = [&](int j, int id, float less) {
+            const uint32_t e = static_cast<uint32_t>(id);
+            if (id < 0) return;
+            const uint32_t behind = span.head + span.vectors * VEC;
+            const bool before = e < span.head, after = e >= behind;
+            uint32_t at = (e - span.head) / VEC - span.first;
+            bool here = at < vectors;
+            if (before) here = span.begins, at = vectors + e;
+            if (after) here = span.ends, at = vectors + S::LINE + (e - behind);
+            if (!here) return;
+            named[j] = Named{less, id, atomicExch(first_of + at, static_cast<uint32_t>(j))};
+        };
+        auto less_of = [&](float y) {
+            const float term = TeacherSum::term(y, teacher.most, a);
+            return term == 0.0f || teach == 0.0f ? 0.0f : share * term;
+        };
+        entries.each(w, lane, [&](int j, int id, float y, auto, int) { note(j, id, less_of(y)); });
+        if (lane == 0) {
+            note(a.top, label, tell);
+            teacher_sum = teacher.sum;
+        }
     }
     __syncthreads();
+    const float sum = teacher_sum;
+    // nothing to learn: the logits do not matter
+    const bool nothing = sum == 0.0f && label < 0;
+    const float origin = stats[0] == -INFINITY ? 0.0f : stats[0];
+    float factor = sum == 0.0f || stats[1] == 0.0f ? 0.0f : teach / stats[1];
+    const float factor_1 = stats[1] == 0.0f || label < 0 ? 0.0f : tell / stats[2];
+    if (POWER == 1) factor += factor_1;                                   // both at temperature 1, or no labels
     auto value = [&](float x) {
         const float d = x - origin, e = __builtin_amdgcn_exp2f(d * a.to_log2);
         return POWER == 1 ? factor * e : __builtin_fmaf(factor_1, power_of<POWER>(e, d), factor * e);
     };
-    const typename S::v* from = reinterpret_cast<const typename S::v*>(row + span.head);
-    uint32_t base = span.first + static_cast<uint32_t>(wave_index()) * kWave;
-    auto put = [&](uint32_t i, const typename S::v& q) {
+    // What more than two entries of a list take from element `id`, in the order of their places, whatever order the list has.
+    auto less_of = [&](uint32_t list, int id) {
+        float less = 0.0f;
+        for (uint32_t place = 0;; ++place) {
+            uint32_t next = kNoEntry;                                     // the first place from `place` on that the list has
+            for (uint32_t i = list; i != kNoEntry; i = named[i].next) next = i >= place ? min(next, i) : next;
+            if (next == kNoEntry) return less;
+            if (named[next].id == id) less += named[next].less;
+            place = next;
+        }
+    };
+    // N consecutive values, the first of them element `id`, less what their list takes.
+    auto take = [&](auto& v, uint32_t list, int id) {
+        constexpr int N = sizeof(v) / sizeof(v[0]);
+        float less[N] = {};
+        uint32_t once = 0, twice = 0, more = 0;
+        for (uint32_t i = list; i != kNoEntry;) {
+            const Named n = named[i];
+            const uint32_t at = static_cast<uint32_t>(n.id - id), bit = 1u << at;
+#pragma unroll
+            for (int e = 0; e < N; ++e) less[e] += at == static_cast<uint32_t>(e) ? n.less : 0.0f;
+            more |= twice & bit;
+            twice |= once & bit;
+            once |= bit;
+            i = n.next;
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] -= more >> e & 1u ? less_of(list, id + e) : less[e];
+    };
+    auto put = [&](uint32_t i, const typename S::v& x, uint32_t list) {
+        float v[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[e] = value(Elem<TYPE>::widen(x[e]));
+        if (list != kNoEntry) take(v, list, static_cast<int>(span.head + (span.first + i) * VEC));
         typename S::v o;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) o[e] = Elem<TYPE>::narrow(value(Elem<TYPE>::widen(q[e])));
-        __builtin_nontemporal_store(o, to + i);
+        for (int e = 0; e < VEC; ++e) o[e] = Elem<TYPE>::narrow(v[e]);
+        __builtin_nontemporal_store(nothing ? typename S::v(0) : o, to + i);
     };
-    for (; base + (UNROLL - 1) * THREADS + kWave <= span.last; base += UNROLL * THREADS) {
+    for (uint32_t base = static_cast<uint32_t>(wave) * kWave; base < vectors; base += UNROLL * THREADS) {
         typename S::v q[UNROLL];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) q[u] = __builtin_nontemporal_load(from + base + u * THREADS + lane);
+        for (int u = 0; u < UNROLL; ++u) q[u] = __builtin_nontemporal_load(from + min(base + u * THREADS + lane, vectors - 1));
+        uint32_t list[UNROLL];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) put(base + u * THREADS + lane, q[u]);
-    }
-    if (base < span.last) {
-        typename S::v q[UNROLL];
+        for (int u = 0; u < UNROLL; ++u) list[u] = first_of[min(base + u * THREADS + lane, vectors - 1)];
+        if (base + (UNROLL - 1) * THREADS + kWave <= vectors) {
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) q[u] = __builtin_nontemporal_load(from + min(base + u * THREADS + lane, span.last - 1));
+            for (int u = 0; u < UNROLL; ++u) put(base + u * THREADS + lane, q[u], list[u]);
+        } else {
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u)
-            if (base + u * THREADS + lane < span.last) put(base + u * THREADS + lane, q[u]);
+            for (int u = 0; u < UNROLL; ++u)
+                if (base + u * THREADS + lane < vectors) put(base + u * THREADS + lane, q[u], list[u]);
+        }
     }
-    if (alone < a.vocab) out[alone] = Elem<TYPE>::narrow(value(Elem<TYPE>::widen(row[alone])));
-    pace_loads();                                                         // what is out cannot overtake what is written over it
-    __syncthreads();
-    for (int j = static_cast<int>(threadIdx.x); j <= a.top; j += THREADS) {
-        const int id = named_id[j];
-        if (id < 0) continue;
-        float less = 0.0f;
-        for (int i = 0; i <= a.top; ++i) less += named_id[i] == id ? named_less[i] : 0.0f;
-        out[id] = Elem<TYPE>::narrow(value(named_x[j]) - less);
-    }
+    span.singles(threadIdx.x, THREADS, a.vocab, [&](uint32_t e, uint32_t place) {
+        float v[1] = {value(Elem<TYPE>::widen(row[e]))};
+        take(v, first_of[vectors + place], static_cast<int>(e));
+        out[e] = nothing ? one(0) : Elem<TYPE>::narrow(v[0]);
+    });
 }
 
 constexpr uint32_t kDistillThreads = 256;
-constexpr uint32_t kShortVocab = 4096;        // up to here a wave for each row
+// A wave for each row, where rows are short and many; otherwise a workgroup, whose waves share what a row waits for.  Wave | workgroup, bf16, loss and gradient:
+// 4096 x 1009 7.9 | 11.3 and 9.8 | 14.5 us, 4096 x 4001 13.0 | 16.1 and 19.6 | 21.3, 2048 x 1009 6.0 | 6.1 and 7.9 | 9.7, 2048 x 4001 9.9 | 9.2 and 14.5 | 14.0,
+// 1024 x 1009 5.7 | 5.6 and 7.0 | 6.7, 1024 x 4001 8.6 | 7.3 and 12.1 | 8.8.
+constexpr size_t kShortVocab = 4096, kManyRows = 2048;
 
-// Parts of a row: enough workgroups for the chip, and none shorter than is worth one.
-inline uint32_t distill_parts(size_t rows, size_t vocab, size_t shortest, size_t longest)
+// Parts of a row in the forward pass: enough workgroups for the chip, and none shorter than is worth one.
+inline uint32_t loss_parts(size_t rows, size_t vocab)
 {
-    size_t parts = (vocab + longest - 1) / longest;
-    const size_t wanted = rows ? (8 * static_cast<size_t>(kCus) + rows - 1) / rows : 1, most = (vocab + shortest - 1) / shortest;
-    parts = std::max(parts, std::min(wanted, most));
-    return static_cast<uint32_t>(std::max<size_t>(1, std::min<size_t>(parts, kMostParts)));
+    const size_t wanted = rows ? (8 * static_cast<size_t>(kCus) + rows - 1) / rows : 1;
+    return static_cast<uint32_t>(std::max<size_t>(1, std::min<size_t>({wanted, (vocab + 8191) / 8192, kMostParts})));
 }
-inline uint32_t loss_parts(size_t rows, size_t vocab) { return distill_parts(rows, vocab, 8192, static_cast<size_t>(1) << 40); }
-inline uint32_t grad_parts(size_t rows, size_t vocab) { return distill_parts(rows, vocab, 8192, 32768); }
+// In the backward pass: one batch of loads a workgroup, where rows are long; several (whole rows of 30522 or of 131072, 2 or 4 x as long) are slower than what looking at
+// the entries again costs: 4096 x 131072, bf16, 382 | 361 | 339 us with 32768 | 16384 | 8192 elements, 8 x 512 x 30522 106 | 97 | 98.
+constexpr size_t kGradPart = 8192;
+inline uint32_t grad_parts(size_t vocab) { return static_cast<uint32_t>((vocab + kGradPart - 1) / kGradPart); }
 
 struct DistillCall {
     int dtype;
@@ -469,6 +557,7 @@ inline int distill_check(const DistillCall& c, Lists<P>& ls, DistillArgs& a, Ran
     a.vocab = static_cast<uint32_t>(c.vocab);
     a.top = c.top, a.id_bytes = c.id_bytes, a.teacher_type = c.teacher_type, a.label_bytes = c.labels ? c.label_bytes : 0;
     a.temperature = static_cast<float>(c.temperature);
+    a.per_temperature = static_cast<float>(1.0 / c.temperature);
     a.to_log2 = static_cast<float>(1.44269504088896340736 / c.temperature);
     a.teacher_weight = static_cast<float>(c.teacher_weight);
     a.label_weight = static_cast<float>(c.label_weight);
@@ -477,11 +566,11 @@ inline int distill_check(const DistillCall& c, Lists<P>& ls, DistillArgs& a, Ran
 
 // f with the type, what power of an exponential at the teacher's temperature is one at 1, and the threads of a workgroup.
 template <typename F>
-inline void with_distill(int dtype, bool labels, double temperature, size_t vocab, const F& f)
+inline void with_distill(int dtype, bool labels, double temperature, size_t rows, size_t vocab, const F& f)
 {
     auto of_type = [&](auto type) {
         auto of_power = [&](auto power) {
-            if (vocab <= kShortVocab) f(type, power, std::integral_constant<int, kWave>());
+            if (vocab <= kShortVocab && rows >= kManyRows) f(type, power, std::integral_constant<int, kWave>());
             else f(type, power, std::integral_constant<int, kDistillThreads>());
         };
         if (!labels || temperature == 1.0) of_power(std::integral_constant<int, 1>());
@@ -539,7 +628,7 @@ extern "C" int bagua_distill_loss(int dtype, const void* const* logits, size_t l
     if (total * a.parts > kMaxGrid) return BAGUA_ERR_UNSUPPORTED;
     hipStream_t s = static_cast<hipStream_t>(stream);
     int status = BAGUA_OK;
-    with_distill(dtype, labels != nullptr, temperature, vocab, [&](auto type, auto power, auto threads) {
+    with_distill(dtype, labels != nullptr, temperature, total, vocab, [&](auto type, auto power, auto threads) {
         constexpr int TYPE = decltype(type)::value, POWER = decltype(power)::value, THREADS = decltype(threads)::value;
         launch_kernel(k_distill<TYPE, POWER, THREADS>, dim3(static_cast<uint32_t>(total) * a.parts), dim3(THREADS), 0, s, ls, a);
         status = launch_status();
@@ -582,12 +671,14 @@ extern "C" int bagua_distill_grad(int dtype, const void* const* logits, size_t l
     if (total == 0) return BAGUA_OK;
     a.out_ld = ld_out;
     a.up_per_row = upstream_per_row != 0;
-    a.parts = grad_parts(total, vocab);
+    a.parts = grad_parts(vocab);
     if (total * a.parts > kMaxGrid) return BAGUA_ERR_UNSUPPORTED;
     int status = BAGUA_OK;
-    with_distill(dtype, labels != nullptr, temperature, vocab, [&](auto type, auto power, auto threads) {
+    with_distill(dtype, labels != nullptr, temperature, total, vocab, [&](auto type, auto power, auto threads) {
         constexpr int TYPE = decltype(type)::value, POWER = decltype(power)::value, THREADS = decltype(threads)::value;
-        launch_kernel(k_distill_grad<TYPE, POWER, THREADS>, dim3(static_cast<uint32_t>(total) * a.parts), dim3(THREADS), static_cast<size_t>(top + 1) * 3 * sizeof(float),
+        typedef Span<TYPE, THREADS> S;
+        const size_t lists = S::part_vectors(a.vocab / S::VEC, a.parts) + S::SINGLES + 4;     // of a part at most, rounded up
+        launch_kernel(k_distill_grad<TYPE, POWER, THREADS>, dim3(static_cast<uint32_t>(total) * a.parts), dim3(THREADS), static_cast<size_t>(top + 1) * sizeof(Named) + lists * sizeof(uint32_t),
                       static_cast<hipStream_t>(stream), ls, a);
         status = launch_status();
     });

@@ -39,6 +39,13 @@ struct ListTile {
     __device__ __forceinline__ T* ptr(int p) const { return table_ptr<T>(reinterpret_cast<uintptr_t>(ls.at[p][worker])); }
 };
 
+constexpr float kLog2e = 1.44269504088896340736f;
+// exp(x) for x <= 0: the rounding of x * log2(e) and of log2(e) are made up for.
+__device__ __forceinline__ float exp_below(float x)
+{
+    const float t = x * kLog2e, off = __builtin_fmaf(x, 1.925963033500e-8f, __builtin_fmaf(x, kLog2e, -t)), e = __builtin_amdgcn_exp2f(t);
+    return t < -150.0f ? 0.0f : __builtin_fmaf(e, off * 0.693147180559945f, e);
+}
 // Cuts the workers' rows into tiles of `of` rows; the value: how many there are, or more than kMaxGrid.
 template <int P>
 inline uint64_t tiles_of(Lists<P>& ls, const size_t* rows, int k, uint32_t of)

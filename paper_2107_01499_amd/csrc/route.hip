@@ -57,7 +57,6 @@ __device__ __forceinline__ void unrolled_const(const F& f)
 }
 struct OpMaxU { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); } };
 
-constexpr float kLog2e = 1.44269504088896340736f;
 // To 2 units of its last place and as many as the size of x.
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
 
@@ -183,12 +182,6 @@ __device__ __forceinline__ T take(T (&key)[N], T none)
     return best;
 }
 
-// exp(x) for x <= 0: the rounding of x * log2(e) and of log2(e) are made up for.
-__device__ __forceinline__ float exp_below(float x)
-{
-    const float t = x * kLog2e, off = __builtin_fmaf(x, 1.925963033500e-8f, __builtin_fmaf(x, kLog2e, -t)), e = __builtin_amdgcn_exp2f(t);
-    return t < -150.0f ? 0.0f : __builtin_fmaf(e, off * 0.693147180559945f, e);
-}
 // What a choice weighs before sums: most is what softmax is relative to, and for sigmoid at most 0 and not below the largest of the choices' logits or 0.
 __device__ __forceinline__ float weight_of(float x, float most, bool softmax)
 {
