@@ -55,6 +55,7 @@ __device__ __forceinline__ void unrolled_const(const F& f)
         unrolled_const<N, I + 1>(f);
     }
 }
+struct OpAddU { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a + b; } };
 struct OpMaxU { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); } };
 
 // To 2 units of its last place and as many as the size of x.
@@ -68,13 +69,22 @@ __device__ __forceinline__ void wave_sync()
 }
 __device__ __forceinline__ uint32_t quotient(uint32_t i, uint32_t reciprocal) { return reciprocal ? __umulhi(i, reciprocal) : i; }
 
+// The largest of the wave, in every lane: exchanges in each row of 16, then the four rows.
 __device__ __forceinline__ uint64_t wave_max(uint64_t v)
 {
-    for (int d = 32; d > 0; d /= 2) {
-        const uint64_t o = __shfl_xor(v, d);
-        v = o > v ? o : v;
-    }
-    return v;
+    auto with = [&](auto exchange) {
+        const uint64_t o = static_cast<uint64_t>(exchange(static_cast<uint32_t>(v >> 32))) << 32 | exchange(static_cast<uint32_t>(v));
+        v = max(v, o);
+    };
+    with([](uint32_t x) { return dpp<kXor1>(x); });
+    with([](uint32_t x) { return dpp<kXor2>(x); });
+    with([](uint32_t x) { return dpp<kHalfMirror>(x); });
+    with([](uint32_t x) { return dpp<kMirror>(x); });
+    auto of_row = [&](int r) {
+        return static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v >> 32), 16 * r))) << 32 |
+               static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 16 * r));
+    };
+    return max(max(of_row(0), of_row(1)), max(of_row(2), of_row(3)));
 }
 
 // One row by the whole wave, in 64 bits; key: in LDS, one for every expert.  Leaves the choices as the fast way does: experts - id, and the logit.
@@ -201,6 +211,134 @@ __device__ __forceinline__ uint64_t lanes_of_row(int row) { return (L == 64 ? ~0
 
 constexpr int kFewChoices = 8;
 
+// The choice scores of a row in 32 bits, and what the weights need of it.
+template <int TYPE, int VEC, int L, int NV>
+struct Scores {
+    typedef Row<TYPE, VEC, L, NV> R;
+    float c[VEC * NV], top = -INFINITY, inverse = 1.0f, error = 0.0f;      // error: of a score, at most
+    __device__ __forceinline__ void form(const R& raw, const RouteArgs& a)
+    {
+        const bool softmax = a.score == BAGUA_SCORE_SOFTMAX;
+        if (a.by_logit && !(softmax && !a.renormalise)) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) c[j * VEC + i] = Elem<TYPE>::widen(raw.q[j][i]) + 0.0f;
+            return;
+        }
+        float e[1][NV][VEC], most[1];
+        most[0] = top = raw.largest(e[0]);
+        if (softmax) {
+            float own[NV][VEC];
+            R::owned(a.experts, own);
+            exponentials_of<R>(e, most, TYPE != BAGUA_F16);
+            inverse = R::reciprocal_sum(own, e[0]);
+            error = inverse * 0x1p-21f;
+        } else {
+            const float low = fminf(top, 0.0f);
+            error = sigmoid(low) * __builtin_fmaf(-low, 0x1p-23f, 0x1p-21f);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float bias[VEC] = {};
+            if (a.bias) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) bias[i] = a.bias[R::at(j, a.experts) + i];
+            }
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                c[j * VEC + i] = a.by_logit ? Elem<TYPE>::widen(raw.q[j][i]) + 0.0f : (softmax ? e[0][j][i] * inverse : sigmoid(e[0][j][i])) + bias[i];
+        }
+    }
+    __device__ __forceinline__ bool has_nan() const
+    {
+        bool nan = false;
+#pragma unroll
+        for (int i = 0; i < VEC * NV; i += 2) nan |= __builtin_isunordered(c[i], c[(i + 1) % (VEC * NV)]);
+        return nan;
+    }
+    // The same score, of one logit.
+    __device__ __forceinline__ float of(float x, uint32_t expert, const RouteArgs& a) const
+    {
+        if (a.by_logit) return x;
+        const float s = a.score == BAGUA_SCORE_SOFTMAX ? __builtin_amdgcn_exp2f((x - (top == -INFINITY ? 0.0f : top)) * kLog2e) * inverse : sigmoid(x);
+        return a.bias ? s + a.bias[expert] : s;
+    }
+};
+
+// The groups whose experts may be chosen, a bit for each, for the lane's row.  nan: the lane has one; uncertain: 32 bits cannot tell.  score_of: LDS of 64 / L
+// rows of scores (each group one further, so that lanes that go through different groups meet in no bank), group sums, and three words.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); }      // of numbers, one instruction wherever they come from
+__device__ __forceinline__ float smaller(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, -INFINITY); }
+template <int TYPE, int VEC, int L, int NV>
+__device__ __forceinline__ uint32_t groups_that_stay(const RouteArgs& a, const float (&c)[VEC * NV], float* score_of, int row, int in_row, float error, bool nan, bool& uncertain)
+{
+    typedef Row<TYPE, VEC, L, NV> R;
+    constexpr int RW = R::kRows;
+    const int lane = threadIdx.x & 63, experts = a.experts, wide = experts + a.groups;
+    float *good = score_of + RW * wide, *errors = good + RW * a.groups;
+    uint32_t* state = reinterpret_cast<uint32_t*>(errors + RW);                 // of every row: the groups that stay; whether that is not certain
+    const bool aligned = a.each % VEC == 0 && experts % VEC == 0;               // a vector is of one group
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const uint32_t at = static_cast<uint32_t>(R::at(j, experts)), g = quotient(at, a.per_each);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) score_of[row * wide + static_cast<int>(at + i + (aligned ? g : quotient(at + i, a.per_each)))] = c[j * VEC + i];
+    }
+    if (in_row == 0) state[row] = 0, state[RW + row] = 0, errors[row] = error;
+    wave_sync();
+    if (nan) state[RW + row] = 1;                                               // (64 bits know what to do)
+    const uint32_t pairs = static_cast<uint32_t>(RW * a.groups), at_once = kWave / a.part, sub = static_cast<uint32_t>(lane) & (a.part - 1);
+    for (uint32_t p0 = 0; p0 < pairs; p0 += at_once) {
+        const uint32_t pair = min(p0 + static_cast<uint32_t>(lane) / a.part, pairs - 1), r = quotient(pair, a.per_groups), g = pair - r * a.groups;
+        const float* of_group = score_of + r * wide + g * (a.each + 1);
+        float first = -INFINITY, second = -INFINITY;
+#pragma unroll 8
+        for (uint32_t i = sub; i < static_cast<uint32_t>(a.each); i += a.part) {
+            const float v = of_group[i];
+            second = __builtin_amdgcn_fmed3f(first, second, v);                 // (first >= second)
+            first = larger(first, v);
+        }
+        for (uint32_t d = 1; d < a.part; d *= 2) {
+            const float f = __shfl_xor(first, d), s = __shfl_xor(second, d);
+            second = larger(smaller(first, f), larger(second, s));
+            first = larger(first, f);
+        }
+        if (sub == 0) good[pair] = a.group_best == 2 ? first + second : first;
+    }
+    wave_sync();
+    for (uint32_t pair = lane; pair < pairs; pair += kWave) {
+        const uint32_t r = quotient(pair, a.per_groups), g = pair - r * a.groups;
+        const float mine = good[pair];
+        int before = 0, perhaps = 0;
+        if (a.by_logit) {                                                       // these are the logits themselves
+            for (uint32_t h = 0; h < static_cast<uint32_t>(a.groups); ++h) {
+                const float other = good[r * a.groups + h];
+                before += other > mine || (other == mine && h < g);
+            }
+            perhaps = before;
+        } else {
+            // (a group as close as that is of nearly this size)
+            const float apart = __builtin_fmaf(fabsf(mine), 0x1p-20f, 4.0f * errors[r]), above = mine + apart, below = mine - apart;
+            perhaps = -1;                                                       // itself
+#pragma unroll 8
+            for (uint32_t h = 0; h < static_cast<uint32_t>(a.groups); ++h) {
+                const float other = good[r * a.groups + h];
+                before += other > above;
+                perhaps += !(other < below);
+            }
+        }
+        if (perhaps < a.top_groups) atomicOr(state + r, 1u << g);
+        else if (before < a.top_groups) atomicOr(state + RW + r, 1u);
+    }
+    wave_sync();
+    uncertain |= state[RW + row] != 0;
+    const uint32_t allowed = state[row];
+    wave_sync();
+    return allowed;
+}
+
+
 // The forward pass for 16-bit logits that are themselves what experts are chosen by, and few choices.  A key is then the whole logit and the expert's
 // place in 32 bits.  Every lane sorts the keys of its part of a row, and the row's lanes take the largest of their first ones, one choice after another;
 // a choice stays in the lane that will write it.
@@ -320,40 +458,11 @@ k_route(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
     R raw;
     raw.load(x_row, experts, true);
     const bool counts = !t.has(kMask) || t.template ptr<const uint8_t>(kMask)[t.t0 + my_row] != 0;
-    float c[PER], top = -INFINITY, inverse = 1.0f, error = 0.0f;                // choice scores; error: of one, at most
-    if (a.by_logit && !(softmax && !a.renormalise)) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) c[j * VEC + i] = Elem<TYPE>::widen(raw.q[j][i]) + 0.0f;
-    } else {
-        float e[1][NV][VEC], most[1];
-        most[0] = top = raw.largest(e[0]);
-        if (softmax) {
-            float own[NV][VEC];
-            R::owned(experts, own);
-            exponentials_of<R>(e, most, TYPE != BAGUA_F16);
-            inverse = R::reciprocal_sum(own, e[0]);
-            error = inverse * 0x1p-21f;
-        } else {
-            const float low = fminf(top, 0.0f);
-            error = sigmoid(low) * __builtin_fmaf(-low, 0x1p-23f, 0x1p-21f);
-        }
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            float bias[VEC] = {};
-            if (a.bias) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) bias[i] = a.bias[R::at(j, experts) + i];
-            }
-#pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                c[j * VEC + i] = a.by_logit ? Elem<TYPE>::widen(raw.q[j][i]) + 0.0f : (softmax ? e[0][j][i] * inverse : sigmoid(e[0][j][i])) + bias[i];
-        }
-    }
-    bool nan = false;
-#pragma unroll
-    for (int i = 0; i < PER; i += 2) nan |= __builtin_isunordered(c[i], c[(i + 1) % PER]);
+    Scores<TYPE, VEC, L, NV> scores;
+    scores.form(raw, a);
+    auto& c = scores.c;
+    const float top = scores.top, inverse = scores.inverse, error = scores.error;
+    const bool nan = scores.has_nan();
     if (__any(nan)) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) c[i] = one_nan(c[i]);
@@ -363,65 +472,7 @@ k_route(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
     for (int i = 0; i < PER; ++i) key[i] = ordered_one_nan(c[i]);
     bool again = false;                                                         // the row needs 64 bits
     uint32_t allowed = 0xffffffffu;
-    if (a.groups > 1) {
-        uint32_t* score_of = more;
-        float* good = reinterpret_cast<float*>(more + RW * experts);
-        uint32_t* state = more + RW * experts + RW * a.groups;                  // of every row: the groups that stay; whether that is not certain
-        float* errors = reinterpret_cast<float*>(state + 2 * RW);
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) score_of[row * experts + R::at(j, experts) + i] = key[j * VEC + i];
-        if (in_row == 0) state[row] = 0, state[RW + row] = 0, errors[row] = error;
-        wave_sync();
-        const uint32_t pairs = static_cast<uint32_t>(RW * a.groups), at_once = kWave / a.part, sub = static_cast<uint32_t>(lane) & (a.part - 1);
-        for (uint32_t p0 = 0; p0 < pairs; p0 += at_once) {
-            const uint32_t pair = p0 + static_cast<uint32_t>(lane) / a.part, r = quotient(min(pair, pairs - 1), a.per_groups), g = min(pair, pairs - 1) - r * a.groups;
-            uint32_t first = 0, second = 0;
-#pragma unroll 8
-            for (uint32_t i = sub; i < static_cast<uint32_t>(a.each); i += a.part) {
-                const uint32_t v = score_of[r * experts + g * a.each + i];
-                second = max(second, min(first, v));
-                first = max(first, v);
-            }
-            for (uint32_t d = 1; d < a.part; d *= 2) {
-                const uint32_t f = __shfl_xor(first, d), s = __shfl_xor(second, d);
-                second = max(min(first, f), max(second, s));
-                first = max(first, f);
-            }
-            if (pair < pairs && sub == 0) good[pair] = a.group_best == 2 ? number(first) + number(second) : number(first);
-        }
-        wave_sync();
-        for (uint32_t pair = lane; pair < pairs; pair += kWave) {
-            const uint32_t r = quotient(pair, a.per_groups), g = pair - r * a.groups;
-            const float mine = good[pair];
-            int before = 0, perhaps = 0;
-            if (a.by_logit) {
-                const uint32_t o = ordered(mine);
-                for (uint32_t h = 0; h < static_cast<uint32_t>(a.groups); ++h) {
-                    const uint32_t other = ordered(good[r * a.groups + h]);
-                    before += other > o || (other == o && h < g);
-                }
-                perhaps = before;
-            } else {
-                // (a group as close as that is of nearly this size)
-                const float apart = __builtin_fmaf(fabsf(mine), 0x1p-20f, 4.0f * errors[r]), above = mine + apart, below = mine - apart;
-                perhaps = -1;                                                   // itself
-#pragma unroll 8
-                for (uint32_t h = 0; h < static_cast<uint32_t>(a.groups); ++h) {
-                    const float other = good[r * a.groups + h];
-                    before += other > above;
-                    perhaps += !(other < below);
-                }
-            }
-            if (perhaps < a.top_groups) atomicOr(state + r, 1u << g);
-            else if (before < a.top_groups) atomicOr(state + RW + r, 1u);
-        }
-        wave_sync();
-        allowed = state[row];
-        again = state[RW + row] != 0;
-        wave_sync();
-    }
+    if (a.groups > 1) allowed = groups_that_stay<TYPE, VEC, L, NV>(a, c, reinterpret_cast<float*>(more), row, in_row, error, nan, again);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int at = R::at(j, experts);
@@ -493,16 +544,10 @@ k_route(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
         // By the scores themselves, each candidate by how many are before it.  (Into another place: what a row's lanes have not come to is not moved.)
         float* score_of = reinterpret_cast<float*>(more) + row * slots;
         uint32_t *new_keys = more + RW * slots + row * slots, *new_logits = more + 2 * RW * slots + row * slots;
-        const float shift = -(top == -INFINITY ? 0.0f : top);
         for (int j = in_row; j < taken; j += L) {
             const uint32_t k = keys[j];
             const float x = logits[j];
-            float s = x;
-            if (!a.by_logit) {
-                s = softmax ? __builtin_amdgcn_exp2f((x + shift) * kLog2e) * inverse : sigmoid(x);
-                if (a.bias && k != 0) s = s + a.bias[static_cast<uint32_t>(experts) - k];
-            }
-            score_of[j] = s;
+            score_of[j] = k != 0 ? scores.of(x, static_cast<uint32_t>(experts) - k, a) : 0.0f;
         }
         wave_sync();
         for (int j = in_row; j < taken; j += L) {
@@ -566,6 +611,232 @@ k_route(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
         else t.template ptr<int32_t>(kIds)[token * a.ids_ld + j] = id;
         t.template ptr<float>(kWeights)[token * a.weights_ld + j] = counts ? logits[j] * factor : 0.0f;
     }
+}
+
+// The forward pass with 16 lanes a row and more, and few choices.  The k-th largest of the 16 largest scores of 16 parts of a row is not above the k-th
+// largest of all; what reaches it, less what 32 bits may be off by, are the candidates, some ten of a row.  They meet in LDS, one for each lane, and a
+// candidate's place is how many are better.  So no score is shortened and nothing sorted.
+constexpr int kCandidates = 16;
+template <int TYPE, int VEC, typename V>
+__device__ __forceinline__ float scores_logit(const V& v, int i)      // element i of a vector, where i is no constant
+{
+    typename Elem<TYPE>::one x = v[0];
+#pragma unroll
+    for (int e = 1; e < VEC; ++e) x = i == e ? v[e] : x;
+    return Elem<TYPE>::widen(x);
+}
+template <int L>
+__device__ __forceinline__ double lanes_sum(double v)                 // over the L >= 16 lanes of a row
+{
+    auto of = [](double x, auto exchange) {
+        const uint64_t b = __builtin_bit_cast(uint64_t, x);
+        return __builtin_bit_cast(double, static_cast<uint64_t>(exchange(static_cast<uint32_t>(b >> 32))) << 32 | exchange(static_cast<uint32_t>(b)));
+    };
+    v += of(v, [](uint32_t x) { return dpp<kXor1>(x); });
+    v += of(v, [](uint32_t x) { return dpp<kXor2>(x); });
+    v += of(v, [](uint32_t x) { return dpp<kHalfMirror>(x); });
+    v += of(v, [](uint32_t x) { return dpp<kMirror>(x); });
+    if (L >= 32) v += __shfl_xor(v, 16);
+    if (L >= 64) v += __shfl_xor(v, 32);
+    return v;
+}
+constexpr int kRor = 0x120;                // + n: the lane n places further in its row of 16, around its end
+template <int N, typename F>
+__device__ __forceinline__ void rotations(float v, const F& f)      // f(v of every other lane of the row of 16)
+{
+    if constexpr (N > 0) {
+        f(dpp<kRor + N>(v));
+        rotations<N - 1>(v, f);
+    }
+}
+template <int N, typename F>
+__device__ __forceinline__ void rotations(float v, uint32_t i, const F& f)
+{
+    if constexpr (N > 0) {
+        f(dpp<kRor + N>(v), dpp<kRor + N>(i));
+        rotations<N - 1>(v, i, f);
+    }
+}
+template <int TYPE, int VEC, int L, int NV>
+__global__ void __launch_bounds__(kWave * kRouteWaves)
+k_route_wide(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
+{
+    typedef Row<TYPE, VEC, L, NV> R;
+    typedef typename R::one one;
+    constexpr int RW = R::kRows, PER = VEC * NV;
+    static_assert(L >= kCandidates, "a lane for every candidate");
+    extern __shared__ uint64_t lds_of_waves[];
+    const int lane = threadIdx.x & 63, wave = wave_index(), row = lane / L, in_row = lane % L, experts = a.experts, top_k = a.top_k;
+    uint32_t* lds = reinterpret_cast<uint32_t*>(lds_of_waves) + static_cast<uint32_t>(wave) * a.wave_words;
+    float *found_score = reinterpret_cast<float*>(lds) + row * kCandidates, *found_logit = found_score + RW * kCandidates;
+    uint32_t *found = lds + 2 * RW * kCandidates + row * kCandidates, *count = lds + 3 * RW * kCandidates + row;
+    uint32_t* more = lds + 3 * RW * kCandidates + 4;                            // for the groups, or the keys of 64 bits
+    const uint32_t tile = blockIdx.x * (blockDim.x / kWave) + static_cast<uint32_t>(wave);
+    if (tile >= tiles) return;
+    const ListTile<kRouteLists> t(ls, tile, RW);
+    const bool softmax = a.score == BAGUA_SCORE_SOFTMAX;
+    const uint32_t my_row = min(static_cast<uint32_t>(row), t.rows - 1);
+    R raw;
+    raw.load(t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0 + my_row) * a.ld, experts, true);
+    const bool counts = !t.has(kMask) || t.template ptr<const uint8_t>(kMask)[t.t0 + my_row] != 0;
+    if (in_row == 0) *count = 0;
+    Scores<TYPE, VEC, L, NV> scores;
+    scores.form(raw, a);
+    auto& c = scores.c;
+    bool again = scores.has_nan();                                              // the row needs 64 bits
+    if (a.groups > 1) {
+        const uint32_t allowed = groups_that_stay<TYPE, VEC, L, NV>(a, c, reinterpret_cast<float*>(more), row, in_row, scores.error, again, again);
+        if (a.each % VEC == 0 && experts % VEC == 0) {                          // a vector is of one group
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const bool stays = allowed >> quotient(static_cast<uint32_t>(R::at(j, experts)), a.per_each) & 1u;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) c[j * VEC + i] = stays ? c[j * VEC + i] : -INFINITY;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    c[j * VEC + i] = allowed >> quotient(static_cast<uint32_t>(R::at(j, experts) + i), a.per_each) & 1u ? c[j * VEC + i] : -INFINITY;
+        }
+    }
+    if (experts != L * PER) {                                                   // the lanes behind a row's last element hold its last ones once more
+#pragma unroll
+        for (int j = NV / 2; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (R::at(j, experts) + i < R::slot(j)) c[j * VEC + i] = -INFINITY;
+    }
+    float best = c[0];
+#pragma unroll
+    for (int i = 1; i < PER; ++i) best = fmaxf(best, c[i]);
+    if (L >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(best), __float_as_uint(best), false, false);
+        best = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    if (L >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(best), __float_as_uint(best), false, false);
+        best = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    int better = 0;
+    rotations<15>(best, [&](float other) { better += other > best; });
+    const float bound = -lanes_most<16>(-(better < top_k ? best : INFINITY));
+    const float apart = a.by_logit ? 0.0f : __builtin_fmaf(fabsf(bound), 0x1p-21f, 2.0f * scores.error);
+    float least = bound - apart;
+    again |= !(least > -INFINITY);                                              // too few numbers
+    // How many of the row's scores reach x, and of the lane's own.
+    auto reach = [&](float x, int& own) {
+        own = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) own += c[i] >= x;
+        return static_cast<int>(lanes_reduce<L>(static_cast<uint32_t>(own), OpAddU()));
+    };
+    int mine = 0;
+    bool many = reach(least, mine) > kCandidates && !again;
+    if (__any(many)) {
+        // Parts that are not alike (groups that do not stay leave some empty): halving the way to the largest finds a better line.
+        float low = bound, high = lanes_most<16>(best);
+        for (int n = 0; n < 24 && __any(many); ++n) {
+            const float middle = 0.5f * low + 0.5f * high;
+            int own, unused;
+            const bool enough = reach(middle, unused) >= top_k, fits = reach(middle - apart, own) <= kCandidates;
+            if (many && enough && fits) least = middle - apart, mine = own, many = false;
+            if (enough) low = middle;
+            else high = middle;
+        }
+        again |= many;
+    }
+    if (again) mine = 0;
+    wave_sync();
+    uint32_t at = mine ? atomicAdd(count, static_cast<uint32_t>(mine)) : kCandidates;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (c[j * VEC + i] >= least && at < kCandidates) {
+                found_score[at] = c[j * VEC + i];
+                found_logit[at] = Elem<TYPE>::widen(raw.q[j][i]);
+                found[at] = static_cast<uint32_t>(R::at(j, experts) + i);
+                ++at;
+            }
+    wave_sync();
+    const uint32_t total = *count, candidate = static_cast<uint32_t>(lane) % kCandidates;
+    again |= total > kCandidates;
+    const bool is = candidate < total;
+    float score = is ? found_score[candidate] : -INFINITY, x = is ? found_logit[candidate] : -INFINITY;
+    uint32_t expert = is ? found[candidate] : 0;
+    const float near_by = __builtin_fmaf(fabsf(score), 0x1p-21f, 2.0f * scores.error);
+    int place = 0;
+    bool close = false;
+    if (a.by_logit) {                                                           // exact: equal ones are in order of their experts
+        rotations<15>(score, expert, [&](float other, uint32_t its) { place += other > score || (other == score && its < expert); });
+    } else {
+        rotations<15>(score, [&](float other) {
+            const float d = other - score;
+            place += d > 0.0f;
+            close |= fabsf(d) <= near_by;
+        });
+    }
+    if (__any(close && is)) {
+        // Too close to tell in 32 bits: the candidates' scores in 64.
+        double sum = 1.0;
+        const double most = scores.top == -INFINITY ? 0.0 : scores.top;
+        if (softmax) {
+            sum = 0.0;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll 1
+                for (int i = 0; i < VEC; ++i)
+                    if (R::at(j, experts) + i >= R::slot(j)) sum += exp(static_cast<double>(scores_logit<TYPE, VEC>(raw.q[j], i)) - most);
+            sum = lanes_sum<L>(sum);
+        }
+        double exact = -INFINITY;
+        if (is) {
+            exact = softmax ? (sum == 0.0 ? 0.0 : exp(static_cast<double>(x) - most) / sum) : 1.0 / (1.0 + exp(-static_cast<double>(x)));
+            if (a.bias) exact += static_cast<double>(a.bias[expert]);
+        }
+        double* scores_64 = reinterpret_cast<double*>(more) + row * kCandidates;
+        if (in_row < kCandidates) scores_64[candidate] = exact;
+        wave_sync();
+        place = 0;
+        for (uint32_t i = 0; i < kCandidates; ++i) {
+            const double other = scores_64[i];
+            place += i < total && (other > exact || (other == exact && found[i] < expert));
+        }
+        wave_sync();
+    }
+    if (!is) place = kCandidates;
+    again |= is && score == INFINITY;                                           // differences tell nothing
+    again = again && counts && static_cast<uint32_t>(row) < t.rows;
+    for (uint64_t left = __ballot(again); left != 0;) {
+        const int r = (__ffsll(static_cast<unsigned long long>(left)) - 1) / L;
+        left &= ~lanes_of_row<L>(r);
+        wave_sync();
+        choose_in_64<TYPE>(t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0 + static_cast<uint32_t>(r)) * a.ld, a, reinterpret_cast<uint64_t*>(more),
+                           lds, reinterpret_cast<float*>(lds) + kCandidates);   // (the candidates are in registers)
+        if (row == r) {
+            place = candidate < static_cast<uint32_t>(top_k) ? static_cast<int>(candidate) : kCandidates;
+            expert = candidate < static_cast<uint32_t>(top_k) ? static_cast<uint32_t>(experts) - lds[candidate] : 0;
+            x = candidate < static_cast<uint32_t>(top_k) ? reinterpret_cast<const float*>(lds)[kCandidates + candidate] : -INFINITY;
+        }
+    }
+    if (!counts) place = static_cast<int>(candidate);
+    // The weights, formed of the chosen logits.
+    const bool chosen = place < top_k;
+    float most = softmax ? scores.top : 0.0f;
+    if (a.renormalise) {
+        most = lanes_most<16>(chosen ? fmaxf(x, -INFINITY) : -INFINITY);
+        if (!softmax) most = fminf(most, 0.0f);
+    }
+    if (most == -INFINITY) most = INFINITY;                                     // nothing but -infinity: weights of 0
+    const float w = chosen ? weight_of(x, most, softmax) : 0.0f, factor = weight_factor(a, lanes_reduce<16>(w, OpAddF()), scores.inverse);
+    if (!chosen || in_row >= kCandidates || static_cast<uint32_t>(row) >= t.rows) return;
+    const size_t token = t.t0 + static_cast<uint32_t>(row);
+    const int32_t id = counts ? static_cast<int32_t>(expert) : -1;
+    if (a.id_bytes == 8) t.template ptr<int64_t>(kIds)[token * a.ids_ld + static_cast<size_t>(place)] = id;
+    else t.template ptr<int32_t>(kIds)[token * a.ids_ld + static_cast<size_t>(place)] = id;
+    t.template ptr<float>(kWeights)[token * a.weights_ld + static_cast<size_t>(place)] = counts ? w * factor : 0.0f;
 }
 
 // ---------------------------------------------------------------------------------------------- backward
@@ -747,13 +1018,33 @@ inline void with_lanes(int experts, const F& f)
     else if (experts <= 1024) f(RouteLayout<V, 64, N>());
     else f(RouteLayout<V, 64, 2 * N>());
 }
-template <typename F>
-inline void with_route_layout(int dtype, int experts, const F& f)
+// 16 lanes at least.
+template <int V, typename F>
+inline void with_many_lanes(int experts, const F& f)
 {
-    if (dtype == BAGUA_F32) with_lanes<4>(experts, [&](auto layout) { f(layout, std::integral_constant<int, BAGUA_F32>()); });
-    else if (dtype == BAGUA_BF16) with_lanes<8>(experts, [&](auto layout) { f(layout, std::integral_constant<int, BAGUA_BF16>()); });
-    else with_lanes<8>(experts, [&](auto layout) { f(layout, std::integral_constant<int, BAGUA_F16>()); });
+    constexpr int N = 16 / V;
+    if (experts <= 64) f(RouteLayout<4, 16, 1>());
+    else if (experts <= 128) f(RouteLayout<V, 16, N / 2>());
+    else if (experts <= 256) f(RouteLayout<V, 16, N>());
+    else if (experts <= 512) f(RouteLayout<V, 32, N>());
+    else if (experts <= 1024) f(RouteLayout<V, 64, N>());
+    else f(RouteLayout<V, 64, 2 * N>());
 }
+template <typename F>
+inline void with_route_layout(int dtype, int experts, bool wide, const F& f)
+{
+    auto of_type = [&](auto type) {
+        constexpr int V = decltype(type)::value == BAGUA_F32 ? 4 : 8;
+        if (wide) with_many_lanes<V>(experts, [&](auto layout) { f(layout, type, std::true_type()); });
+        else with_lanes<V>(experts, [&](auto layout) { f(layout, type, std::false_type()); });
+    };
+    if (dtype == BAGUA_F32) of_type(std::integral_constant<int, BAGUA_F32>());
+    else if (dtype == BAGUA_BF16) of_type(std::integral_constant<int, BAGUA_BF16>());
+    else of_type(std::integral_constant<int, BAGUA_F16>());
+}
+
+constexpr int kNarrowExperts = 128;
+constexpr size_t kFewTokens = 65536;
 
 // Waves of a workgroup whose LDS fits, and the grid.
 inline int route_waves(size_t wave_bytes)
@@ -819,10 +1110,15 @@ extern "C" int bagua_route(int dtype, const void* const* logits, size_t ld, cons
     a.index_mask = (1u << bits) - 1;
     a.per_each = reciprocal_of(a.each), a.per_groups = reciprocal_of(groups);
     int status = BAGUA_OK;
-    with_route_layout(dtype, experts, [&](auto layout, auto type) {
+    const bool few = top_k <= kFewChoices, whole_keys = a.by_logit && dtype != BAGUA_F32 && groups == 1;
+    size_t all = 0;
+    for (int w = 0; w < k; ++w) all += tokens[w];
+    const bool wide = few && !whole_keys && experts > 32 && (experts > kNarrowExperts || all <= kFewTokens);
+    with_route_layout(dtype, experts, wide, [&](auto layout, auto type, auto is_wide) {
         typedef decltype(layout) Lay;
         constexpr int TYPE = decltype(type)::value;
         constexpr uint32_t RW = kWave / Lay::L;
+        constexpr bool WIDE = decltype(is_wide)::value;
         const uint64_t tiles = tiles_of(ls, tokens, k, RW);
         if (tiles > kMaxGrid) {
             status = BAGUA_ERR_UNSUPPORTED;
@@ -837,17 +1133,27 @@ extern "C" int bagua_route(int dtype, const void* const* logits, size_t ld, cons
                           wave_bytes * static_cast<size_t>(waves), static_cast<hipStream_t>(stream), ls, a, static_cast<uint32_t>(tiles));
             status = launch_status();
         };
-        if constexpr (TYPE != BAGUA_F32) {
-            if (a.by_logit && groups == 1 && top_k <= kFewChoices) {
-                launch(k_route_16<TYPE, Lay::VEC, Lay::L, Lay::NV>, 0);
-                return;
+        const uint32_t columns = static_cast<uint32_t>(experts), for_groups = groups > 1 ? RW * (columns + 2 * static_cast<uint32_t>(groups) + 3) : 0;
+        if constexpr (WIDE) {
+            a.wave_words = (3 * RW * kCandidates + 4 + std::max({for_groups, 2 * columns, 2 * RW * kCandidates}) + 1) & ~1u;
+            launch(k_route_wide<TYPE, Lay::VEC, Lay::L, Lay::NV>, a.wave_words * sizeof(uint32_t));
+        } else {
+            if constexpr (TYPE != BAGUA_F32) {
+                if (whole_keys && few) {
+                    launch(k_route_16<TYPE, Lay::VEC, Lay::L, Lay::NV>, 0);
+                    return;
+                }
+            }
+            const uint32_t slots = RW * static_cast<uint32_t>(top_k + kMoreChoices);
+            a.wave_words = (2 * slots + std::max({for_groups, 2 * columns, 3 * slots}) + 1) & ~1u;
+            // (few choices of many experts have gone the other way, and more than few need more than few experts)
+            if constexpr (Lay::VEC * Lay::NV * Lay::L <= kNarrowExperts) {
+                if (few) launch(k_route<TYPE, Lay::VEC, Lay::L, Lay::NV, true>, a.wave_words * sizeof(uint32_t));
+            }
+            if constexpr (Lay::VEC * Lay::NV * Lay::L > kFewChoices) {
+                if (!few) launch(k_route<TYPE, Lay::VEC, Lay::L, Lay::NV, false>, a.wave_words * sizeof(uint32_t));
             }
         }
-        const uint32_t slots = RW * static_cast<uint32_t>(top_k + kMoreChoices), columns = static_cast<uint32_t>(experts);
-        const uint32_t for_groups = groups > 1 ? RW * (columns + static_cast<uint32_t>(groups) + 3) : 0;
-        a.wave_words = (2 * slots + std::max({for_groups, 2 * columns, 3 * slots}) + 1) & ~1u;
-        if (top_k <= kFewChoices) launch(k_route<TYPE, Lay::VEC, Lay::L, Lay::NV, true>, a.wave_words * sizeof(uint32_t));
-        else if constexpr (Lay::VEC * Lay::NV * Lay::L > kFewChoices) launch(k_route<TYPE, Lay::VEC, Lay::L, Lay::NV, false>, a.wave_words * sizeof(uint32_t));
     });
     return status;
 }
@@ -888,7 +1194,7 @@ extern "C" int bagua_route_grad(int dtype, const void* const* logits, size_t ld,
     a.ld = ld, a.ids_ld = ids_ld, a.weights_ld = weights_ld, a.up_ld = dweights_ld, a.out_ld = ld_out;
     a.experts = experts, a.top_k = top_k, a.score = score, a.renormalise = renormalise != 0, a.id_bytes = id_bytes, a.scale = static_cast<float>(scale);
     int status = BAGUA_OK;
-    with_route_layout(dtype, experts, [&](auto layout, auto type) {
+    with_route_layout(dtype, experts, false, [&](auto layout, auto type, auto) {
         typedef decltype(layout) Lay;
         constexpr int TYPE = decltype(type)::value;
         constexpr uint32_t RW = kWave / Lay::L;
