@@ -18,7 +18,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIBDIR = os.path.join(HERE, "lib")
 LIB = os.path.join(LIBDIR, "libbagua_hip.so")
-SOURCES = ["api.hip", "batch.hip", "minmax.hip", "sign.hip", "ring.hip", "flatten.hip", "fused.hip", "optim.hip", "topk.hip", "tensors.hip", "balance.hip", "route.hip", "distill.hip",
+SOURCES = ["route_bf16.hip", "route_f16.hip", "route_f32.hip", "ring.hip", "balance.hip",      # (these take longest)
+           "api.hip", "batch.hip", "minmax.hip", "sign.hip", "flatten.hip", "fused.hip", "optim.hip", "topk.hip", "tensors.hip", "route.hip", "distill.hip",
            "probe.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

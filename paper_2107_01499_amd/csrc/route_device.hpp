@@ -1,0 +1,1099 @@
+// Kernels of routing of tokens to experts and its backward pass (see bagua_hip.h), and their launches; every element type is built in a file of its own.
+//
+// A row of logits lies in L lanes as in rows.hpp.  Which experts are chosen has to be what numbers of 64 bits give, though the scores are formed in
+// 32: an element's key is its choice score, as an integer that is ordered as the numbers are, with the last bits replaced by how far its
+// expert lies from the last one, so that a maximum of keys is the best score and of equal ones the lowest expert.  Where two neighbours among
+// the chosen lie closer than the error of 32 bits (and are not the same logit with the same bias), the row is done again in 64 bits.
+#pragma once
+#include "route.hpp"
+#include "rows.hpp"
+
+#pragma clang fp contract(off)
+
+namespace bagua {
+
+constexpr int kRouteWaves = 4;
+constexpr int kMoreChoices = 4;               // rounds beyond the last choice that look for the end of a run of equal scores
+
+// Integers that are ordered as the numbers are; NaN above all, both zeros the same.
+__device__ __forceinline__ float one_nan(float x) { return x != x ? __builtin_nanf("") : x; }
+__device__ __forceinline__ uint32_t ordered_one_nan(float x)      // of a number that is no -0, and NaN without a sign
+{
+    const uint32_t b = __float_as_uint(x);
+    return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ uint32_t ordered(float x) { return ordered_one_nan(one_nan(x + 0.0f)); }
+__device__ __forceinline__ float number(uint32_t o) { return __uint_as_float(o ^ (static_cast<int32_t>(o) < 0 ? 0x80000000u : 0xffffffffu)); }
+__device__ __forceinline__ uint64_t ordered(double x)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, x + 0.0);
+    return x != x ? ~0ull : b ^ (static_cast<uint64_t>(static_cast<int64_t>(b) >> 63) | 1ull << 63);
+}
+__device__ __forceinline__ double number(uint64_t o) { return __builtin_bit_cast(double, o ^ (static_cast<int64_t>(o) < 0 ? 1ull << 63 : ~0ull)); }
+
+// f(std::integral_constant<int, 0>()), ..., N - 1
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void unrolled_const(const F& f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        unrolled_const<N, I + 1>(f);
+    }
+}
+struct OpAddU { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a + b; } };
+struct OpMaxU { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); } };
+
+// To 2 units of its last place and as many as the size of x.
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
+
+// Lanes of a wave wait for what others of it have written to LDS.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+__device__ __forceinline__ uint32_t quotient(uint32_t i, uint32_t reciprocal) { return reciprocal ? __umulhi(i, reciprocal) : i; }
+
+// The largest of the wave, in every lane: exchanges in each row of 16, then the four rows.
+__device__ __forceinline__ uint64_t wave_max(uint64_t v)
+{
+    auto with = [&](auto exchange) {
+        const uint64_t o = static_cast<uint64_t>(exchange(static_cast<uint32_t>(v >> 32))) << 32 | exchange(static_cast<uint32_t>(v));
+        v = max(v, o);
+    };
+    with([](uint32_t x) { return dpp<kXor1>(x); });
+    with([](uint32_t x) { return dpp<kXor2>(x); });
+    with([](uint32_t x) { return dpp<kHalfMirror>(x); });
+    with([](uint32_t x) { return dpp<kMirror>(x); });
+    auto of_row = [&](int r) {
+        return static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v >> 32), 16 * r))) << 32 |
+               static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 16 * r));
+    };
+    return max(max(of_row(0), of_row(1)), max(of_row(2), of_row(3)));
+}
+
+// One row by the whole wave, in 64 bits; key: in LDS, one for every expert.  Leaves the choices as the fast way does: experts - id, and the logit.
+template <int TYPE>
+__device__ __forceinline__ void choose_in_64(const typename Elem<TYPE>::one* row, const RouteArgs& a, uint64_t* key, uint32_t* chosen, float* logit)
+{
+    const int lane = threadIdx.x & 63;
+    double most = -INFINITY, sum = 0.0;
+    if (!a.by_logit && a.score == BAGUA_SCORE_SOFTMAX) {
+        float top = -INFINITY;
+        for (int e = lane; e < a.experts; e += kWave) top = fmaxf(top, Elem<TYPE>::widen(row[e]));
+        most = lanes_most<kWave>(top);
+        if (most == -INFINITY) most = 0.0;                   // nothing but -infinity: all scores are 0
+        for (int e = lane; e < a.experts; e += kWave) sum += exp(static_cast<double>(Elem<TYPE>::widen(row[e])) - most);
+        sum = wave_sum(sum);
+    }
+    for (int e = lane; e < a.experts; e += kWave) {
+        const double x = Elem<TYPE>::widen(row[e]);
+        double c = x;
+        if (!a.by_logit) {
+            c = a.score == BAGUA_SCORE_SOFTMAX ? (sum == 0.0 ? 0.0 : exp(x - most) / sum) : 1.0 / (1.0 + exp(-x));
+            if (a.bias) c += static_cast<double>(a.bias[e]);
+        }
+        key[e] = ordered(c);
+    }
+    wave_sync();
+    if (a.groups > 1) {
+        double good = 0.0;
+        if (lane < a.groups) {
+            uint64_t first = 0, second = 0;
+            for (int i = 0; i < a.each; ++i) {
+                const uint64_t v = key[lane * a.each + i];
+                second = max(second, min(first, v));
+                first = max(first, v);
+            }
+            good = a.group_best == 2 ? number(first) + number(second) : number(first);
+        }
+        const uint64_t mine = ordered(good);
+        int better = 0;
+        for (int g = 0; g < a.groups; ++g) {
+            const uint64_t o = __shfl(mine, g);
+            better += o > mine || (o == mine && g < lane);
+        }
+        const uint64_t allowed = __ballot(lane < a.groups && better < a.top_groups);
+        for (int e = lane; e < a.experts; e += kWave)
+            if (!(allowed >> quotient(static_cast<uint32_t>(e), a.per_each) & 1)) key[e] = 0;
+        wave_sync();
+    }
+    for (int j = 0; j < a.top_k; ++j) {
+        uint64_t best = 0;
+        uint32_t at = 0xffffffffu;
+        for (int e = lane; e < a.experts; e += kWave) {
+            const uint64_t v = key[e];
+            if (v > best) best = v, at = static_cast<uint32_t>(e);
+        }
+        const uint64_t of_all = wave_max(best);
+        at = ~lanes_reduce<kWave>(best == of_all ? ~at : 0u, OpMaxU());    // the lowest of those that are as good
+        if (lane == 0) {
+            key[at] = 0;
+            chosen[j] = static_cast<uint32_t>(a.experts) - at;
+            logit[j] = Elem<TYPE>::widen(row[at]);
+        }
+        wave_sync();
+    }
+}
+
+// Sorts N keys, the largest first, by a fixed network (odd-even merging of sorted halves, Batcher 1968); what no one asks for afterwards is not computed.
+template <int P, int K, int I, typename T, int N>
+__device__ __forceinline__ void sort_step(T (&v)[N])     // exchanges at distance K on the way to sorted runs of 2 P
+{
+    if constexpr (I + K < N) {
+        if constexpr (I >= K % P && (I - K % P) / K % 2 == 0 && I / (2 * P) == (I + K) / (2 * P)) {
+            const T x = v[I], y = v[I + K];
+            v[I] = max(x, y);
+            v[I + K] = min(x, y);
+        }
+        sort_step<P, K, I + 1>(v);
+    } else if constexpr (K > 1) {
+        sort_step<P, K / 2, 0>(v);
+    } else if constexpr (2 * P < N) {
+        sort_step<2 * P, 2 * P, 0>(v);
+    }
+}
+template <typename T, int N>
+__device__ __forceinline__ void sort_keys(T (&v)[N])
+{
+    if constexpr (N > 1) sort_step<1, 1, 0>(v);
+}
+// The first AHEAD of the keys move up one place where `here` is true.
+template <int AHEAD, int I, typename T, int N>
+__device__ __forceinline__ void move_up(T (&v)[N], bool here, T none)
+{
+    if constexpr (I < AHEAD && I < N) {
+        if constexpr (I + 1 < N) v[I] = here ? v[I + 1] : v[I];
+        else v[I] = here ? none : v[I];
+        move_up<AHEAD, I + 1>(v, here, none);
+    }
+}
+// Takes the largest key of a row's lanes, whose keys are sorted.  AHEAD: how many more will be asked for.
+template <int L, int AHEAD, typename OP, typename T, int N>
+__device__ __forceinline__ T take(T (&key)[N], T none)
+{
+    const T best = static_cast<T>(lanes_reduce<L>(static_cast<uint32_t>(key[0]), OP()));
+    move_up<AHEAD, 0>(key, key[0] == best, none);
+    return best;
+}
+
+// What a choice weighs before sums: most is what softmax is relative to, and for sigmoid at most 0 and not below the largest of the choices' logits or 0.
+__device__ __forceinline__ float weight_of(float x, float most, bool softmax)
+{
+    if (softmax) return exp_below(x - most);
+    const float far = exp_below(-fabsf(x)), s = x <= 0.0f ? exp_below(x - most) : 1.0f;
+    const float w = s / (1.0f + far);
+    return x != x ? x : w;
+}
+// The weights' common factor from their sum.
+__device__ __forceinline__ float weight_factor(const RouteArgs& a, float sum, float inverse)
+{
+    if (a.renormalise) return inverse != inverse ? inverse : sum == 0.0f ? 0.0f : a.scale / sum;
+    return a.score == BAGUA_SCORE_SOFTMAX ? inverse * a.scale : a.scale;
+}
+template <int L>
+__device__ __forceinline__ uint64_t lanes_of_row(int row) { return (L == 64 ? ~0ull : (1ull << (L & 63)) - 1) << (row * L & 63); }
+
+constexpr int kFewChoices = 8;
+
+// The choice scores of a row in 32 bits, and what the weights need of it.
+template <int TYPE, int VEC, int L, int NV>
+struct Scores {
+    typedef Row<TYPE, VEC, L, NV> R;
+    float c[VEC * NV], top = -INFINITY, inverse = 1.0f, error = 0.0f;      // error: of a score, at most
+    __device__ __forceinline__ void form(const R& raw, const RouteArgs& a)
+    {
+        const bool softmax = a.score == BAGUA_SCORE_SOFTMAX;
+        if (a.by_logit && !(softmax && !a.renormalise)) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) c[j * VEC + i] = Elem<TYPE>::widen(raw.q[j][i]) + 0.0f;
+            return;
+        }
+        float e[1][NV][VEC], most[1];
+        most[0] = top = raw.largest(e[0]);
+        if (softmax) {
+            float own[NV][VEC];
+            R::owned(a.experts, own);
+            exponentials_of<R>(e, most, TYPE != BAGUA_F16);
+            inverse = R::reciprocal_sum(own, e[0]);
+            error = inverse * 0x1p-21f;
+        } else {
+            const float low = fminf(top, 0.0f);
+            error = sigmoid(low) * __builtin_fmaf(-low, 0x1p-23f, 0x1p-21f);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float bias[VEC] = {};
+            if (a.bias) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) bias[i] = a.bias[R::at(j, a.experts) + i];
+            }
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                c[j * VEC + i] = a.by_logit ? Elem<TYPE>::widen(raw.q[j][i]) + 0.0f : (softmax ? e[0][j][i] * inverse : sigmoid(e[0][j][i])) + bias[i];
+        }
+    }
+    __device__ __forceinline__ bool has_nan() const
+    {
+        bool nan = false;
+#pragma unroll
+        for (int i = 0; i < VEC * NV; i += 2) nan |= __builtin_isunordered(c[i], c[(i + 1) % (VEC * NV)]);
+        return nan;
+    }
+    // The same score, of one logit.
+    __device__ __forceinline__ float of(float x, uint32_t expert, const RouteArgs& a) const
+    {
+        if (a.by_logit) return x;
+        const float s = a.score == BAGUA_SCORE_SOFTMAX ? __builtin_amdgcn_exp2f((x - (top == -INFINITY ? 0.0f : top)) * kLog2e) * inverse : sigmoid(x);
+        return a.bias ? s + a.bias[expert] : s;
+    }
+};
+
+// The groups whose experts may be chosen, a bit for each, for the lane's row.  nan: the lane has one; uncertain: 32 bits cannot tell.  score_of: LDS of 64 / L
+// rows of scores (each group one further, so that lanes that go through different groups meet in no bank), group sums, and three words.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); }      // of numbers, one instruction wherever they come from
+__device__ __forceinline__ float smaller(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, -INFINITY); }
+template <int TYPE, int VEC, int L, int NV>
+__device__ __forceinline__ uint32_t groups_that_stay(const RouteArgs& a, const float (&c)[VEC * NV], float* score_of, int row, int in_row, float error, bool nan, bool& uncertain)
+{
+    typedef Row<TYPE, VEC, L, NV> R;
+    constexpr int RW = R::kRows;
+    const int lane = threadIdx.x & 63, experts = a.experts, wide = experts + a.groups;
+    float *good = score_of + RW * wide, *errors = good + RW * a.groups;
+    uint32_t* state = reinterpret_cast<uint32_t*>(errors + RW);                 // of every row: the groups that stay; whether that is not certain
+    const bool aligned = a.each % VEC == 0 && experts % VEC == 0;               // a vector is of one group
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const uint32_t at = static_cast<uint32_t>(R::at(j, experts)), g = quotient(at, a.per_each);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) score_of[row * wide + static_cast<int>(at + i + (aligned ? g : quotient(at + i, a.per_each)))] = c[j * VEC + i];
+    }
+    if (in_row == 0) state[row] = 0, state[RW + row] = 0, errors[row] = error;
+    wave_sync();
+    if (nan) state[RW + row] = 1;                                               // (64 bits know what to do)
+    const uint32_t pairs = static_cast<uint32_t>(RW * a.groups), at_once = kWave / a.part, sub = static_cast<uint32_t>(lane) & (a.part - 1);
+    for (uint32_t p0 = 0; p0 < pairs; p0 += at_once) {
+        const uint32_t pair = min(p0 + static_cast<uint32_t>(lane) / a.part, pairs - 1), r = quotient(pair, a.per_groups), g = pair - r * a.groups;
+        const float* of_group = score_of + r * wide + g * (a.each + 1);
+        float first = -INFINITY, second = -INFINITY;
+#pragma unroll 8
+        for (uint32_t i = sub; i < static_cast<uint32_t>(a.each); i += a.part) {
+            const float v = of_group[i];
+            second = __builtin_amdgcn_fmed3f(first, second, v);                 // (first >= second)
+            first = larger(first, v);
+        }
+        for (uint32_t d = 1; d < a.part; d *= 2) {
+            const float f = __shfl_xor(first, d), s = __shfl_xor(second, d);
+            second = larger(smaller(first, f), larger(second, s));
+            first = larger(first, f);
+        }
+        if (sub == 0) good[pair] = a.group_best == 2 ? first + second : first;
+    }
+    wave_sync();
+    for (uint32_t pair = lane; pair < pairs; pair += kWave) {
+        const uint32_t r = quotient(pair, a.per_groups), g = pair - r * a.groups;
+        const float mine = good[pair];
+        int before = 0, perhaps = 0;
+        if (a.by_logit) {                                                       // these are the logits themselves
+            for (uint32_t h = 0; h < static_cast<uint32_t>(a.groups); ++h) {
+                const float other = good[r * a.groups + h];
+                before += other > mine || (other == mine && h < g);
+            }
+            perhaps = before;
+        } else {
+            // (a group as close as that is of nearly this size)
+            const float apart = __builtin_fmaf(fabsf(mine), 0x1p-20f, 4.0f * errors[r]), above = mine + apart, below = mine - apart;
+            perhaps = -1;                                                       // itself
+#pragma unroll 8
+            for (uint32_t h = 0; h < static_cast<uint32_t>(a.groups); ++h) {
+                const float other = good[r * a.groups + h];
+                before += other > above;
+                perhaps += !(other < below);
+            }
+        }
+        if (perhaps < a.top_groups) atomicOr(state + r, 1u << g);
+        else if (before < a.top_groups) atomicOr(state + RW + r, 1u);
+    }
+    wave_sync();
+    uncertain |= state[RW + row] != 0;
+    const uint32_t allowed = state[row];
+    wave_sync();
+    return allowed;
+}
+
+
+// The forward pass for 16-bit logits that are themselves what experts are chosen by, and few choices.  A key is then the whole logit and the expert's
+// place in 32 bits.  Every lane sorts the keys of its part of a row, and the row's lanes take the largest of their first ones, one choice after another;
+// a choice stays in the lane that will write it.
+template <int TYPE, int VEC, int L, int NV>
+__global__ void __launch_bounds__(kWave * kRouteWaves)
+k_route_16(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
+{
+    typedef Row<TYPE, VEC, L, NV> R;
+    typedef typename R::one one;
+    constexpr int RW = R::kRows, PER = VEC * NV, MINE = (kFewChoices + L - 1) / L;
+    constexpr int32_t kNone = INT32_MIN;
+    constexpr uint32_t kInf = TYPE == BAGUA_BF16 ? 0x7f80 : 0x7c00;
+    const int lane = threadIdx.x & 63, row = lane / L, in_row = lane % L, experts = a.experts, top_k = a.top_k;
+    const uint32_t tile = blockIdx.x * (blockDim.x / kWave) + static_cast<uint32_t>(wave_index());
+    if (tile >= tiles) return;
+    const ListTile<kRouteLists> t(ls, tile, RW);
+    const uint32_t my_row = min(static_cast<uint32_t>(row), t.rows - 1);
+    R raw;
+    raw.load(t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0 + my_row) * a.ld, experts, true);
+    const bool counts = !t.has(kMask) || t.template ptr<const uint8_t>(kMask)[t.t0 + my_row] != 0, softmax = a.score == BAGUA_SCORE_SOFTMAX;
+    int32_t key[PER];
+    // Sign and magnitude to two's complement, two elements at a time: both zeros are 0 then, and NaN is the largest, if it has no sign.
+    typedef int16_t s2 __attribute__((ext_vector_type(2)));
+    typedef uint16_t u2 __attribute__((ext_vector_type(2)));
+    u2 most_bits = {0, 0};
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < VEC; i += 2) {
+            s2 q = {static_cast<int16_t>(raw.q[j][i]), static_cast<int16_t>(VEC > 1 ? raw.q[j][(i + 1) % VEC] : 0)};
+            const s2 sign = q >> 15, size = q & static_cast<int16_t>(0x7fff);
+            most_bits = __builtin_elementwise_max(most_bits, __builtin_bit_cast(u2, size));
+            const uint32_t both = __builtin_bit_cast(uint32_t, (size ^ sign) - sign), place = static_cast<uint32_t>(experts - R::at(j, experts) - i);
+            key[j * VEC + i] = static_cast<int32_t>(both << 16 | place);
+            if (VEC > 1) key[j * VEC + (i + 1) % VEC] = static_cast<int32_t>((both & 0xffff0000u) | (place - 1));
+        }
+    if (__any(max(most_bits[0], most_bits[1]) > kInf)) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if ((raw.q[j][i] & 0x7fff) > kInf) key[j * VEC + i] = 0x7fff0000 | (key[j * VEC + i] & 0xffff);
+    }
+    if (experts != L * PER) {                                   // the lanes behind a row's last element hold its last ones once more
+#pragma unroll
+        for (int j = NV / 2; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (R::at(j, experts) + i < R::slot(j)) key[j * VEC + i] = kNone;
+    }
+    sort_keys(key);
+    int32_t mine[MINE], first = 0;
+#pragma unroll
+    for (int m = 0; m < MINE; ++m) mine[m] = 0;
+    unrolled_const<kFewChoices>([&](auto j) {
+        constexpr int J = decltype(j)::value;
+        if (J < top_k) {
+            const int32_t best = take<L, kFewChoices - 1 - J, OpMaxI>(key, kNone);
+            if (J == 0) first = best;
+            mine[J / L] = in_row == J % L ? best : mine[J / L];
+        }
+    });
+    auto logit = [](int32_t k) {
+        const int32_t o = k >> 16;
+        return Elem<TYPE>::widen(static_cast<uint16_t>(o < 0 ? 0x8000 | -o : o));
+    };
+    float top = logit(first), inverse = 1.0f;                   // the row's largest, too; NaN if there is one
+    if (softmax && !a.renormalise) {
+        float e[1][NV][VEC], most[1], own[NV][VEC];
+        R::owned(experts, own);
+        most[0] = raw.largest(e[0]);
+        exponentials_of<R>(e, most, TYPE != BAGUA_F16);
+        inverse = R::reciprocal_sum(own, e[0]);
+    }
+    const float most = !softmax ? (a.renormalise ? fminf(top, 0.0f) : 0.0f) : top, from = most == -INFINITY ? INFINITY : most;
+    float w[MINE], sum = 0.0f;
+#pragma unroll
+    for (int m = 0; m < MINE; ++m) {
+        w[m] = weight_of(logit(mine[m]), from, softmax);
+        sum += m * L + in_row < top_k ? w[m] : 0.0f;
+    }
+    const float factor = weight_factor(a, lanes_reduce<L>(sum, OpAddF()), inverse);
+    if (static_cast<uint32_t>(row) >= t.rows) return;
+    const size_t token = t.t0 + static_cast<uint32_t>(row);
+#pragma unroll
+    for (int m = 0; m < MINE; ++m) {
+        const int j = m * L + in_row;
+        if (j >= top_k) continue;
+        const int32_t id = counts ? experts - (mine[m] & 0xffff) : -1;
+        if (a.id_bytes == 8) t.template ptr<int64_t>(kIds)[token * a.ids_ld + j] = id;
+        else t.template ptr<int32_t>(kIds)[token * a.ids_ld + j] = id;
+        t.template ptr<float>(kWeights)[token * a.weights_ld + j] = counts ? w[m] * factor : 0.0f;
+    }
+}
+
+// The forward pass of everything else.  As above, but a key has lost the last bits of its score to the expert's place: some runners-up are taken too, and
+// the candidates put in order by their scores in 32 bits where two keys are close.  FEW: at most kFewChoices.
+template <int TYPE, int VEC, int L, int NV, bool FEW>
+__global__ void __launch_bounds__(kWave * kRouteWaves)
+k_route(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
+{
+    typedef Row<TYPE, VEC, L, NV> R;
+    typedef typename R::one one;
+    constexpr int RW = R::kRows, PER = VEC * NV;
+    extern __shared__ uint64_t lds_of_waves[];
+    const int lane = threadIdx.x & 63, wave = wave_index(), row = lane / L, in_row = lane % L, experts = a.experts, top_k = a.top_k, slots = top_k + kMoreChoices;
+    uint32_t* lds = reinterpret_cast<uint32_t*>(lds_of_waves) + static_cast<uint32_t>(wave) * a.wave_words;
+    uint32_t* keys = lds + row * slots;                                          // the candidates, as keys and then as experts - id
+    float* logits = reinterpret_cast<float*>(lds + RW * slots) + row * slots;    // theirs; at last the weights
+    uint32_t* more = lds + 2 * RW * slots;                                       // for the groups, the candidates' order, or the keys of 64 bits
+    const uint32_t tile = blockIdx.x * (blockDim.x / kWave) + static_cast<uint32_t>(wave), index_mask = a.index_mask;
+    if (tile >= tiles) return;
+    const ListTile<kRouteLists> t(ls, tile, RW);
+    const bool softmax = a.score == BAGUA_SCORE_SOFTMAX;
+    const uint32_t my_row = min(static_cast<uint32_t>(row), t.rows - 1);
+    const one* x_row = t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0 + my_row) * a.ld;
+    R raw;
+    raw.load(x_row, experts, true);
+    const bool counts = !t.has(kMask) || t.template ptr<const uint8_t>(kMask)[t.t0 + my_row] != 0;
+    Scores<TYPE, VEC, L, NV> scores;
+    scores.form(raw, a);
+    auto& c = scores.c;
+    const float top = scores.top, inverse = scores.inverse, error = scores.error;
+    const bool nan = scores.has_nan();
+    if (__any(nan)) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c[i] = one_nan(c[i]);
+    }
+    uint32_t key[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) key[i] = ordered_one_nan(c[i]);
+    bool again = false;                                                         // the row needs 64 bits
+    uint32_t allowed = 0xffffffffu;
+    if (a.groups > 1) allowed = groups_that_stay<TYPE, VEC, L, NV>(a, c, reinterpret_cast<float*>(more), row, in_row, error, nan, again);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int at = R::at(j, experts);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) key[j * VEC + i] = (key[j * VEC + i] & ~index_mask) | static_cast<uint32_t>(experts - at - i);
+        if (a.groups > 1) {
+            if (a.each % VEC == 0 && experts % VEC == 0) {                      // a vector is of one group
+                const uint32_t stays = 0u - (allowed >> quotient(static_cast<uint32_t>(at), a.per_each) & 1u);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) key[j * VEC + i] &= stays;
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) key[j * VEC + i] &= 0u - (allowed >> quotient(static_cast<uint32_t>(at + i), a.per_each) & 1u);
+            }
+        }
+    }
+    if (experts != L * PER) {                                                   // the lanes behind a row's last element hold its last ones once more
+#pragma unroll
+        for (int j = NV / 2; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (R::at(j, experts) + i < R::slot(j)) key[j * VEC + i] = 0;
+    }
+    sort_keys(key);
+    // Scores of two keys, the better one first, cannot be told apart by the keys.
+    auto close = [&](uint32_t better, uint32_t worse) {
+        if (worse == 0) return false;                                           // there is none
+        if (a.by_logit) return (better & ~index_mask) == (worse & ~index_mask);
+        const float b = number(better & ~index_mask), w = number(worse & ~index_mask);
+        return !(b - w > __builtin_fmaf(fmaxf(fabsf(b), fabsf(w)), __builtin_fmaf(static_cast<float>(index_mask), 0x1p-22f, 0x1p-21f), 2.0f * error));
+    };
+    uint32_t last = 0;
+    int taken = top_k;
+    if (FEW) {
+        unrolled_const<kFewChoices>([&](auto j) {
+            constexpr int J = decltype(j)::value;
+            if (J < top_k) {
+                last = take<L, kFewChoices - 1 - J + kMoreChoices, OpMaxU>(key, 0u);
+                if (in_row == 0) keys[J] = last;
+            }
+        });
+    } else {
+        for (int j = 0; j < top_k; ++j) {
+            last = take<L, PER, OpMaxU>(key, 0u);
+            if (in_row == 0) keys[j] = last;
+        }
+    }
+    // Runners-up, until one is so far behind that what the keys left out cannot matter.
+    bool ends = false;
+    for (int j = 0; j < kMoreChoices; ++j) {
+        const uint32_t next = take<L, PER, OpMaxU>(key, 0u);
+        if (in_row == 0) keys[taken] = next;
+        ++taken;
+        ends = ends || !close(last, next);
+        if (__all(ends)) break;
+    }
+    again = again || !ends;
+    wave_sync();
+    bool order = false;
+    for (int j = in_row; j < taken; j += L) {
+        const uint32_t k = keys[j];
+        order |= j + 1 < taken && close(k, keys[j + 1]);
+        logits[j] = k != 0 ? Elem<TYPE>::widen(x_row[static_cast<uint32_t>(experts) - (k & index_mask)]) : 0.0f;
+    }
+    wave_sync();
+    for (int j = in_row; j < taken; j += L) keys[j] &= index_mask;
+    wave_sync();
+    if (__any(order)) {
+        // By the scores themselves, each candidate by how many are before it.  (Into another place: what a row's lanes have not come to is not moved.)
+        float* score_of = reinterpret_cast<float*>(more) + row * slots;
+        uint32_t *new_keys = more + RW * slots + row * slots, *new_logits = more + 2 * RW * slots + row * slots;
+        for (int j = in_row; j < taken; j += L) {
+            const uint32_t k = keys[j];
+            const float x = logits[j];
+            score_of[j] = k != 0 ? scores.of(x, static_cast<uint32_t>(experts) - k, a) : 0.0f;
+        }
+        wave_sync();
+        for (int j = in_row; j < taken; j += L) {
+            const uint32_t mine = keys[j];
+            if (mine == 0) continue;
+            const float x = logits[j], s = score_of[j];
+            const uint32_t o = ordered(s);
+            int before = 0;
+            bool near = false;
+            for (int i = 0; i < taken; ++i) {
+                const uint32_t other = keys[i];
+                if (other == 0) break;
+                const float d = score_of[i];
+                const uint32_t p = ordered(d);
+                before += p > o || (p == o && other > mine);
+                // too close to tell in 32 bits, and not the same logit with the same bias, which the expert's place decides
+                if (!a.by_logit && i != j && !(fabsf(s - d) > __builtin_fmaf(fmaxf(fabsf(s), fabsf(d)), 0x1p-22f, 2.0f * error)) &&
+                    !(logits[i] == x && (!a.bias || a.bias[static_cast<uint32_t>(experts) - mine] == a.bias[static_cast<uint32_t>(experts) - other])))
+                    near = true;
+            }
+            again |= near && before < top_k;
+            new_keys[before] = mine;
+            new_logits[before] = __float_as_uint(x);
+        }
+        wave_sync();
+        for (int j = in_row; j < top_k; j += L) {
+            keys[j] = new_keys[j];
+            logits[j] = __uint_as_float(new_logits[j]);
+        }
+        wave_sync();
+    }
+    again = again && counts && static_cast<uint32_t>(row) < t.rows;
+    for (uint64_t left = __ballot(again); left != 0;) {
+        const int r = (__ffsll(static_cast<unsigned long long>(left)) - 1) / L;
+        left &= ~lanes_of_row<L>(r);
+        choose_in_64<TYPE>(t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0 + static_cast<uint32_t>(r)) * a.ld, a, reinterpret_cast<uint64_t*>(more),
+                           lds + r * slots, reinterpret_cast<float*>(lds + RW * slots) + r * slots);
+    }
+    wave_sync();
+    // The weights, formed of the chosen logits.
+    float most = softmax ? top : 0.0f;
+    if (a.renormalise) {
+        most = -INFINITY;
+        for (int j = in_row; j < top_k; j += L) most = fmaxf(most, logits[j]);
+        most = lanes_most<L>(most);
+        if (!softmax) most = fminf(most, 0.0f);
+    }
+    if (most == -INFINITY) most = INFINITY;                                     // nothing but -infinity: weights of 0
+    float sum = 0.0f;
+    for (int j = in_row; j < top_k; j += L) {
+        const float w = weight_of(logits[j], most, softmax);
+        sum += w;
+        logits[j] = w;
+    }
+    const float factor = weight_factor(a, lanes_reduce<L>(sum, OpAddF()), inverse);
+    if (static_cast<uint32_t>(row) >= t.rows) return;
+    const size_t token = t.t0 + static_cast<uint32_t>(row);
+    for (int j = in_row; j < top_k; j += L) {
+        const int32_t id = counts ? experts - static_cast<int32_t>(keys[j]) : -1;
+        if (a.id_bytes == 8) t.template ptr<int64_t>(kIds)[token * a.ids_ld + j] = id;
+        else t.template ptr<int32_t>(kIds)[token * a.ids_ld + j] = id;
+        t.template ptr<float>(kWeights)[token * a.weights_ld + j] = counts ? logits[j] * factor : 0.0f;
+    }
+}
+
+// The forward pass with 16 lanes a row and more, and few choices.  The k-th largest of the 16 largest scores of 16 parts of a row is not above the k-th
+// largest of all; what reaches it, less what 32 bits may be off by, are the candidates, some ten of a row.  They meet in LDS, one for each lane, and a
+// candidate's place is how many are better.  So no score is shortened and nothing sorted.
+constexpr int kCandidates = 16;
+template <int TYPE, int VEC, typename V>
+__device__ __forceinline__ float scores_logit(const V& v, int i)      // element i of a vector, where i is no constant
+{
+    typename Elem<TYPE>::one x = v[0];
+#pragma unroll
+    for (int e = 1; e < VEC; ++e) x = i == e ? v[e] : x;
+    return Elem<TYPE>::widen(x);
+}
+template <int L>
+__device__ __forceinline__ double lanes_sum(double v)                 // over the L >= 16 lanes of a row
+{
+    auto of = [](double x, auto exchange) {
+        const uint64_t b = __builtin_bit_cast(uint64_t, x);
+        return __builtin_bit_cast(double, static_cast<uint64_t>(exchange(static_cast<uint32_t>(b >> 32))) << 32 | exchange(static_cast<uint32_t>(b)));
+    };
+    v += of(v, [](uint32_t x) { return dpp<kXor1>(x); });
+    v += of(v, [](uint32_t x) { return dpp<kXor2>(x); });
+    v += of(v, [](uint32_t x) { return dpp<kHalfMirror>(x); });
+    v += of(v, [](uint32_t x) { return dpp<kMirror>(x); });
+    if (L >= 32) v += __shfl_xor(v, 16);
+    if (L >= 64) v += __shfl_xor(v, 32);
+    return v;
+}
+constexpr int kRor = 0x120;                // + n: the lane n places further in its row of 16, around its end
+template <int N, typename F>
+__device__ __forceinline__ void rotations(float v, const F& f)      // f(v of every other lane of the row of 16)
+{
+    if constexpr (N > 0) {
+        f(dpp<kRor + N>(v));
+        rotations<N - 1>(v, f);
+    }
+}
+template <int N, typename F>
+__device__ __forceinline__ void rotations(float v, uint32_t i, const F& f)
+{
+    if constexpr (N > 0) {
+        f(dpp<kRor + N>(v), dpp<kRor + N>(i));
+        rotations<N - 1>(v, i, f);
+    }
+}
+template <int TYPE, int VEC, int L, int NV>
+__global__ void __launch_bounds__(kWave * kRouteWaves)
+k_route_wide(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
+{
+    typedef Row<TYPE, VEC, L, NV> R;
+    typedef typename R::one one;
+    constexpr int RW = R::kRows, PER = VEC * NV;
+    static_assert(L >= kCandidates, "a lane for every candidate");
+    extern __shared__ uint64_t lds_of_waves[];
+    const int lane = threadIdx.x & 63, wave = wave_index(), row = lane / L, in_row = lane % L, experts = a.experts, top_k = a.top_k;
+    uint32_t* lds = reinterpret_cast<uint32_t*>(lds_of_waves) + static_cast<uint32_t>(wave) * a.wave_words;
+    float *found_score = reinterpret_cast<float*>(lds) + row * kCandidates, *found_logit = found_score + RW * kCandidates;
+    uint32_t *found = lds + 2 * RW * kCandidates + row * kCandidates, *count = lds + 3 * RW * kCandidates + row;
+    uint32_t* more = lds + 3 * RW * kCandidates + 4;                            // for the groups, or the keys of 64 bits
+    const uint32_t tile = blockIdx.x * (blockDim.x / kWave) + static_cast<uint32_t>(wave);
+    if (tile >= tiles) return;
+    const ListTile<kRouteLists> t(ls, tile, RW);
+    const bool softmax = a.score == BAGUA_SCORE_SOFTMAX;
+    const uint32_t my_row = min(static_cast<uint32_t>(row), t.rows - 1);
+    R raw;
+    raw.load(t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0 + my_row) * a.ld, experts, true);
+    const bool counts = !t.has(kMask) || t.template ptr<const uint8_t>(kMask)[t.t0 + my_row] != 0;
+    if (in_row == 0) *count = 0;
+    Scores<TYPE, VEC, L, NV> scores;
+    scores.form(raw, a);
+    auto& c = scores.c;
+    bool again = scores.has_nan();                                              // the row needs 64 bits
+    if (a.groups > 1) {
+        const uint32_t allowed = groups_that_stay<TYPE, VEC, L, NV>(a, c, reinterpret_cast<float*>(more), row, in_row, scores.error, again, again);
+        if (a.each % VEC == 0 && experts % VEC == 0) {                          // a vector is of one group
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const bool stays = allowed >> quotient(static_cast<uint32_t>(R::at(j, experts)), a.per_each) & 1u;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) c[j * VEC + i] = stays ? c[j * VEC + i] : -INFINITY;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    c[j * VEC + i] = allowed >> quotient(static_cast<uint32_t>(R::at(j, experts) + i), a.per_each) & 1u ? c[j * VEC + i] : -INFINITY;
+        }
+    }
+    if (experts != L * PER) {                                                   // the lanes behind a row's last element hold its last ones once more
+#pragma unroll
+        for (int j = NV / 2; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (R::at(j, experts) + i < R::slot(j)) c[j * VEC + i] = -INFINITY;
+    }
+    float best = c[0];
+#pragma unroll
+    for (int i = 1; i < PER; ++i) best = fmaxf(best, c[i]);
+    if (L >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(best), __float_as_uint(best), false, false);
+        best = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    if (L >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(best), __float_as_uint(best), false, false);
+        best = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    int better = 0;
+    rotations<15>(best, [&](float other) { better += other > best; });
+    const float bound = -lanes_most<16>(-(better < top_k ? best : INFINITY));
+    const float apart = a.by_logit ? 0.0f : __builtin_fmaf(fabsf(bound), 0x1p-21f, 2.0f * scores.error);
+    float least = bound - apart;
+    again |= !(least > -INFINITY);                                              // too few numbers
+    // How many of the row's scores reach x, and of the lane's own.
+    auto reach = [&](float x, int& own) {
+        own = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) own += c[i] >= x;
+        return static_cast<int>(lanes_reduce<L>(static_cast<uint32_t>(own), OpAddU()));
+    };
+    int mine = 0;
+    bool many = reach(least, mine) > kCandidates && !again;
+    if (__any(many)) {
+        // Parts that are not alike (groups that do not stay leave some empty): halving the way to the largest finds a better line.
+        float low = bound, high = lanes_most<16>(best);
+        for (int n = 0; n < 24 && __any(many); ++n) {
+            const float middle = 0.5f * low + 0.5f * high;
+            int own, unused;
+            const bool enough = reach(middle, unused) >= top_k, fits = reach(middle - apart, own) <= kCandidates;
+            if (many && enough && fits) least = middle - apart, mine = own, many = false;
+            if (enough) low = middle;
+            else high = middle;
+        }
+        again |= many;
+    }
+    if (again) mine = 0;
+    wave_sync();
+    uint32_t at = mine ? atomicAdd(count, static_cast<uint32_t>(mine)) : kCandidates;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (c[j * VEC + i] >= least && at < kCandidates) {
+                found_score[at] = c[j * VEC + i];
+                found_logit[at] = Elem<TYPE>::widen(raw.q[j][i]);
+                found[at] = static_cast<uint32_t>(R::at(j, experts) + i);
+                ++at;
+            }
+    wave_sync();
+    const uint32_t total = *count, candidate = static_cast<uint32_t>(lane) % kCandidates;
+    again |= total > kCandidates;
+    const bool is = candidate < total;
+    float score = is ? found_score[candidate] : -INFINITY, x = is ? found_logit[candidate] : -INFINITY;
+    uint32_t expert = is ? found[candidate] : 0;
+    const float near_by = __builtin_fmaf(fabsf(score), 0x1p-21f, 2.0f * scores.error);
+    int place = 0;
+    bool close = false;
+    if (a.by_logit) {                                                           // exact: equal ones are in order of their experts
+        rotations<15>(score, expert, [&](float other, uint32_t its) { place += other > score || (other == score && its < expert); });
+    } else {
+        rotations<15>(score, [&](float other) {
+            const float d = other - score;
+            place += d > 0.0f;
+            close |= fabsf(d) <= near_by;
+        });
+    }
+    if (__any(close && is)) {
+        // Too close to tell in 32 bits: the candidates' scores in 64.
+        double sum = 1.0;
+        const double most = scores.top == -INFINITY ? 0.0 : scores.top;
+        if (softmax) {
+            sum = 0.0;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll 1
+                for (int i = 0; i < VEC; ++i)
+                    if (R::at(j, experts) + i >= R::slot(j)) sum += exp(static_cast<double>(scores_logit<TYPE, VEC>(raw.q[j], i)) - most);
+            sum = lanes_sum<L>(sum);
+        }
+        double exact = -INFINITY;
+        if (is) {
+            exact = softmax ? (sum == 0.0 ? 0.0 : exp(static_cast<double>(x) - most) / sum) : 1.0 / (1.0 + exp(-static_cast<double>(x)));
+            if (a.bias) exact += static_cast<double>(a.bias[expert]);
+        }
+        double* scores_64 = reinterpret_cast<double*>(more) + row * kCandidates;
+        if (in_row < kCandidates) scores_64[candidate] = exact;
+        wave_sync();
+        place = 0;
+        for (uint32_t i = 0; i < kCandidates; ++i) {
+            const double other = scores_64[i];
+            place += i < total && (other > exact || (other == exact && found[i] < expert));
+        }
+        wave_sync();
+    }
+    if (!is) place = kCandidates;
+    again |= is && score == INFINITY;                                           // differences tell nothing
+    again = again && counts && static_cast<uint32_t>(row) < t.rows;
+    for (uint64_t left = __ballot(again); left != 0;) {
+        const int r = (__ffsll(static_cast<unsigned long long>(left)) - 1) / L;
+        left &= ~lanes_of_row<L>(r);
+        wave_sync();
+        choose_in_64<TYPE>(t.template ptr<const one>(kLogits) + static_cast<size_t>(t.t0 + static_cast<uint32_t>(r)) * a.ld, a, reinterpret_cast<uint64_t*>(more),
+                           lds, reinterpret_cast<float*>(lds) + kCandidates);   // (the candidates are in registers)
+        if (row == r) {
+            place = candidate < static_cast<uint32_t>(top_k) ? static_cast<int>(candidate) : kCandidates;
+            expert = candidate < static_cast<uint32_t>(top_k) ? static_cast<uint32_t>(experts) - lds[candidate] : 0;
+            x = candidate < static_cast<uint32_t>(top_k) ? reinterpret_cast<const float*>(lds)[kCandidates + candidate] : -INFINITY;
+        }
+    }
+    if (!counts) place = static_cast<int>(candidate);
+    // The weights, formed of the chosen logits.
+    const bool chosen = place < top_k;
+    float most = softmax ? scores.top : 0.0f;
+    if (a.renormalise) {
+        most = lanes_most<16>(chosen ? fmaxf(x, -INFINITY) : -INFINITY);
+        if (!softmax) most = fminf(most, 0.0f);
+    }
+    if (most == -INFINITY) most = INFINITY;                                     // nothing but -infinity: weights of 0
+    const float w = chosen ? weight_of(x, most, softmax) : 0.0f, factor = weight_factor(a, lanes_reduce<16>(w, OpAddF()), scores.inverse);
+    if (!chosen || in_row >= kCandidates || static_cast<uint32_t>(row) >= t.rows) return;
+    const size_t token = t.t0 + static_cast<uint32_t>(row);
+    const int32_t id = counts ? static_cast<int32_t>(expert) : -1;
+    if (a.id_bytes == 8) t.template ptr<int64_t>(kIds)[token * a.ids_ld + static_cast<size_t>(place)] = id;
+    else t.template ptr<int32_t>(kIds)[token * a.ids_ld + static_cast<size_t>(place)] = id;
+    t.template ptr<float>(kWeights)[token * a.weights_ld + static_cast<size_t>(place)] = counts ? w * factor : 0.0f;
+}
+
+// ---------------------------------------------------------------------------------------------- backward
+// One gradient of a weight goes to one logit, but where the scores are a whole row's softmax: a row's choices are written to a row in LDS that is zero
+// elsewhere, and it is read from there as it goes to memory.  FULL: softmax that was not renormalised, whose gradient reaches every logit; the row in
+// LDS then holds the weights' gradients, in fp32, elsewhere the logits' as they will be stored.
+template <int TYPE, int VEC, int L, int NV, bool FULL>
+__global__ void __launch_bounds__(kWave * kRouteWaves)
+k_route_grad(Lists<kRouteGradLists> ls, RouteGradArgs a, uint32_t tiles)
+{
+    typedef Row<TYPE, VEC, L, NV> R;
+    typedef typename R::one one;
+    typedef std::conditional_t<FULL, float, one> held;
+    typedef held held_vector __attribute__((ext_vector_type(VEC), aligned(sizeof(held) * VEC < 16 ? sizeof(held) * VEC : 16)));
+    constexpr int RW = R::kRows;
+    extern __shared__ uint64_t lds_of_waves[];
+    const int lane = threadIdx.x & 63, wave = wave_index(), row = lane / L, in_row = lane % L, experts = a.experts, top_k = a.top_k;
+    const uint32_t tile = blockIdx.x * (blockDim.x / kWave) + static_cast<uint32_t>(wave);
+    if (tile >= tiles) return;
+    const ListTile<kRouteGradLists> t(ls, tile, RW);
+    const bool there = static_cast<uint32_t>(row) < t.rows, shares = !FULL && a.renormalise, softmax = FULL || a.score == BAGUA_SCORE_SOFTMAX;
+    const size_t token = t.t0 + min(static_cast<uint32_t>(row), t.rows - 1);
+    const one* x_row = shares && softmax ? nullptr : t.template ptr<const one>(kGradLogits) + token * a.ld;
+    R raw;
+    if (FULL) raw.load(x_row, experts, true);
+    // Choice j of the lane's row: the expert, or -1; the gradient of its weight; its weight, or its logit.
+    struct Choice {
+        int expert;
+        float up, value;
+    };
+    auto load = [&](int j) {
+        Choice c;
+        const size_t at = token * a.ids_ld + static_cast<size_t>(j);
+        const uint64_t id = a.id_bytes == 8 ? t.template ptr<const uint64_t>(kGradIds)[at] : static_cast<uint64_t>(static_cast<int64_t>(t.template ptr<const int32_t>(kGradIds)[at]));
+        c.expert = there && id < static_cast<uint64_t>(experts) ? static_cast<int>(id) : -1;
+        c.up = t.template ptr<const float>(kGradUp)[token * a.up_ld + static_cast<size_t>(j)];
+        c.value = 0.0f;
+        if (shares && softmax) c.value = t.template ptr<const float>(kGradWeights)[token * a.weights_ld + static_cast<size_t>(j)];
+        else if (!FULL && c.expert >= 0) c.value = Elem<TYPE>::widen(x_row[c.expert]);
+        return c;
+    };
+    // The lane's choices: the first one is kept, and read once.
+    Choice own_choice{-1, 0.0f, 0.0f};
+    if (in_row < top_k) own_choice = load(in_row);
+    auto choices = [&](auto&& f) {
+        if (own_choice.expert >= 0) f(in_row, own_choice);
+        for (int j = in_row + L; j < top_k; j += L) {
+            const Choice c = load(j);
+            if (c.expert >= 0) f(j, c);
+        }
+    };
+    held* spread = reinterpret_cast<held*>(reinterpret_cast<uint32_t*>(lds_of_waves) + static_cast<uint32_t>(wave) * a.wave_words) + row * a.row_held;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (R::slot(j) < a.row_held) *reinterpret_cast<held_vector*>(spread + R::slot(j)) = held_vector(0);
+    // a choice's part of the sum that the weights were divided by, and the mean gradient of the weights
+    float most = -INFINITY, sum = 0.0f, mean = 0.0f;
+    bool any = false;
+    if (shares) {
+        if (!softmax) {
+            choices([&](int, const Choice& c) { most = fmaxf(most, c.value); });
+            most = fminf(lanes_most<L>(most), 0.0f);
+            if (most == -INFINITY) most = INFINITY;
+        }
+    }
+    const float per_scale = 1.0f / a.scale;
+    auto share = [&](const Choice& c) { return softmax ? c.value * per_scale : weight_of(c.value, most, false); };
+    if (shares) {
+        choices([&](int, const Choice& c) {
+            const float r = share(c);
+            sum += r;
+            mean = __builtin_fmaf(r, c.up, mean);
+        });
+        sum = softmax ? 1.0f : lanes_reduce<L>(sum, OpAddF());
+        mean = lanes_reduce<L>(mean, OpAddF());
+        mean = sum == 0.0f ? 0.0f : mean / sum;
+    } else if (FULL) {
+        choices([&](int, const Choice&) { any = true; });
+    }
+    // what a choice adds to its logit, in FULL to its score
+    auto part = [&](const Choice& c) {
+        if (FULL) return c.up;
+        if (shares && softmax) return c.value * (c.up - mean);
+        const float far = exp_below(-fabsf(c.value)), q = 1.0f / (1.0f + far);     // 1 - sigmoid is 1 / (1 + exp(x))
+        if (!shares) return a.scale * c.up * (far * q * q);
+        const float rest = c.value <= 0.0f ? q : far * q;
+        return sum == 0.0f ? 0.0f : a.scale * (share(c) / sum) * (c.up - mean) * rest;
+    };
+    // An expert that a row names twice gets both.  The rows that have one are found by writing the choices' places first.
+    wave_sync();
+    auto place = [](int j) { return FULL ? __builtin_bit_cast(held, static_cast<std::conditional_t<FULL || TYPE == BAGUA_F32, uint32_t, uint16_t>>(j)) : held(j); };
+    choices([&](int j, const Choice& c) { spread[c.expert] = place(j); });
+    wave_sync();
+    bool twice = false;
+    choices([&](int j, const Choice& c) { twice |= spread[c.expert] != place(j); });
+    wave_sync();
+    auto narrow = [](float v) {
+        if constexpr (FULL) return v;
+        else return Elem<TYPE>::narrow(v);
+    };
+    if (!__any(twice)) {
+        choices([&](int, const Choice& c) { spread[c.expert] = narrow(part(c)); });
+    } else {
+        choices([&](int, const Choice& c) {
+            float all = 0.0f;
+            for (int i = 0; i < top_k; ++i) {
+                const Choice d = load(i);
+                if (d.expert == c.expert) all += part(d);
+            }
+            spread[c.expert] = narrow(all);
+        });
+    }
+    wave_sync();
+    float e[1][NV][VEC], factor = 0.0f, shift = 0.0f, most_of[1], own[NV][VEC];
+    if (FULL) {
+        float dot = 0.0f;
+        R::owned(experts, own);
+        most_of[0] = raw.largest(e[0]);
+        exponentials_of<R>(e, most_of, TYPE != BAGUA_F16);
+        const float inverse = R::reciprocal_sum(own, e[0]);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) dot = __builtin_fmaf(e[0][j][i], static_cast<float>(spread[R::at(j, experts) + i]) * own[j][i], dot);
+        shift = lanes_reduce<L>(dot, OpAddF()) * inverse;
+        factor = a.scale * inverse;
+        any = (__ballot(any) & lanes_of_row<L>(row)) != 0;      // a row without a choice (padding) has no gradient, whatever its logits are
+    }
+    if (!there) return;
+    one* out = t.template ptr<one>(kGradOut) + token * a.out_ld;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        typename R::raw q;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const held s = spread[R::at(j, experts) + i];
+            if constexpr (FULL) q[i] = Elem<TYPE>::narrow(any ? e[0][j][i] * (factor * (s - shift)) : 0.0f);
+            else q[i] = s;
+        }
+        __builtin_nontemporal_store(q, reinterpret_cast<typename R::raw*>(out + R::at(j, experts)));
+    }
+}
+
+// Calls f with the layout of a row of `experts` logits: as many lanes as leave each some 16 of them, so that a choice, an exchange over the row's
+// lanes, is one for many rows.
+template <int VEC_, int L_, int NV_>
+struct RouteLayout {
+    static constexpr int VEC = VEC_, L = L_, NV = NV_;
+};
+template <int V, typename F>
+inline void with_lanes(int experts, const F& f)
+{
+    constexpr int N = 16 / V;                            // vectors of a lane
+    if (experts < V) {
+        if (experts <= 1) f(RouteLayout<1, 1, 1>());
+        else if (experts <= 2) f(RouteLayout<1, 2, 1>());
+        else if (experts <= 4) f(RouteLayout<1, 4, 1>());
+        else f(RouteLayout<1, 8, 1>());
+    } else if (experts <= V) f(RouteLayout<V, 1, 1>());
+    else if (experts <= 8 && V == 4) f(RouteLayout<V, 1, 2>());
+    else if (experts <= 16) f(RouteLayout<V, 1, N>());
+    else if (experts <= 32) f(RouteLayout<V, 2, N>());
+    else if (experts <= 64) f(RouteLayout<V, 4, N>());
+    else if (experts <= 128) f(RouteLayout<V, 8, N>());
+    else if (experts <= 256) f(RouteLayout<V, 16, N>());
+    else if (experts <= 512) f(RouteLayout<V, 32, N>());
+    else if (experts <= 1024) f(RouteLayout<V, 64, N>());
+    else f(RouteLayout<V, 64, 2 * N>());
+}
+// 16 lanes at least.
+template <int V, typename F>
+inline void with_many_lanes(int experts, const F& f)
+{
+    constexpr int N = 16 / V;
+    if (experts <= 64) f(RouteLayout<4, 16, 1>());
+    else if (experts <= 128) f(RouteLayout<V, 16, N / 2>());
+    else if (experts <= 256) f(RouteLayout<V, 16, N>());
+    else if (experts <= 512) f(RouteLayout<V, 32, N>());
+    else if (experts <= 1024) f(RouteLayout<V, 64, N>());
+    else f(RouteLayout<V, 64, 2 * N>());
+}
+
+// The line between the two layouts, for what is not chosen by whole 16-bit logits, and few choices.  Few lanes a row | 16 lanes and more, bf16 with a bias and fp32 without:
+// 1024 x 60 9.9 | 4.8 and 5.8 | 4.6 us, 32768 x 60 14.1 | 8.7 and 9.1 | 8.0, 131072 x 60 23.3 | 23.8 and 18.4 | 21.8; 131072 x 128 30.7 | 27.9 and 23.1 | 23.8, 131072 x 256
+// 56.8 | 40.9 and 41.6 | 30.7.
+constexpr int kNarrowExperts = 64;
+constexpr size_t kFewTokens = 65536;
+
+template <typename K, typename A, int P>
+inline int launch_tiles(K kernel, const Lists<P>& ls, const A& a, uint64_t tiles, size_t wave_bytes, hipStream_t stream)
+{
+    int waves = kRouteWaves;                   // of a workgroup: as many as have room in 64 KiB
+    while (waves > 1 && static_cast<size_t>(waves) * wave_bytes > 64 * 1024) waves /= 2;
+    const uint64_t of = static_cast<uint64_t>(waves);
+    launch_kernel(kernel, dim3(static_cast<uint32_t>((tiles + of - 1) / of)), dim3(static_cast<uint32_t>(kWave * waves)), wave_bytes * static_cast<size_t>(waves), stream, ls, a,
+                  static_cast<uint32_t>(tiles));
+    return launch_status();
+}
+
+template <int TYPE>
+int launch_route(Lists<kRouteLists>& ls, RouteArgs a, const size_t* tokens, int k, hipStream_t stream)
+{
+    constexpr int V = TYPE == BAGUA_F32 ? 4 : 8;
+    const bool few = a.top_k <= kFewChoices, whole_keys = a.by_logit && TYPE != BAGUA_F32 && a.groups == 1;
+    size_t all = 0;
+    for (int w = 0; w < k; ++w) all += tokens[w];
+    int status = BAGUA_OK;
+    const uint32_t columns = static_cast<uint32_t>(a.experts), groups = static_cast<uint32_t>(a.groups);
+    auto with = [&](uint32_t rows, auto&& f) {
+        const uint64_t tiles = tiles_of(ls, tokens, k, rows);
+        if (tiles > kMaxGrid) status = BAGUA_ERR_UNSUPPORTED;
+        if (tiles == 0 || tiles > kMaxGrid) return;
+        a.part = 1;
+        while (a.part < 16 && 2 * a.part * rows * groups <= kWave && 2 * a.part <= static_cast<uint32_t>(a.each)) a.part *= 2;
+        const uint32_t for_groups = groups > 1 ? rows * (columns + 2 * groups + 3) : 0;
+        f(for_groups, [&](auto kernel, uint32_t words) {
+            a.wave_words = (words + 1) & ~1u;
+            status = launch_tiles(kernel, ls, a, tiles, a.wave_words * sizeof(uint32_t), stream);
+        });
+    };
+    if (few && !whole_keys && a.experts > 32 && (a.experts > kNarrowExperts || all <= kFewTokens)) {
+        with_many_lanes<V>(a.experts, [&](auto layout) {
+            typedef decltype(layout) Lay;
+            constexpr uint32_t RW = kWave / Lay::L;
+            with(RW, [&](uint32_t for_groups, auto&& launch) {
+                launch(k_route_wide<TYPE, Lay::VEC, Lay::L, Lay::NV>, 3 * RW * kCandidates + 4 + std::max({for_groups, 2 * columns, 2 * RW * kCandidates}));
+            });
+        });
+        return status;
+    }
+    with_lanes<V>(a.experts, [&](auto layout) {
+        typedef decltype(layout) Lay;
+        constexpr uint32_t RW = kWave / Lay::L;
+        with(RW, [&](uint32_t for_groups, auto&& launch) {
+            if constexpr (TYPE != BAGUA_F32) {
+                if (whole_keys && few) {
+                    launch(k_route_16<TYPE, Lay::VEC, Lay::L, Lay::NV>, 0);
+                    return;
+                }
+            }
+            const uint32_t slots = RW * static_cast<uint32_t>(a.top_k + kMoreChoices), words = 2 * slots + std::max({for_groups, 2 * columns, 3 * slots});
+            // (few choices of many experts have gone the other way, and more than few need more than few experts)
+            if constexpr (Lay::VEC * Lay::NV * Lay::L <= kNarrowExperts) {
+                if (few) launch(k_route<TYPE, Lay::VEC, Lay::L, Lay::NV, true>, words);
+            }
+            if constexpr (Lay::VEC * Lay::NV * Lay::L > kFewChoices) {
+                if (!few) launch(k_route<TYPE, Lay::VEC, Lay::L, Lay::NV, false>, words);
+            }
+        });
+    });
+    return status;
+}
+
+template <int TYPE>
+int launch_route_grad(Lists<kRouteGradLists>& ls, RouteGradArgs a, const size_t* tokens, int k, hipStream_t stream)
+{
+    constexpr int V = TYPE == BAGUA_F32 ? 4 : 8;
+    const bool full = a.score == BAGUA_SCORE_SOFTMAX && !a.renormalise;
+    int status = BAGUA_OK;
+    with_lanes<V>(a.experts, [&](auto layout) {
+        typedef decltype(layout) Lay;
+        constexpr uint32_t RW = kWave / Lay::L;
+        const uint64_t tiles = tiles_of(ls, tokens, k, RW);
+        if (tiles > kMaxGrid) status = BAGUA_ERR_UNSUPPORTED;
+        if (tiles == 0 || tiles > kMaxGrid) return;
+        a.row_held = (a.experts + Lay::VEC - 1) / Lay::VEC * Lay::VEC;
+        const size_t wave_bytes = (RW * static_cast<size_t>(a.row_held) * (full ? sizeof(float) : type_bytes(TYPE)) + 15) / 16 * 16;
+        a.wave_words = static_cast<uint32_t>(wave_bytes / sizeof(uint32_t));
+        status = full ? launch_tiles(k_route_grad<TYPE, Lay::VEC, Lay::L, Lay::NV, true>, ls, a, tiles, wave_bytes, stream)
+                      : launch_tiles(k_route_grad<TYPE, Lay::VEC, Lay::L, Lay::NV, false>, ls, a, tiles, wave_bytes, stream);
+    });
+    return status;
+}
+
+}  // namespace bagua
