@@ -2,7 +2,7 @@
 
 Every one of the k workers (k sets of buffers on one GPU) has its own tokens.  A step:
 
-  1. logits = tokens @ weight + bias, the top-k experts of each token; the task wants every token at the expert of its kind, and some
+  1. logits = tokens @ weight + bias, the top-k experts of each token (bagua_route); the task wants every token at the expert of its kind, and some
      kinds are far more frequent than others, so that the task alone overloads a few experts;
   2. balance loss of all workers' tokens together and its gradient (bagua_balance_stats, bagua_balance_grad), added to the task's;
   3. each worker's gradients of weight and bias are flattened into its bucket and compressed with error feedback
@@ -84,11 +84,12 @@ def train(steps=150, workers=4, tokens=2048, width=128, experts=16, top_k=2, alp
     ws = empty(bg.bagua_balance_workspace_bytes(experts), torch.uint8)
     # the balance loss is of all workers' tokens: a worker's share of it is as large as the average over workers makes it small
     upstream = torch.full((1,), alpha * workers, device="cuda")
+    ids, weights = [empty((tokens, top_k), torch.int64) for _ in range(workers)], [empty((tokens, top_k)) for _ in range(workers)]
     history = []
     for step in range(1, steps + 1):
         xs, kinds = w.batch()
         logits = [x @ params[0] + params[1] for x in xs]
-        ids = [torch.topk(z, top_k, dim=1).indices for z in logits]
+        bg.bagua_route(logits, None, ids, weights)
         bg.bagua_balance_stats(logits, ids, None, counts, prob, ws, 1.0, loss, weight)
         dbalance = [torch.empty_like(z) for z in logits]
         bg.bagua_balance_grad(logits, None, weight, upstream, dbalance)
