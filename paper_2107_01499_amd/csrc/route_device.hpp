@@ -264,12 +264,17 @@ __device__ __forceinline__ uint32_t groups_that_stay(const RouteArgs& a, const f
     float *good = score_of + RW * wide, *errors = good + RW * a.groups;
     uint32_t* state = reinterpret_cast<uint32_t*>(errors + RW);                 // of every row: the groups that stay; whether that is not certain
     const bool aligned = a.each % VEC == 0 && experts % VEC == 0;               // a vector is of one group
+    auto keep = [&](auto of_vector) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const uint32_t at = static_cast<uint32_t>(R::at(j, experts)), g = quotient(at, a.per_each);
+        for (int j = 0; j < NV; ++j) {
+            const uint32_t at = static_cast<uint32_t>(R::at(j, experts));
+            float* to = score_of + row * wide + at + (decltype(of_vector)::value ? quotient(at, a.per_each) : 0);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) score_of[row * wide + static_cast<int>(at + i + (aligned ? g : quotient(at + i, a.per_each)))] = c[j * VEC + i];
-    }
+            for (int i = 0; i < VEC; ++i) to[i + (decltype(of_vector)::value ? 0 : quotient(at + i, a.per_each))] = c[j * VEC + i];
+        }
+    };
+    if (aligned) keep(std::true_type());
+    else keep(std::false_type());
     if (in_row == 0) state[row] = 0, state[RW + row] = 0, errors[row] = error;
     wave_sync();
     if (nan) state[RW + row] = 1;                                               // (64 bits know what to do)
