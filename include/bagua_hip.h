@@ -530,13 +530,13 @@ int bagua_balance_grad(int dtype, const void* const* logits, size_t ld, const si
  *   ids       host[k] of device [tokens[i]][top_k], int32 (id_bytes 4) or int64 (8), rows `ids_ld` >= top_k apart, written
  *   weights   host[k] of device fp32[tokens[i]][top_k], rows `weights_ld` >= top_k apart, written
  *   limits    1 <= k <= BAGUA_MAX_WORKERS, experts <= BAGUA_MAX_EXPERTS, a multiple of groups <= BAGUA_MAX_EXPERT_GROUPS, top_k <= BAGUA_MAX_CHOICES and
- *             <= top_groups * experts / groups, group_best <= experts / groups
+ *             <= top_groups * experts / groups, group_best <= experts / groups, |scale| <= 2^64
  * A NaN ranks above every number, among logits, scores and groups.  A row of softmax with a NaN or +infinity has weights NaN, one that is -infinity
  * throughout has scores and weights 0; the ids of a token are distinct and in range whatever its logits are.
  *
  * bagua_route_grad: gradient of the logits from dweights, that of the weights.  The choices have no gradient.
  *   ids       as bagua_route left them; an id outside [0, experts) is none (so padding's gradient is 0); one that comes twice counts twice
- *   weights   as bagua_route left them: read where softmax scores were renormalised (which needs scale != 0), NULL elsewhere
+ *   weights   as bagua_route left them: read where softmax scores were renormalised (which needs |scale| >= 2^-64), NULL elsewhere
  *   logits    read elsewhere; NULL where softmax scores were renormalised
  *   dweights  host[k] of device fp32[tokens[i]][top_k], rows dweights_ld apart; those of ids that are none are not used
  *   dlogits   host[k] of device [tokens[i]][experts] of dtype, rows ld_out apart, written: every element.  A row without an id has gradient 0.
@@ -566,13 +566,14 @@ int bagua_route_grad(int dtype, const void* const* logits, size_t ld, const size
  *   rows      host[k], any may be 0 (its pointers may then be NULL)
  *   ids       host[k] of device [rows[i]][top], int32 (id_bytes 4) or int64 (8), rows `ids_ld` apart.  An id outside [0, vocab) is no entry; one that
  *             comes twice counts twice.  A row without entries, or with none above -infinity, has no teacher's part.
- *   teacher   host[k] of device [rows[i]][top], rows `teacher_ld` apart
+ *   teacher   host[k] of device [rows[i]][top], rows `teacher_ld` apart; finite, or -infinity
  *   labels    host[k] of device int32 or int64 (label_bytes) [rows[i]]; outside [0, vocab): the row has no label's part.  NULL: none has
  *   mask      host[k] of device u8[rows[i]], 0 = padding: nothing of the row matters, its loss, statistics and gradient are 0; NULL: none
  *   loss      host[k] of device fp32[rows[i]], written: of each row
  *   stats     host[k] of device fp32[rows[i]][3], written: m = max x, sum of exp((x - m) / T), and with labels the sum of exp(x - m), else 0
- *   workspace device, >= bagua_distill_workspace_bytes(sum of rows, vocab) bytes, 16-byte aligned.  Calls on one workspace must not overlap in time.
- *   limits    1 <= k <= BAGUA_MAX_WORKERS, vocab <= BAGUA_MAX_VOCABULARY, 1 <= top <= BAGUA_MAX_TEACHER_ENTRIES, 2^-60 <= T <= 2^60
+ *   workspace device, >= bagua_distill_workspace_bytes(sum of rows, vocab) bytes, 16-byte aligned; one for more rows or a larger vocabulary does for fewer.
+ *             Calls on one workspace must not overlap in time.
+ *   limits    1 <= k <= BAGUA_MAX_WORKERS, vocab <= BAGUA_MAX_VOCABULARY, 1 <= top <= BAGUA_MAX_TEACHER_ENTRIES, 2^-60 <= T <= 2^60, |weights| <= 2^64
  * bagua_distill_grad: backward, with the same arguments; stats as bagua_distill_loss left them.
  *   upstream  host[k] of device fp32, the gradient of each row's loss (upstream_per_row: [rows[i]]) or of all of a worker's ([1]); NULL: 1
  *   dlogits   host[k] of device [rows[i]][vocab] of dtype, rows ld_out apart, written: every element.  It may be the logits' own memory (dlogits[i] == logits[i],

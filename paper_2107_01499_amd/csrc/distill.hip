@@ -359,7 +359,7 @@ k_distill_grad(Lists<kDistillGradLists> ls, DistillArgs a)
     typedef typename Elem<TYPE>::one one;
     typedef Span<TYPE, THREADS> S;
     constexpr int VEC = S::VEC, UNROLL = 4;
-    extern __shared__ uint32_t first_of[];                               // of every vector of the part, and of the elements that lie in none
+    extern __shared__ __attribute__((aligned(16))) uint32_t first_of[];                               // of every vector of the part, and of the elements that lie in none
     const int lane = threadIdx.x & 63, wave = wave_index();
     const uint32_t unit = blockIdx.x / a.parts, part = blockIdx.x - unit * a.parts;
     const ListTile<kDistillGradLists> t(ls, unit, 1);
@@ -491,10 +491,18 @@ constexpr uint32_t kDistillThreads = 256;
 constexpr size_t kShortVocab = 4096, kManyRows = 2048;
 
 // Parts of a row in the forward pass: enough workgroups for the chip, and none shorter than is worth one.
+constexpr size_t kWantedGroups = 8 * static_cast<size_t>(kCus);
+inline size_t most_parts(size_t vocab) { return std::min<size_t>((vocab + 8191) / 8192, kMostParts); }
 inline uint32_t loss_parts(size_t rows, size_t vocab)
 {
-    const size_t wanted = rows ? (8 * static_cast<size_t>(kCus) + rows - 1) / rows : 1;
-    return static_cast<uint32_t>(std::max<size_t>(1, std::min<size_t>({wanted, (vocab + 8191) / 8192, kMostParts})));
+    const size_t wanted = rows ? (kWantedGroups + rows - 1) / rows : 1;
+    return static_cast<uint32_t>(std::max<size_t>(1, std::min(wanted, most_parts(vocab))));
+}
+// Floats that the parts of so many rows, or of fewer, need at most: rows * parts is below kWantedGroups + rows, and none are needed from there on.
+inline size_t part_floats(size_t rows, size_t vocab)
+{
+    const size_t r = std::min(rows, kWantedGroups);
+    return most_parts(vocab) > 1 ? std::min(3 * most_parts(vocab) * r, 3 * (kWantedGroups + r)) + kLessonFloats * r : 0;
 }
 // In the backward pass: one batch of loads a workgroup, where rows are long; several (whole rows of 30522 or of 131072, 2 or 4 x as long) are slower than what looking at
 // the entries again costs: 4096 x 131072, bf16, 382 | 361 | 339 us with 32768 | 16384 | 8192 elements, 8 x 512 x 30522 106 | 97 | 98.
@@ -527,7 +535,7 @@ inline int distill_check(const DistillCall& c, Lists<P>& ls, DistillArgs& a, Ran
         c.top < 1 || c.ids_ld < static_cast<size_t>(c.top) || !type_ok(c.teacher_type) || !c.teacher || c.teacher_ld < static_cast<size_t>(c.top) ||
         (c.labels && c.label_bytes != 4 && c.label_bytes != 8) || !(c.temperature > 0.0) || !(c.temperature < INFINITY) || !(std::fabs(c.teacher_weight) < INFINITY) || !(std::fabs(c.label_weight) < INFINITY))
         return BAGUA_ERR_INVALID_ARG;
-    if (c.temperature < 0x1p-60 || c.temperature > 0x1p60) return BAGUA_ERR_UNSUPPORTED;
+    if (c.temperature < 0x1p-60 || c.temperature > 0x1p60 || std::fabs(c.teacher_weight) > 0x1p64 || std::fabs(c.label_weight) > 0x1p64) return BAGUA_ERR_UNSUPPORTED;
     if (c.vocab > BAGUA_MAX_VOCABULARY || c.top > BAGUA_MAX_TEACHER_ENTRIES || c.ld > kMostStride || c.ids_ld > kMostStride || c.teacher_ld > kMostStride) return BAGUA_ERR_UNSUPPORTED;
     const size_t element = type_bytes(c.dtype), top = static_cast<size_t>(c.top), id_size = static_cast<size_t>(c.id_bytes), label_size = static_cast<size_t>(c.label_bytes);
     total = 0;
@@ -591,8 +599,7 @@ using namespace bagua;
 extern "C" size_t bagua_distill_workspace_bytes(size_t rows, size_t vocab)
 {
     if (vocab < 1 || vocab > BAGUA_MAX_VOCABULARY || rows > kMaxGrid) return 0;
-    const size_t parts = loss_parts(rows, vocab);
-    return 16 + (parts > 1 ? (rows * (parts * 3 + kLessonFloats) * sizeof(float) + 15) / 16 * 16 : 0);
+    return 16 + (part_floats(rows, vocab) * sizeof(float) + 15) / 16 * 16;
 }
 
 extern "C" int bagua_distill_loss(int dtype, const void* const* logits, size_t ld, const size_t* rows, int k, size_t vocab, const void* const* ids, int id_bytes,

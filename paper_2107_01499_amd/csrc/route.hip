@@ -12,7 +12,7 @@ inline int route_check(int dtype, const size_t* tokens, int k, int experts, int 
     if (!tokens || !type_ok(dtype) || k < 1 || k > BAGUA_MAX_WORKERS || experts < 1 || top_k < 1 || top_k > experts || (id_bytes != 4 && id_bytes != 8) ||
         (score != BAGUA_SCORE_SOFTMAX && score != BAGUA_SCORE_SIGMOID) || !(std::fabs(scale) < INFINITY))
         return BAGUA_ERR_INVALID_ARG;
-    if (experts > BAGUA_MAX_EXPERTS || top_k > BAGUA_MAX_CHOICES) return BAGUA_ERR_UNSUPPORTED;
+    if (experts > BAGUA_MAX_EXPERTS || top_k > BAGUA_MAX_CHOICES || std::fabs(scale) > 0x1p64) return BAGUA_ERR_UNSUPPORTED;
     for (int w = 0; w < k; ++w)
         if (tokens[w] > kMaxGrid) return BAGUA_ERR_UNSUPPORTED;
     return BAGUA_OK;
@@ -78,6 +78,7 @@ extern "C" int bagua_route_grad(int dtype, const void* const* logits, size_t ld,
     if (!ids || !dweights || !dlogits || ids_ld < static_cast<size_t>(top_k) || dweights_ld < static_cast<size_t>(top_k) || ld_out < static_cast<size_t>(experts))
         return BAGUA_ERR_INVALID_ARG;
     if (of_weights ? !weights || weights_ld < static_cast<size_t>(top_k) || scale == 0.0 : !logits || ld < static_cast<size_t>(experts)) return BAGUA_ERR_INVALID_ARG;
+    if (of_weights && std::fabs(scale) < 0x1p-64) return BAGUA_ERR_UNSUPPORTED;      // (it is divided by)
     if (ids_ld > kMostStride || dweights_ld > kMostStride || ld_out > kMostStride || (of_weights ? weights_ld : ld) > kMostStride) return BAGUA_ERR_UNSUPPORTED;
     Lists<kRouteGradLists> ls{};
     RangeCheck rc;

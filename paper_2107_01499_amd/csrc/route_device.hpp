@@ -433,7 +433,7 @@ k_route(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
     typedef Row<TYPE, VEC, L, NV> R;
     typedef typename R::one one;
     constexpr int RW = R::kRows, PER = VEC * NV;
-    extern __shared__ uint64_t lds_of_waves[];
+    extern __shared__ __attribute__((aligned(16))) uint64_t lds_of_waves[];
     const int lane = threadIdx.x & 63, wave = wave_index(), row = lane / L, in_row = lane % L, experts = a.experts, top_k = a.top_k, slots = top_k + kMoreChoices;
     uint32_t* lds = reinterpret_cast<uint32_t*>(lds_of_waves) + static_cast<uint32_t>(wave) * a.wave_words;
     uint32_t* keys = lds + row * slots;                                          // the candidates, as keys and then as experts - id
@@ -655,7 +655,7 @@ k_route_wide(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
     typedef typename R::one one;
     constexpr int RW = R::kRows, PER = VEC * NV;
     static_assert(L >= kCandidates, "a lane for every candidate");
-    extern __shared__ uint64_t lds_of_waves[];
+    extern __shared__ __attribute__((aligned(16))) uint64_t lds_of_waves[];
     const int lane = threadIdx.x & 63, wave = wave_index(), row = lane / L, in_row = lane % L, experts = a.experts, top_k = a.top_k;
     uint32_t* lds = reinterpret_cast<uint32_t*>(lds_of_waves) + static_cast<uint32_t>(wave) * a.wave_words;
     float *found_score = reinterpret_cast<float*>(lds) + row * kCandidates, *found_logit = found_score + RW * kCandidates;
@@ -842,7 +842,7 @@ k_route_grad(Lists<kRouteGradLists> ls, RouteGradArgs a, uint32_t tiles)
     typedef std::conditional_t<FULL, float, one> held;
     typedef held held_vector __attribute__((ext_vector_type(VEC), aligned(sizeof(held) * VEC < 16 ? sizeof(held) * VEC : 16)));
     constexpr int RW = R::kRows;
-    extern __shared__ uint64_t lds_of_waves[];
+    extern __shared__ __attribute__((aligned(16))) uint64_t lds_of_waves[];
     const int lane = threadIdx.x & 63, wave = wave_index(), row = lane / L, in_row = lane % L, experts = a.experts, top_k = a.top_k;
     const uint32_t tile = blockIdx.x * (blockDim.x / kWave) + static_cast<uint32_t>(wave);
     if (tile >= tiles) return;

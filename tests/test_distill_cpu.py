@@ -34,7 +34,7 @@ BAD = [(dict(dtype=3), INVALID), (dict(logits=None), INVALID), (dict(logits=ptrs
        (dict(top=1025, ids_ld=1025, teacher_ld=1025), UNSUPPORTED), (dict(teacher_type=3), INVALID), (dict(teacher=None), INVALID), (dict(teacher=ptrs(None)), INVALID),
        (dict(label_bytes=1), INVALID), (dict(labels=ptrs(None)), INVALID), (dict(mask=ptrs(None)), INVALID), (dict(temperature=0.0), INVALID), (dict(temperature=-1.0), INVALID),
        (dict(temperature=math.nan), INVALID), (dict(temperature=math.inf), INVALID), (dict(temperature=1e-30), UNSUPPORTED), (dict(temperature=1e30), UNSUPPORTED),
-       (dict(teach=math.nan), INVALID), (dict(tell=math.inf), INVALID), (dict(ld=1 << 50), UNSUPPORTED), (dict(ids_ld=1 << 50), UNSUPPORTED), (dict(teacher_ld=1 << 50), UNSUPPORTED),
+       (dict(teach=math.nan), INVALID), (dict(tell=math.inf), INVALID), (dict(teach=1e30), UNSUPPORTED), (dict(tell=-1e300), UNSUPPORTED), (dict(ld=1 << 50), UNSUPPORTED), (dict(ids_ld=1 << 50), UNSUPPORTED), (dict(teacher_ld=1 << 50), UNSUPPORTED),
        (dict(logits=ptrs(X + 2)), ALIGN), (dict(dtype=1, logits=ptrs(X + 1)), ALIGN), (dict(ids=ptrs(I + 4)), ALIGN), (dict(teacher=ptrs(T + 2)), ALIGN),
        (dict(teacher_type=2, teacher=ptrs(T + 1)), ALIGN), (dict(labels=ptrs(B + 4)), ALIGN), (dict(stats=None), INVALID), (dict(stats=ptrs(None)), INVALID), (dict(stats=ptrs(S + 2)), ALIGN)]
 
@@ -62,6 +62,11 @@ def test_workspace(bg):
     size = bg.bagua_distill_workspace_bytes
     assert size(10, 0) == 0 == size(10, (1 << 30) + 1) == size(1 << 31, 10)
     assert 0 < size(0, 100) <= size(1, 100) and size(1, 1 << 20) > size(1, 100)
+    # one for more rows, or a larger vocabulary, does for fewer
+    for v in (100, 8192, 8193, 50000, 1 << 22):
+        sizes_of = [size(r, v) for r in sorted(list(range(0, 2100, 7)) + [2047, 2048, 2049, 4096, 100000])]
+        assert sizes_of == sorted(sizes_of)
+    assert all(size(r, 50000) <= size(r, 50001) <= size(r, 1 << 20) for r in (1, 40, 1000, 5000))
     # few rows never take more than many parts of each: what a call has to hold stays small
     assert max(size(r, v) for r in (1, 5, 100, 2047, 2048, 100000) for v in (1, 4096, 50000, 1 << 30)) < 1 << 20
 

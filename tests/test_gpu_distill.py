@@ -263,6 +263,25 @@ def test_logits_of_great_magnitude(bg):
         check(bg, s, 2.0)
 
 
+def test_as_many_workers_as_there_may_be(bg):
+    rows = [0, 5, 0, 0, 17] + [(7 * i) % 11 for i in range(25)] + [0, 3]
+    assert len(rows) == bg.MAX_WORKERS
+    for vocab in (500, 20011):
+        check(bg, inputs(rows, vocab, 5, "bf16", 12, masked=0.2), 2.0, up="rows")
+
+
+def test_a_part_of_weight_0_adds_nothing_where_it_is_infinite(bg):
+    x = torch.zeros(2, 300, device="cuda")
+    x[:, 7] = -math.inf
+    ids, y, labels = torch.full((2, 1), 7, device="cuda"), torch.zeros(2, 1, device="cuda"), torch.full((2,), 7, device="cuda")
+    loss, stats, ws = [torch.zeros(2, device="cuda")], [torch.zeros(2, 3, device="cuda")], torch.zeros(1 << 16, dtype=torch.uint8, device="cuda")
+    bg.bagua_distill_loss([x], [ids], [y], [labels], None, loss, stats, ws, 2.0, 0.0, 0.0)
+    assert torch.all(loss[0] == 0)
+    for teach, tell in ((1.0, 0.0), (0.0, 1.0)):
+        bg.bagua_distill_loss([x], [ids], [y], [labels], None, loss, stats, ws, 2.0, teach, tell)
+        assert torch.all(loss[0] == math.inf)
+
+
 def test_weights_of_zero_and_below(bg):
     for teach, tell in ((0.0, 1.0), (1.0, 0.0), (-0.5, 2.0), (0.0, 0.0)):
         check(bg, inputs([4], 700, 5, "f32", 9), 2.0, teach, tell)

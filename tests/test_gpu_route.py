@@ -279,6 +279,16 @@ def test_many_tokens(bg):
     check(bg, xs, 4, bias=torch.zeros(300, device="cuda"), score="sigmoid")
 
 
+def test_as_many_workers_as_there_may_be(bg):
+    tokens = [0, 5, 0, 0, 17] + [(7 * i) % 11 for i in range(25)] + [0, 3]
+    assert len(tokens) == bg.MAX_WORKERS
+    for experts, dtype, kw in ((8, "f32", {}), (64, "bf16", {}), (60, "f16", dict(score="sigmoid")), (256, "f32", dict(groups=8, top_groups=2))):
+        xs = logits_of(tokens, experts, dtype, 4)
+        ids, weights = check(bg, xs, 4, scale=2.0, **kw)
+        up = [torch.randn_like(w) for w in weights]
+        check_grad(bg, xs, ids, weights, up, dtype, kw.get("score", "softmax"), True, 2.0)
+
+
 # ---------------------------------------------------------------------------------------------- gradient
 def grad_truth(x, ids, up, score, renormalise, scale):
     z, out = x.double().cpu().numpy(), np.zeros(x.shape)

@@ -39,7 +39,7 @@ OF_LOGITS = dict(logits=ptrs(X), ld=8, weights=None, weights_ld=0)
     (dict(score=2), INVALID), (dict(score=-1), INVALID), (dict(groups=0), INVALID), (dict(groups=3), INVALID), (dict(groups=4, top_groups=0), INVALID),
     (dict(groups=4, top_groups=5), INVALID), (dict(groups=8, top_groups=1), INVALID), (dict(groups=8, top_groups=4, group_best=2), INVALID),
     (dict(groups=4, top_groups=2, group_best=3), INVALID), (dict(groups=4, top_groups=2, group_best=0), INVALID),
-    (dict(experts=66, ld=66, groups=33, top_groups=3), UNSUPPORTED), (dict(scale=math.nan), INVALID), (dict(scale=math.inf), INVALID), (dict(mask=ptrs(None)), INVALID),
+    (dict(experts=66, ld=66, groups=33, top_groups=3), UNSUPPORTED), (dict(scale=math.nan), INVALID), (dict(scale=math.inf), INVALID), (dict(scale=1e300), UNSUPPORTED), (dict(mask=ptrs(None)), INVALID),
     (dict(logits=ptrs(X + 2)), ALIGN), (dict(dtype=1, logits=ptrs(X + 1)), ALIGN), (dict(ids=ptrs(I + 4)), ALIGN), (dict(ids=ptrs(I + 2), id_bytes=4), ALIGN),
     (dict(weights=ptrs(W + 2)), ALIGN), (dict(bias=B + 1), ALIGN), (dict(ids=ptrs(X)), INVALID), (dict(weights=ptrs(X + 316)), INVALID), (dict(weights=ptrs(I + 156)), INVALID),
     (dict(bias=I), INVALID), (dict(mask=ptrs(W + 3)), INVALID), (dict(tokens=sizes(0), logits=ptrs(None), ids=ptrs(None), weights=ptrs(None)), OK)])
@@ -51,7 +51,8 @@ def test_routing_refuses(bg, kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(dtype=3), INVALID), (dict(tokens=None), INVALID), (dict(k=0), INVALID), (dict(k=33), INVALID), (dict(experts=0), INVALID), (dict(ids=None), INVALID),
     (dict(ids=ptrs(None)), INVALID), (dict(up=None), INVALID), (dict(up=ptrs(None)), INVALID), (dict(out=None), INVALID), (dict(out=ptrs(None)), INVALID),
-    (dict(weights=None), INVALID), (dict(weights=ptrs(None)), INVALID), (dict(weights_ld=1), INVALID), (dict(scale=0.0), INVALID), (dict(scale=math.nan), INVALID),
+    (dict(weights=None), INVALID), (dict(weights=ptrs(None)), INVALID), (dict(weights_ld=1), INVALID), (dict(scale=0.0), INVALID), (dict(scale=1e-40), UNSUPPORTED), (dict(scale=-1e30), UNSUPPORTED),
+    (dict(scale=math.nan), INVALID),
     (dict(score=1), INVALID), (dict(renormalise=0), INVALID), (dict(OF_LOGITS), INVALID), (dict(OF_LOGITS, score=1, ld=7), INVALID),
     (dict(OF_LOGITS, score=1, logits=ptrs(None)), INVALID), (dict(OF_LOGITS, score=1, logits=ptrs(X + 2)), ALIGN), (dict(OF_LOGITS, score=1, out=ptrs(X)), INVALID),
     (dict(OF_LOGITS, score=1, ld=1 << 50), UNSUPPORTED), (dict(weights_ld=1 << 50), UNSUPPORTED), (dict(up_ld=1 << 50), UNSUPPORTED), (dict(ids_ld=1 << 50), UNSUPPORTED),
