@@ -196,11 +196,21 @@ __device__ __forceinline__ uint64_t lanes_of_row(int row) { return (L == 64 ? ~0
 
 constexpr int kFewChoices = 8;
 
-// The choice scores of a row in 32 bits, and what the weights need of it.
+template <int I, int N, int VEC, int NV>
+__device__ __forceinline__ float sum_in_pairs(const float (&v)[NV][VEC])
+{
+    if constexpr (N == 1) return v[I / VEC][I % VEC];
+    else return sum_in_pairs<I, N / 2, VEC>(v) + sum_in_pairs<I + N / 2, N / 2, VEC>(v);
+}
+
+// The choice scores of a row in 32 bits, and what the weights need of it.  error: what a score is off by at most before its bias is added, u = 2^-24.  A softmax's
+// exponential is off by 2 u (the instruction) and by its argument's rounding, which as a part of the row's largest is 0.4 u; the sum, put together in pairs, by
+// as much again and 11 u (11 levels of 2048 logits), the reciprocal and the product by 3 u: below 24 u of the row's largest.  A sigmoid is off by (1 - s)(|x| + 2) u + 3 u
+// of itself: below 12 u of 1/2 where the largest logit is not below 0, else below (2 |x| + 12) u of the largest.
 template <int TYPE, int VEC, int L, int NV>
 struct Scores {
     typedef Row<TYPE, VEC, L, NV> R;
-    float c[VEC * NV], top = -INFINITY, inverse = 1.0f, error = 0.0f;      // error: of a score, at most
+    float c[VEC * NV], top = -INFINITY, inverse = 1.0f, error = 0.0f;
     __device__ __forceinline__ void form(const R& raw, const RouteArgs& a)
     {
         const bool softmax = a.score == BAGUA_SCORE_SOFTMAX;
@@ -214,14 +224,22 @@ struct Scores {
         float e[1][NV][VEC], most[1];
         most[0] = top = raw.largest(e[0]);
         if (softmax) {
-            float own[NV][VEC];
-            R::owned(a.experts, own);
             exponentials_of<R>(e, most, TYPE != BAGUA_F16);
-            inverse = R::reciprocal_sum(own, e[0]);
-            error = inverse * 0x1p-21f;
+            float own = sum_in_pairs<0, VEC * NV, VEC>(e[0]);
+            if (a.experts != L * VEC * NV) {                    // the lanes behind a row's last element hold its last ones once more
+                float once[NV][VEC];
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) once[j][i] = j < NV / 2 || R::at(j, a.experts) + i >= R::slot(j) ? e[0][j][i] : 0.0f;
+                own = sum_in_pairs<0, VEC * NV, VEC>(once);
+            }
+            const float sum = lanes_reduce<L>(own, OpAddF()), r = __builtin_amdgcn_rcpf(sum);
+            inverse = sum == 0.0f ? 0.0f : __builtin_fmaf(__builtin_fmaf(-sum, r, 1.0f), r, r);
+            error = inverse * 0x1.8p-20f;
         } else {
             const float low = fminf(top, 0.0f);
-            error = sigmoid(low) * __builtin_fmaf(-low, 0x1p-23f, 0x1p-21f);
+            error = sigmoid(low) * __builtin_fmaf(-low, 0x1p-23f, 0x1.8p-21f);
         }
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -252,7 +270,7 @@ struct Scores {
 };
 
 // The groups whose experts may be chosen, a bit for each, for the lane's row.  nan: the lane has one; uncertain: 32 bits cannot tell.  score_of: LDS of 64 / L
-// rows of scores (each group one further, so that lanes that go through different groups meet in no bank), group sums, and three words.
+// rows of scores (each group one further, so that lanes that go through different groups meet in no bank), group sums, and four words.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); }      // of numbers, one instruction wherever they come from
 __device__ __forceinline__ float smaller(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, -INFINITY); }
 template <int TYPE, int VEC, int L, int NV>
@@ -263,6 +281,7 @@ __device__ __forceinline__ uint32_t groups_that_stay(const RouteArgs& a, const f
     const int lane = threadIdx.x & 63, experts = a.experts, wide = experts + a.groups;
     float *good = score_of + RW * wide, *errors = good + RW * a.groups;
     uint32_t* state = reinterpret_cast<uint32_t*>(errors + RW);                 // of every row: the groups that stay; whether that is not certain
+    uint32_t* size = state + 2 * RW;                                            // the largest that was added up for a sum
     const bool aligned = a.each % VEC == 0 && experts % VEC == 0;               // a vector is of one group
     auto keep = [&](auto of_vector) {
 #pragma unroll
@@ -275,7 +294,7 @@ __device__ __forceinline__ uint32_t groups_that_stay(const RouteArgs& a, const f
     };
     if (aligned) keep(std::true_type());
     else keep(std::false_type());
-    if (in_row == 0) state[row] = 0, state[RW + row] = 0, errors[row] = error;
+    if (in_row == 0) state[row] = 0, state[RW + row] = 0, size[row] = 0, errors[row] = error;
     wave_sync();
     if (nan) state[RW + row] = 1;                                               // (64 bits know what to do)
     const uint32_t pairs = static_cast<uint32_t>(RW * a.groups), at_once = kWave / a.part, sub = static_cast<uint32_t>(lane) & (a.part - 1);
@@ -294,7 +313,11 @@ __device__ __forceinline__ uint32_t groups_that_stay(const RouteArgs& a, const f
             second = larger(smaller(first, f), larger(second, s));
             first = larger(first, f);
         }
-        if (sub == 0) good[pair] = a.group_best == 2 ? first + second : first;
+        if (sub == 0) {
+            good[pair] = a.group_best == 2 ? first + second : first;
+            const float both = fabsf(first) + fabsf(second);
+            if (both < INFINITY) atomicMax(size + r, __float_as_uint(both));
+        }
     }
     wave_sync();
     for (uint32_t pair = lane; pair < pairs; pair += kWave) {
@@ -308,8 +331,8 @@ __device__ __forceinline__ uint32_t groups_that_stay(const RouteArgs& a, const f
             }
             perhaps = before;
         } else {
-            // (a group as close as that is of nearly this size)
-            const float apart = __builtin_fmaf(fabsf(mine), 0x1p-20f, 4.0f * errors[r]), above = mine + apart, below = mine - apart;
+            // two sums of two scores each: their errors, and the roundings of scores and sums, 4 u of what is added up
+            const float apart = __builtin_fmaf(__uint_as_float(size[r]), 0x1p-21f, 4.0f * errors[r]), above = mine + apart, below = mine - apart;
             perhaps = -1;                                                       // itself
 #pragma unroll 8
             for (uint32_t h = 0; h < static_cast<uint32_t>(a.groups); ++h) {
@@ -711,8 +734,9 @@ k_route_wide(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
     }
     int better = 0;
     rotations<15>(best, [&](float other) { better += other > best; });
-    const float bound = -lanes_most<16>(-(better < top_k ? best : INFINITY));
-    const float apart = a.by_logit ? 0.0f : __builtin_fmaf(fabsf(bound), 0x1p-21f, 2.0f * scores.error);
+    const float bound = -lanes_most<16>(-(better < top_k ? best : INFINITY)), largest = lanes_most<16>(best);
+    // two scores' errors, and their roundings, 2 u of the larger one
+    const float apart = a.by_logit ? 0.0f : __builtin_fmaf(larger(fabsf(bound), fabsf(largest)), 0x1p-21f, 2.0f * scores.error);
     float least = bound - apart;
     again |= !(least > -INFINITY);                                              // too few numbers
     // How many of the row's scores reach x, and of the lane's own.
@@ -726,7 +750,7 @@ k_route_wide(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
     bool many = reach(least, mine) > kCandidates && !again;
     if (__any(many)) {
         // Parts that are not alike (groups that do not stay leave some empty): halving the way to the largest finds a better line.
-        float low = bound, high = lanes_most<16>(best);
+        float low = bound, high = largest;
         for (int n = 0; n < 24 && __any(many); ++n) {
             const float middle = 0.5f * low + 0.5f * high;
             int own, unused;
@@ -1041,7 +1065,7 @@ int launch_route(Lists<kRouteLists>& ls, RouteArgs a, const size_t* tokens, int 
         if (tiles == 0 || tiles > kMaxGrid) return;
         a.part = 1;
         while (a.part < 16 && 2 * a.part * rows * groups <= kWave && 2 * a.part <= static_cast<uint32_t>(a.each)) a.part *= 2;
-        const uint32_t for_groups = groups > 1 ? rows * (columns + 2 * groups + 3) : 0;
+        const uint32_t for_groups = groups > 1 ? rows * (columns + 2 * groups + 4) : 0;
         f(for_groups, [&](auto kernel, uint32_t words) {
             a.wave_words = (words + 1) & ~1u;
             status = launch_tiles(kernel, ls, a, tiles, a.wave_words * sizeof(uint32_t), stream);

@@ -207,6 +207,26 @@ def test_scores_that_32_bits_cannot_tell_apart(bg, experts, score):
     check(bg, [x], 8, bias=bias, score=score)
 
 
+@pytest.mark.parametrize("experts", [8, 24, 64, 128, 256, 1030])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_pairs_that_a_bias_brings_together(bg, experts, score):
+    """The best experts in pairs whose scores with bias differ by next to nothing: one order in 64 bits, the other or none in 32.  Flat and peaked rows."""
+    g = np.random.default_rng(experts)
+    for case in range(60):
+        z = g.normal(0.0, (0.3, 1.5, 4.0)[case % 3], (1, experts)).astype(np.float32)
+        if score == "sigmoid" and case % 2:
+            z -= 9.0
+        s = scores(z.astype(np.float64), score)[0]
+        bias, order = np.zeros(experts, np.float32), np.argsort(-s)
+        for m in range(0, min(experts, 12) - 1, 2):
+            i, j = order[m:m + 2] if case % 5 else order[[m // 2, -1 - m // 2]]
+            bias[j] = np.float32(s[i] + bias[i] - s[j] + g.choice([0.0, 1e-9, -1e-9, 1e-8, -1e-8, 1e-7, -1e-7]))
+        x, b = torch.from_numpy(z).cuda(), torch.from_numpy(bias).cuda()
+        check(bg, [x], min(experts, 8), bias=b, score=score)
+        if experts % 8 == 0 and experts > 8:
+            check(bg, [x], 6, bias=b, score=score, groups=8, top_groups=4, group_best=2)
+
+
 def test_numbers_that_are_not_finite(bg):
     for experts in (8, 60, 256, 1030):
         g = torch.Generator(device="cuda").manual_seed(experts)
