@@ -225,6 +225,8 @@ def test_pairs_that_a_bias_brings_together(bg, experts, score):
         check(bg, [x], min(experts, 8), bias=b, score=score)
         if experts % 8 == 0 and experts > 8:
             check(bg, [x], 6, bias=b, score=score, groups=8, top_groups=4, group_best=2)
+        if experts <= 32:                                              # a group for every expert
+            check(bg, [x], 4, bias=b, score=score, groups=experts, top_groups=experts // 2 + 1)
 
 
 def test_numbers_that_are_not_finite(bg):
