@@ -1,9 +1,9 @@
 // Kernels of routing of tokens to experts and its backward pass (see bagua_hip.h), and their launches; every element type is built in a file of its own.
 //
 // A row of logits lies in L lanes as in rows.hpp.  Which experts are chosen has to be what numbers of 64 bits give, though the scores are formed in
-// 32: an element's key is its choice score, as an integer that is ordered as the numbers are, with the last bits replaced by how far its
-// expert lies from the last one, so that a maximum of keys is the best score and of equal ones the lowest expert.  Where two neighbours among
-// the chosen lie closer than the error of 32 bits (and are not the same logit with the same bias), the row is done again in 64 bits.
+// 32.  What all kernels do about it: they know by how much a score in 32 bits may be off (Scores::error), and where that could change the choice, look again in
+// 64 bits, at the candidates or, if that is not enough, at the row (choose_in_64).  Without a bias and with groups that are as good as their best expert, scores
+// need not be formed: they rise with the logits, and these are exact.
 #pragma once
 #include "route.hpp"
 #include "rows.hpp"
@@ -449,7 +449,8 @@ k_route_16(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
     }
 }
 
-// The forward pass of everything else.  As above, but a key has lost the last bits of its score to the expert's place: some runners-up are taken too, and
+// The forward pass of few experts, and of more choices than few.  As above, but a key is a score as an integer that is ordered as numbers are, and has lost its
+// last bits to the expert's place (how far it lies from the last one, so that of equal scores the lowest expert's key is the largest): some runners-up are taken too, and
 // the candidates put in order by their scores in 32 bits where two keys are close.  FEW: at most kFewChoices.  Bound by the vector ALU: 131072 x 60, bf16 with a bias, 24.3 us,
 // fp32 by its logits 18.1.  Small launches by latency: 96 rows of 8, fp32, 4.6 us.
 template <int TYPE, int VEC, int L, int NV, bool FEW>

@@ -156,11 +156,8 @@ def test_groups(bg, experts, groups, top_groups, top, dtype):
                 check(bg, xs, top, bias=b, score=score, groups=groups, top_groups=top_groups, group_best=best)
 
 
-@pytest.mark.parametrize("top", [1, 2, 3, 5, 8, 17, 63, 64])
-@pytest.mark.parametrize("experts", [8, 64, 70, 256, 2048])
+@pytest.mark.parametrize("experts,top", [(e, k) for e in (8, 64, 70, 256, 2048) for k in (1, 2, 3, 5, 8, 17, 63, 64) if k <= e])
 def test_every_number_of_choices(bg, experts, top):
-    if top > experts:
-        pytest.skip("more choices than experts")
     for dtype in TYPES:
         xs = logits_of([19], experts, dtype, top)
         check(bg, xs, top)
