@@ -452,7 +452,7 @@ k_route_16(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
 // The forward pass of few experts, and of more choices than few.  As above, but a key is a score as an integer that is ordered as numbers are, and has lost its
 // last bits to the expert's place (how far it lies from the last one, so that of equal scores the lowest expert's key is the largest): some runners-up are taken too, and
 // the candidates put in order by their scores in 32 bits where two keys are close.  FEW: at most kFewChoices.  Bound by the vector ALU: 131072 x 60, bf16 with a bias, 24.3 us,
-// fp32 by its logits 18.1.  Small launches by latency: 96 rows of 8, fp32, 4.6 us.
+// fp32 by its logits 18.1.
 template <int TYPE, int VEC, int L, int NV, bool FEW>
 __global__ void __launch_bounds__(kWave * kRouteWaves)
 k_route(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
@@ -628,6 +628,130 @@ k_route(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
         else t.template ptr<int32_t>(kIds)[token * a.ids_ld + j] = id;
         t.template ptr<float>(kWeights)[token * a.weights_ld + j] = counts ? logits[j] * factor : 0.0f;
     }
+}
+
+// Sorts N scores with their experts and logits, the largest first, equal ones by their experts: the network of sort_keys.
+template <int P, int K, int I, typename C, int N>
+__device__ __forceinline__ void sort_step(C (&c)[N], float (&x)[N], int (&e)[N])
+{
+    if constexpr (I + K < N) {
+        if constexpr (I >= K % P && (I - K % P) / K % 2 == 0 && I / (2 * P) == (I + K) / (2 * P)) {
+            const C c0 = c[I], c1 = c[I + K];
+            const float x0 = x[I], x1 = x[I + K];
+            const int e0 = e[I], e1 = e[I + K];
+            const bool turn = c1 > c0 || (c1 == c0 && e1 < e0);
+            c[I] = turn ? c1 : c0, c[I + K] = turn ? c0 : c1;
+            x[I] = turn ? x1 : x0, x[I + K] = turn ? x0 : x1;
+            e[I] = turn ? e1 : e0, e[I + K] = turn ? e0 : e1;
+        }
+        sort_step<P, K, I + 1>(c, x, e);
+    } else if constexpr (K > 1) {
+        sort_step<P, K / 2, 0>(c, x, e);
+    } else if constexpr (2 * P < N) {
+        sort_step<2 * P, 2 * P, 0>(c, x, e);
+    }
+}
+
+// The forward pass of up to 8 experts in one group, but for whole 16-bit logits: a row in a lane, sorted whole, so that no lane asks another anything, and lanes
+// whose scores 32 bits cannot tell apart sort them in 64, all at once.  k_route | this: 262144 rows of 8, bf16, sigmoid and a bias, four choices 23.0 | 11.7 us, of 4 14.7 | 8.9;
+// fp32, two choices, of 8 6.6 | 6.3, of 2 7.7 | 4.6, and where all the scores are within 1e-3 (65536 rows, six choices) 49 | 13.5.  Whole 16-bit logits lose: 1048576 rows of 8,
+// k_route_16 12.4 | 15.3.  16 experts a lane: fp32, 32768 rows 5.6 | 8.0.  Small launches by latency: 96 rows of 8, fp32, 3.9 us (4.6).
+constexpr int kLaneExperts = 8;
+template <int TYPE, int VEC, int NV>
+__global__ void __launch_bounds__(kWave * kRouteWaves)
+k_route_lane(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
+{
+    typedef Row<TYPE, VEC, 1, NV> R;
+    typedef typename R::one one;
+    constexpr int PER = VEC * NV;
+    const int lane = threadIdx.x & 63, experts = a.experts, top_k = a.top_k;
+    const uint32_t tile = blockIdx.x * (blockDim.x / kWave) + static_cast<uint32_t>(wave_index());
+    if (tile >= tiles) return;
+    const ListTile<kRouteLists> t(ls, tile, kWave);
+    if (static_cast<uint32_t>(lane) >= t.rows) return;
+    const size_t token = t.t0 + static_cast<uint32_t>(lane);
+    const bool softmax = a.score == BAGUA_SCORE_SOFTMAX;
+    R raw;
+    raw.load(t.template ptr<const one>(kLogits) + token * a.ld, experts, true);
+    const bool counts = !t.has(kMask) || t.template ptr<const uint8_t>(kMask)[token] != 0;
+    Scores<TYPE, VEC, 1, NV> scores;
+    scores.form(raw, a);
+    bool again = scores.has_nan();
+    float x[PER];
+    int expert[PER];
+    auto unsorted = [&](auto (&c)[PER], auto none, const auto& score) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const int at = R::at(j, experts) + i;
+                const bool there = at >= R::slot(j);            // (a row's last elements come once more where it does not fill the lane)
+                x[j * VEC + i] = Elem<TYPE>::widen(raw.q[j][i]);
+                c[j * VEC + i] = there ? score(j * VEC + i, x[j * VEC + i], at) : none;
+                expert[j * VEC + i] = there ? at : kLaneExperts;                // behind all that are
+            }
+    };
+    float c[PER];
+    unsorted(c, -INFINITY, [&](int n, float, int) { return scores.c[n]; });
+    if constexpr (PER > 1) sort_step<1, 1, 0>(c, x, expert);
+    if (!a.by_logit) {
+        // Neighbours too close to tell in 32 bits, but for one logit with one bias, which are as good in 64; of such, also those behind the choices.
+        bool asked = true;
+#pragma unroll
+        for (int j = 0; j + 1 < PER; ++j) {
+            const float apart = __builtin_fmaf(larger(fabsf(c[j]), fabsf(c[j + 1])), 0x1p-21f, 2.0f * scores.error);
+            asked = (asked || j < top_k) && j + 1 < experts;
+            if (asked && !(c[j] - c[j + 1] > apart)) {
+                const bool same = x[j] == x[j + 1] && (!a.bias || a.bias[expert[j]] == a.bias[expert[j + 1]]);
+                again |= !same;
+                asked = same;
+            } else {
+                asked = false;
+            }
+        }
+    }
+    if (again && counts) {
+        const double most = scores.top == -INFINITY ? 0.0 : scores.top;
+        double sum = 0.0;
+        uint64_t key[PER];
+        unsorted(key, static_cast<uint64_t>(0), [&](int n, float logit, int at) {
+            const double z = logit;
+            if (a.by_logit) return ordered(z);
+            const double s = exp(softmax ? z - most : -z);
+            sum += s;
+            return __builtin_bit_cast(uint64_t, s);
+        });
+        if (!a.by_logit) {
+            unsorted(key, static_cast<uint64_t>(0), [&](int n, float, int at) {
+                const double s = __builtin_bit_cast(double, key[n]);
+                return ordered((softmax ? (sum == 0.0 ? 0.0 : s / sum) : 1.0 / (1.0 + s)) + (a.bias ? static_cast<double>(a.bias[at]) : 0.0));
+            });
+        }
+        if constexpr (PER > 1) sort_step<1, 1, 0>(key, x, expert);
+    }
+    // The weights, formed of the chosen logits.
+    float most = softmax ? scores.top : 0.0f;
+    if (a.renormalise) {
+        most = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (j < top_k) most = fmaxf(most, x[j]);
+        if (!softmax) most = fminf(most, 0.0f);
+    }
+    if (most == -INFINITY) most = INFINITY;                                     // nothing but -infinity: weights of 0
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+        if (j < top_k) sum += x[j] = weight_of(x[j], most, softmax);
+    const float factor = weight_factor(a, sum, scores.inverse);
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+        if (j < top_k) {
+            const int32_t id = counts ? expert[j] : -1;
+            if (a.id_bytes == 8) t.template ptr<int64_t>(kIds)[token * a.ids_ld + j] = id;
+            else t.template ptr<int32_t>(kIds)[token * a.ids_ld + j] = id;
+            t.template ptr<float>(kWeights)[token * a.weights_ld + j] = counts ? x[j] * factor : 0.0f;
+        }
 }
 
 // The forward pass with 16 lanes a row and more, and few choices.  The k-th largest of the 16 largest scores of 16 parts of a row is not above the k-th
@@ -1028,6 +1152,17 @@ inline void with_lanes(int experts, const F& f)
     else if (experts <= 1024) f(RouteLayout<V, 64, N>());
     else f(RouteLayout<V, 64, 2 * N>());
 }
+// One lane.
+template <int V, typename F>
+inline void with_one_lane(int experts, const F& f)
+{
+    if (experts <= 1) f(RouteLayout<1, 1, 1>());
+    else if (experts <= 2) f(RouteLayout<1, 1, 2>());
+    else if (experts < V && experts <= 4) f(RouteLayout<1, 1, 4>());
+    else if (experts < V) f(RouteLayout<1, 1, V>());
+    else if (experts <= V) f(RouteLayout<V, 1, 1>());
+    else f(RouteLayout<V, 1, 8 / V>());
+}
 // 16 lanes at least.
 template <int V, typename F>
 inline void with_many_lanes(int experts, const F& f)
@@ -1089,6 +1224,13 @@ int launch_route(Lists<kRouteLists>& ls, RouteArgs a, const size_t* tokens, int 
         });
         return status;
     }
+    if (a.experts <= kLaneExperts && a.groups == 1 && !whole_keys) {
+        with_one_lane<V>(a.experts, [&](auto layout) {
+            typedef decltype(layout) Lay;
+            with(kWave, [&](uint32_t, auto&& launch) { launch(k_route_lane<TYPE, Lay::VEC, Lay::NV>, 0); });
+        });
+        return status;
+    }
     with_lanes<V>(a.experts, [&](auto layout) {
         typedef decltype(layout) Lay;
         constexpr uint32_t RW = kWave / Lay::L;
@@ -1100,8 +1242,8 @@ int launch_route(Lists<kRouteLists>& ls, RouteArgs a, const size_t* tokens, int 
                 }
             }
             const uint32_t slots = RW * static_cast<uint32_t>(a.top_k + kMoreChoices), words = 2 * slots + std::max({for_groups, 2 * columns, 3 * slots});
-            // (few choices of many experts have gone the other way, and more than few need more than few experts)
-            if constexpr (Lay::VEC * Lay::NV * Lay::L <= kNarrowExperts) {
+            // (few choices of many experts have gone the other way, as has one expert, and more than few need more than few experts)
+            if constexpr (Lay::VEC * Lay::NV * Lay::L <= kNarrowExperts && Lay::VEC * Lay::NV * Lay::L > 1) {
                 if (few) launch(k_route<TYPE, Lay::VEC, Lay::L, Lay::NV, true>, words);
             }
             if constexpr (Lay::VEC * Lay::NV * Lay::L > kFewChoices) {

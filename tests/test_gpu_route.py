@@ -226,6 +226,22 @@ def test_pairs_that_a_bias_brings_together(bg, experts, score):
             check(bg, [x], 4, bias=b, score=score, groups=experts, top_groups=experts // 2 + 1)
 
 
+@pytest.mark.parametrize("experts", [4, 5, 8, 24, 64, 256])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_a_better_one_behind_many_equal_ones(bg, experts, score):
+    """Logits that are all the same but for one or two that are a step apart: 32 bits see one score, and the best expert is behind more equal ones than are chosen."""
+    base = np.full((1, experts), 1.25, np.float32)
+    bias = torch.zeros(experts, device="cuda")
+    for at in {1, 3, experts // 2, experts - 1}:
+        for other in (None, 0, experts - 2):
+            z = base.copy()
+            if other is not None and other != at:
+                z[0, other] = np.nextafter(np.float32(1.25), np.float32(0.0))
+            z[0, at] = np.nextafter(np.float32(1.25), np.float32(2.0))
+            for top in {1, 2, 3, min(experts, 8) - 1}:
+                check(bg, [torch.from_numpy(z).cuda()], top, bias=bias, score=score)
+
+
 def test_numbers_that_are_not_finite(bg):
     for experts in (8, 60, 256, 1030):
         g = torch.Generator(device="cuda").manual_seed(experts)
