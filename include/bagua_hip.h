@@ -573,7 +573,8 @@ int bagua_route_grad(int dtype, const void* const* logits, size_t ld, const size
  *   stats     host[k] of device fp32[rows[i]][3], written: m = max x, sum of exp((x - m) / T), and with labels the sum of exp(x - m), else 0
  *   workspace device, >= bagua_distill_workspace_bytes(sum of rows, vocab) bytes, 16-byte aligned; one for more rows or a larger vocabulary does for fewer.
  *             Calls on one workspace must not overlap in time.
- *   limits    1 <= k <= BAGUA_MAX_WORKERS, vocab <= BAGUA_MAX_VOCABULARY, 1 <= top <= BAGUA_MAX_TEACHER_ENTRIES, 2^-60 <= T <= 2^60, |weights| <= 2^64
+ *   limits    1 <= k <= BAGUA_MAX_WORKERS, vocab <= BAGUA_MAX_VOCABULARY, 1 <= top <= BAGUA_MAX_TEACHER_ENTRIES, 2^-20 <= T <= 2^20, |weights| <= 2^64; a row's finite
+ *             logits less than 2^100 apart.  Exponentials below 2^-126 count as 0.  The teacher's part is T^2 times a difference of entropies in fp32: it is off by some 2^-20 T^2, however small it is.
  * bagua_distill_grad: backward, with the same arguments; stats as bagua_distill_loss left them.
  *   upstream  host[k] of device fp32, the gradient of each row's loss (upstream_per_row: [rows[i]]) or of all of a worker's ([1]); NULL: 1
  *   dlogits   host[k] of device [rows[i]][vocab] of dtype, rows ld_out apart, written: every element.  It may be the logits' own memory (dlogits[i] == logits[i],

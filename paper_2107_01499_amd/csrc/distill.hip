@@ -539,7 +539,8 @@ inline int distill_check(const DistillCall& c, Lists<P>& ls, DistillArgs& a, Ran
         c.top < 1 || c.ids_ld < static_cast<size_t>(c.top) || !type_ok(c.teacher_type) || !c.teacher || c.teacher_ld < static_cast<size_t>(c.top) ||
         (c.labels && c.label_bytes != 4 && c.label_bytes != 8) || !(c.temperature > 0.0) || !(c.temperature < INFINITY) || !(std::fabs(c.teacher_weight) < INFINITY) || !(std::fabs(c.label_weight) < INFINITY))
         return BAGUA_ERR_INVALID_ARG;
-    if (c.temperature < 0x1p-60 || c.temperature > 0x1p60 || std::fabs(c.teacher_weight) > 0x1p64 || std::fabs(c.label_weight) > 0x1p64) return BAGUA_ERR_UNSUPPORTED;
+    // (temperatures whose squares, times the weight, are numbers, and leave the quotients of logits within fp32)
+    if (c.temperature < 0x1p-20 || c.temperature > 0x1p20 || std::fabs(c.teacher_weight) > 0x1p64 || std::fabs(c.label_weight) > 0x1p64) return BAGUA_ERR_UNSUPPORTED;
     if (c.vocab > BAGUA_MAX_VOCABULARY || c.top > BAGUA_MAX_TEACHER_ENTRIES || c.ld > kMostStride || c.ids_ld > kMostStride || c.teacher_ld > kMostStride) return BAGUA_ERR_UNSUPPORTED;
     const size_t element = type_bytes(c.dtype), top = static_cast<size_t>(c.top), id_size = static_cast<size_t>(c.id_bytes), label_size = static_cast<size_t>(c.label_bytes);
     total = 0;

@@ -34,6 +34,7 @@ BAD = [(dict(dtype=3), INVALID), (dict(logits=None), INVALID), (dict(logits=ptrs
        (dict(top=1025, ids_ld=1025, teacher_ld=1025), UNSUPPORTED), (dict(teacher_type=3), INVALID), (dict(teacher=None), INVALID), (dict(teacher=ptrs(None)), INVALID),
        (dict(label_bytes=1), INVALID), (dict(labels=ptrs(None)), INVALID), (dict(mask=ptrs(None)), INVALID), (dict(temperature=0.0), INVALID), (dict(temperature=-1.0), INVALID),
        (dict(temperature=math.nan), INVALID), (dict(temperature=math.inf), INVALID), (dict(temperature=1e-30), UNSUPPORTED), (dict(temperature=1e30), UNSUPPORTED),
+       (dict(temperature=1.1 * 2.0 ** 20), UNSUPPORTED), (dict(temperature=0.9 * 2.0 ** -20), UNSUPPORTED),
        (dict(teach=math.nan), INVALID), (dict(tell=math.inf), INVALID), (dict(teach=1e30), UNSUPPORTED), (dict(tell=-1e300), UNSUPPORTED), (dict(ld=1 << 50), UNSUPPORTED), (dict(ids_ld=1 << 50), UNSUPPORTED), (dict(teacher_ld=1 << 50), UNSUPPORTED),
        (dict(logits=ptrs(X + 2)), ALIGN), (dict(dtype=1, logits=ptrs(X + 1)), ALIGN), (dict(ids=ptrs(I + 4)), ALIGN), (dict(teacher=ptrs(T + 2)), ALIGN),
        (dict(teacher_type=2, teacher=ptrs(T + 1)), ALIGN), (dict(labels=ptrs(B + 4)), ALIGN), (dict(stats=None), INVALID), (dict(stats=ptrs(None)), INVALID), (dict(stats=ptrs(S + 2)), ALIGN)]

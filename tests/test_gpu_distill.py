@@ -142,7 +142,10 @@ def check(bg, s, temperature=1.0, teach=1.0, tell=0.5, up="one", pad=0, offset=0
         got = stats[w][:n].double().cpu().numpy()
         assert np.array_equal(got[:, 0], want_stats[:, 0]) and np.all(np.abs(got[:, 1:] - want_stats[:, 1:]) <= in_sum * want_stats[:, 1:])
         got = out[w].double().cpu().numpy()
-        allowed = 2 * in_exp * size + HALF_ULP[dtype] * np.abs(want) * 1.001 + LEAST[dtype]
+        # (the exponential of the vector ALU gives 0 where it is below 2^-126, the least number that is not subnormal; it is then divided by a sum that is not below 1,
+        # the row's largest logit's part, and multiplied by u T teach or u tell: an element is off by up to 2^-126 (|u| T |teach| + |u tell|))
+        none = 2.0 ** -126 * (1.0 if u is None else np.abs(u.double().numpy()[:, None])) * (temperature * abs(teach) + abs(tell))
+        allowed = 2 * in_exp * size + HALF_ULP[dtype] * np.abs(want) * 1.001 + LEAST[dtype] + none
         assert np.all(np.abs(got - want) <= allowed), np.max(np.abs(got - want) / allowed)
         if not in_place:
             assert untouched(out[w], 5.0)
@@ -160,6 +163,14 @@ def test_every_vocabulary(bg, vocab, dtype):
     for temperature, labels, up in ((1.0, None, "none"), (1.0, torch.int64, "one"), (2.0, torch.int32, "rows"), (0.7, None, "one")):
         s = inputs([5, 0, 1, 3], vocab, top, dtype, vocab, labels=labels, pad=vocab % 3, offset=vocab % 2)
         check(bg, s, temperature, up=up, pad=(vocab + 1) % 4, offset=vocab % 5)
+
+
+@pytest.mark.parametrize("labels", [None, torch.int64])
+@pytest.mark.parametrize("temperature", [2.0 ** -20, 0.01, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 5.0, 100.0, 2.0 ** 20])
+def test_every_temperature(bg, temperature, labels):
+    # (weights that leave the gradients of 16 bits finite)
+    for dtype, rows, vocab, teach in (("f32", [3, 2], 1009, 1.0), ("f32", [2], 17001, -2.0 ** 40), ("bf16", [2, 1], 40001, 1.0), ("f16", [4], 77, 1.0 / temperature)):
+        check(bg, inputs(rows, vocab, 9, dtype, vocab, labels=labels), temperature, teach=teach, tell=0.3, up="rows")
 
 
 @pytest.mark.parametrize("top", [1, 2, 63, 64, 65, 130, 1024])
