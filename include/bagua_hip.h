@@ -580,7 +580,8 @@ int bagua_route_grad(int dtype, const void* const* logits, size_t ld, const size
  *   dlogits   host[k] of device [rows[i]][vocab] of dtype, rows ld_out apart, written: every element.  It may be the logits' own memory (dlogits[i] == logits[i],
  *             ld_out == ld), and then takes their place; any other overlap is refused.
  * A row with neither entries nor a label has gradient 0, whatever its logits are.  NaN and +infinity in a row that counts make its loss and gradient
- * NaN; -infinity is a probability of 0: where the teacher or the label wants it, the loss is +infinity.  Sums are formed in fp32 in a fixed order.
+ * NaN; -infinity is a probability of 0: where the teacher or the label wants it, the loss is +infinity.  Sums are formed in fp32, in an order that
+ * the sizes and the place of a row's first element in its 128 bytes of memory fix.
  */
 #define BAGUA_MAX_VOCABULARY 0x40000000
 #define BAGUA_MAX_TEACHER_ENTRIES 1024

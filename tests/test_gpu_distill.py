@@ -274,6 +274,22 @@ def test_logits_of_great_magnitude(bg):
         check(bg, s, 2.0)
 
 
+def test_rows_far_apart(bg):
+    """Offsets that pass 32 bits."""
+    far = 2 ** 31 + 8
+
+    def apart(rows):
+        wide = torch.empty(2 * far + rows.shape[1], device="cuda", dtype=rows.dtype).as_strided(rows.shape, (far, 1))
+        wide.copy_(rows)
+        return wide
+
+    for vocab, dtype in ((1009, "bf16"), (40001, "f32")):
+        s = inputs([3], vocab, 5, dtype, vocab)
+        # (sums in another order than side by side, where rows begin elsewhere in a line of memory: against 64 bits, then, with the gradient where the logits are)
+        check(bg, dict(s, **{n: [apart(s[n][0])] for n in ("logits", "ids", "teacher")}), 2.0, in_place=True)
+    torch.cuda.empty_cache()
+
+
 def test_as_many_workers_as_there_may_be(bg):
     rows = [0, 5, 0, 0, 17] + [(7 * i) % 11 for i in range(25)] + [0, 3]
     assert len(rows) == bg.MAX_WORKERS

@@ -314,6 +314,33 @@ def test_many_tokens(bg):
     check(bg, xs, 4, bias=torch.zeros(300, device="cuda"), score="sigmoid")
 
 
+def test_rows_far_apart(bg):
+    """Offsets that pass 32 bits, in logits, ids, weights and gradients, give what rows side by side give."""
+    far = 2 ** 31 + 8
+
+    def apart(rows):
+        wide = torch.empty(2 * far + rows.shape[1], device="cuda", dtype=rows.dtype).as_strided(rows.shape, (far, 1))
+        wide.copy_(rows)
+        return wide
+
+    for experts, dtype in ((8, "bf16"), (64, "bf16"), (60, "f32"), (256, "bf16")):
+        x = logits_of([3], experts, dtype, experts)[0]
+        (ids,), (weights,) = run(bg, [x], 4, score="sigmoid")
+        up, want = torch.randn(3, 4, device="cuda"), torch.empty_like(x)
+        bg.bagua_route_grad([x], [ids[:3]], None, [up], [want], score=code(bg, "sigmoid"))
+        far_x = apart(x)
+        for id_type in (torch.int32, torch.int64):
+            far_ids = apart(torch.full((3, 4), -9, device="cuda", dtype=id_type))
+            far_weights = apart(torch.zeros(3, 4, device="cuda"))
+            bg.bagua_route([far_x], None, [far_ids], [far_weights], score=code(bg, "sigmoid"))
+            assert torch.equal(far_ids.long(), ids[:3].long()) and torch.equal(far_weights, weights[:3])
+            out = apart(torch.zeros_like(x))
+            bg.bagua_route_grad([far_x], [far_ids], None, [apart(up)], [out], score=code(bg, "sigmoid"))
+            assert torch.equal(out, want)
+            del far_ids, far_weights, out
+    torch.cuda.empty_cache()
+
+
 def test_as_many_workers_as_there_may_be(bg):
     tokens = [0, 5, 0, 0, 17] + [(7 * i) % 11 for i in range(25)] + [0, 3]
     assert len(tokens) == bg.MAX_WORKERS
