@@ -652,11 +652,13 @@ __device__ __forceinline__ void sort_step(C (&c)[N], float (&x)[N], int (&e)[N])
     }
 }
 
-// The forward pass of up to 8 experts in one group, but for whole 16-bit logits: a row in a lane, sorted whole, so that no lane asks another anything, and lanes
-// whose scores 32 bits cannot tell apart sort them in 64, all at once.  k_route | this: 262144 rows of 8, bf16, sigmoid and a bias, four choices 23.0 | 11.7 us, of 4 14.7 | 8.9;
-// fp32, two choices, of 8 6.6 | 6.3, of 2 7.7 | 4.6, and where all the scores are within 1e-3 (65536 rows, six choices) 49 | 13.5.  Whole 16-bit logits lose: 1048576 rows of 8,
-// k_route_16 12.4 | 15.3.  16 experts a lane: fp32, 32768 rows 5.6 | 8.0.  Small launches by latency: 96 rows of 8, fp32, 3.9 us (4.6).
-constexpr int kLaneExperts = 8;
+// The forward pass of up to 8 experts in one group, and of up to 16 with some choices, but for whole 16-bit logits with few choices: a row in a lane, sorted whole, so that
+// no lane asks another anything, and lanes whose scores 32 bits cannot tell apart sort them in 64, all at once.  k_route | this: 262144 rows of 8, bf16, sigmoid and a bias, four
+// choices 23.0 | 11.7 us, of 4 14.7 | 8.9; fp32, two choices, of 8 6.6 | 6.3, of 2 7.7 | 4.6, and where all the scores are within 1e-3 (65536 rows, six choices) 49 | 13.5.  Rows of
+// 16, bf16 with a bias: 262144 rows, 3 choices 18.0 | 22.6, 4 25.1 | 23.6, 8 57.1 | 26.5; 32768 rows 14.0 | 12.7, 17.7 | 15.1, 31.8 | 18.4; 100 rows 6.5 | 9.4, 7.2 | 9.6, 9.0 | 10.5.
+// Whole 16-bit logits lose: 1048576 rows of 8, k_route_16 12.4 | 15.3.  Scores and places as one key of 64 bits: 8 experts the same, 16 half as fast again.  Small launches by
+// latency: 96 rows of 8, fp32, 3.9 us (4.6).
+constexpr int kLaneExperts = 16, kSomeChoices = 4;
 template <int TYPE, int VEC, int NV>
 __global__ void __launch_bounds__(kWave * kRouteWaves)
 k_route_lane(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
@@ -1161,7 +1163,8 @@ inline void with_one_lane(int experts, const F& f)
     else if (experts < V && experts <= 4) f(RouteLayout<1, 1, 4>());
     else if (experts < V) f(RouteLayout<1, 1, V>());
     else if (experts <= V) f(RouteLayout<V, 1, 1>());
-    else f(RouteLayout<V, 1, 8 / V>());
+    else if (experts <= 8) f(RouteLayout<V, 1, 8 / V>());
+    else f(RouteLayout<V, 1, 16 / V>());
 }
 // 16 lanes at least.
 template <int V, typename F>
@@ -1224,7 +1227,7 @@ int launch_route(Lists<kRouteLists>& ls, RouteArgs a, const size_t* tokens, int 
         });
         return status;
     }
-    if (a.experts <= kLaneExperts && a.groups == 1 && !whole_keys) {
+    if (a.experts <= (a.top_k >= kSomeChoices ? kLaneExperts : 8) && a.groups == 1 && !(whole_keys && few)) {
         with_one_lane<V>(a.experts, [&](auto layout) {
             typedef decltype(layout) Lay;
             with(kWave, [&](uint32_t, auto&& launch) { launch(k_route_lane<TYPE, Lay::VEC, Lay::NV>, 0); });

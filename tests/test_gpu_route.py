@@ -156,7 +156,7 @@ def test_groups(bg, experts, groups, top_groups, top, dtype):
                 check(bg, xs, top, bias=b, score=score, groups=groups, top_groups=top_groups, group_best=best)
 
 
-@pytest.mark.parametrize("experts,top", [(e, k) for e in (8, 64, 70, 256, 2048) for k in (1, 2, 3, 5, 8, 17, 63, 64) if k <= e])
+@pytest.mark.parametrize("experts,top", [(e, k) for e in (8, 9, 16, 64, 70, 256, 2048) for k in (1, 2, 3, 4, 5, 8, 9, 17, 63, 64) if k <= e])
 def test_every_number_of_choices(bg, experts, top):
     for dtype in TYPES:
         xs = logits_of([19], experts, dtype, top)
@@ -164,7 +164,7 @@ def test_every_number_of_choices(bg, experts, top):
         check(bg, xs, top, bias=torch.zeros(experts, device="cuda"), score="sigmoid")
 
 
-@pytest.mark.parametrize("experts", [4, 8, 60, 256, 1030])
+@pytest.mark.parametrize("experts", [4, 8, 11, 16, 60, 256, 1030])
 @pytest.mark.parametrize("bias", [None, "zero", "steps"])
 def test_equal_scores_go_to_the_lowest_index(bg, experts, bias):
     """Few different logits: ties within the choices, at their end, and longer than the rounds that look for their end; whole rows of one value, both zeros."""
@@ -186,7 +186,7 @@ def test_equal_scores_go_to_the_lowest_index(bg, experts, bias):
                     check(bg, [x.to(TYPES[dtype])], min(experts // 2, 6), bias=b, score=score, groups=4, top_groups=2)
 
 
-@pytest.mark.parametrize("experts", [8, 64, 256, 2048])
+@pytest.mark.parametrize("experts", [8, 16, 64, 256, 2048])
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 def test_scores_that_32_bits_cannot_tell_apart(bg, experts, score):
     """Logits one unit of their last place apart, in an order that is not that of the experts: scores in 32 bits are the same, or the wrong way round."""
@@ -204,7 +204,7 @@ def test_scores_that_32_bits_cannot_tell_apart(bg, experts, score):
     check(bg, [x], 8, bias=bias, score=score)
 
 
-@pytest.mark.parametrize("experts", [8, 24, 64, 128, 256, 1030])
+@pytest.mark.parametrize("experts", [8, 15, 16, 24, 64, 128, 256, 1030])
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 def test_pairs_that_a_bias_brings_together(bg, experts, score):
     """The best experts in pairs whose scores with bias differ by next to nothing: one order in 64 bits, the other or none in 32.  Flat and peaked rows."""
@@ -226,7 +226,7 @@ def test_pairs_that_a_bias_brings_together(bg, experts, score):
             check(bg, [x], 4, bias=b, score=score, groups=experts, top_groups=experts // 2 + 1)
 
 
-@pytest.mark.parametrize("experts", [4, 5, 8, 24, 64, 256])
+@pytest.mark.parametrize("experts", [4, 5, 8, 13, 16, 24, 64, 256])
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 def test_a_better_one_behind_many_equal_ones(bg, experts, score):
     """Logits that are all the same but for one or two that are a step apart: 32 bits see one score, and the best expert is behind more equal ones than are chosen."""
@@ -243,7 +243,7 @@ def test_a_better_one_behind_many_equal_ones(bg, experts, score):
 
 
 def test_numbers_that_are_not_finite(bg):
-    for experts in (8, 60, 256, 1030):
+    for experts in (8, 14, 60, 256, 1030):
         g = torch.Generator(device="cuda").manual_seed(experts)
         bias = torch.randn(experts, device="cuda", generator=g) * 0.1
         for dtype in TYPES:
