@@ -1171,7 +1171,9 @@ template <int V, typename F>
 inline void with_many_lanes(int experts, const F& f)
 {
     constexpr int N = 16 / V;
-    if (experts <= 64) f(RouteLayout<4, 16, 1>());
+    if (experts <= 16) f(RouteLayout<1, 16, 1>());          // (an element or two a lane, so that no lane is left without)
+    else if (experts <= 32) f(RouteLayout<1, 16, 2>());
+    else if (experts <= 64) f(RouteLayout<4, 16, 1>());
     else if (experts <= 128) f(RouteLayout<V, 16, N / 2>());
     else if (experts <= 256) f(RouteLayout<V, 16, N>());
     else if (experts <= 512) f(RouteLayout<V, 32, N>());
@@ -1179,9 +1181,12 @@ inline void with_many_lanes(int experts, const F& f)
     else f(RouteLayout<V, 64, 2 * N>());
 }
 
-// The line between the two layouts, for what is not chosen by whole 16-bit logits, and few choices.  Few lanes a row | 16 lanes and more, bf16 with a bias and fp32 without:
+// The line between few lanes a row | 16 lanes and more, for what is not chosen by whole 16-bit logits, and few choices.  More than 32 experts, bf16 with a bias and fp32 without:
 // 1024 x 60 9.9 | 4.8 and 5.8 | 4.6 us, 32768 x 60 14.1 | 8.7 and 9.1 | 8.0, 131072 x 60 23.3 | 23.8 and 18.4 | 21.8; 131072 x 128 30.7 | 27.9 and 23.1 | 23.8, 131072 x 256
-// 56.8 | 40.9 and 41.6 | 30.7.
+// 56.8 | 40.9 and 41.6 | 30.7.  Fewer, where few lanes take less time for long lists, and less again by the logits alone and for few choices: 32 experts, one, four and eight choices,
+// with a bias, 8192 rows 6.9 | 4.5, 12.7 | 4.8, 22.7 | 5.6; 32768 8.0 | 7.6, 13.6 | 7.9, 23.2 | 8.8; 65536 8.3 | 12.0, 14.4 | 12.4, 24.8 | 13.3; without, 8192 4.9 | 4.6, 5.8 | 4.6,
+// 10.1 | 4.7; 32768 5.0 | 7.7, 9.0 | 7.7, 15.8 | 7.9; 65536 6.5 | 11.5, 9.8 | 11.5, 16.8 | 11.8.  12 experts, a lane a row where choices are more: 8192 5.8 | 4.3, 12.1 | 4.5,
+// 15.2 | 4.9; 65536 8.5 | 11.6, 16.4 | 11.9, 17.6 | 12.5.  8 experts, a lane a row: 8192 5.3 | 4.3, 6.0 | 4.4, 8.0 | 4.6; 32768 7.0 | 7.5, 8.3 | 7.7, 9.2 | 8.1.
 constexpr int kNarrowExperts = 64;
 constexpr size_t kFewTokens = 65536;
 
@@ -1217,7 +1222,8 @@ int launch_route(Lists<kRouteLists>& ls, RouteArgs a, const size_t* tokens, int 
             status = launch_tiles(kernel, ls, a, tiles, a.wave_words * sizeof(uint32_t), stream);
         });
     };
-    if (few && !whole_keys && a.experts > 32 && (a.experts > kNarrowExperts || all <= kFewTokens)) {
+    const size_t few_tokens = a.experts > 32 ? kFewTokens : a.experts > 8 ? kFewTokens >> (a.by_logit + (a.top_k < kSomeChoices)) : a.experts > 4 && !a.by_logit ? kFewTokens / 4 : 0;
+    if (few && !whole_keys && (a.experts > kNarrowExperts || all <= few_tokens)) {
         with_many_lanes<V>(a.experts, [&](auto layout) {
             typedef decltype(layout) Lay;
             constexpr uint32_t RW = kWave / Lay::L;

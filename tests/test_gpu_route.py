@@ -96,6 +96,26 @@ def bound(z, score, top):
     return (3 * float(np.max(z.max(1) - z.min(1), initial=0.0)) + 60 + top) * U
 
 
+def in_a_crowd(bg, xs, top, mask, bias, score, ids, pad, out, **kw):
+    """Rows of few experts lie in fewer lanes where a launch has many: beside a worker with many rows of padding they are given the same experts, and weights
+    that are as near to what they should be."""
+    experts, many = xs[0].shape[1], 65537
+    if experts > 64 or len(xs) > 31 or sum(x.shape[0] for x in xs) >= many:
+        return
+    wide = max([x.stride(0) for x in xs if x.shape[0] > 1], default=experts)
+    dtype = [k for k, v in TYPES.items() if v is xs[0].dtype][0]
+    more = list(xs) + [matrix(many, experts, TYPES[dtype], wide - experts)]
+    masks = (list(mask) if mask is not None else [torch.ones(x.shape[0], dtype=torch.bool, device="cuda") for x in xs]) + [torch.zeros(many, dtype=torch.bool, device="cuda")]
+    got = [matrix(x.shape[0], top, ids, pad) for x in more], [matrix(x.shape[0], top, torch.float32, pad, 0, 3.0) for x in more]
+    bg.bagua_route(more, masks, got[0], got[1], bias, code(bg, score), **kw)
+    assert torch.all(got[0][-1] == -1) and torch.all(got[1][-1] == 0)
+    for w, x in enumerate(xs):
+        assert torch.equal(got[0][w], out[0][w])
+        a, b = got[1][w].double().cpu().numpy(), out[1][w].double().cpu().numpy()
+        off = 2 * (bound(x.double().cpu().numpy(), score, top) * np.abs(b) + 2.0 ** -120) if x.shape[0] else 0.0
+        assert np.all((np.abs(a - b) <= off) | (np.isnan(a) & np.isnan(b)))
+
+
 def run(bg, xs, top, mask=None, bias=None, score="softmax", ids=torch.int64, pad=0, **kw):
     out = [matrix(x.shape[0], top, ids, pad, 0, -7) for x in xs], [matrix(x.shape[0], top, torch.float32, pad, 0, math.nan) for x in xs]
     bg.bagua_route(xs, mask, out[0], out[1], bias, code(bg, score), **kw)
@@ -107,6 +127,7 @@ def run(bg, xs, top, mask=None, bias=None, score="softmax", ids=torch.int64, pad
             keep[:n] = False
             keep[:n].reshape(m.shape[0], top + pad)[:, top:] = True
             assert np.all(np.isnan(rest[keep]) if fill != fill else rest[keep] == fill)
+    in_a_crowd(bg, xs, top, mask, bias, score, ids, pad, out, **kw)
     return out
 
 
