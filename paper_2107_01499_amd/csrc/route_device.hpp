@@ -356,7 +356,8 @@ __device__ __forceinline__ uint32_t groups_that_stay(const RouteArgs& a, const f
 // place in 32 bits.  Every lane sorts the keys of its part of a row, and the row's lanes take the largest of their first ones, one choice after another;
 // a choice stays in the lane that will write it.  354 instructions of the vector ALU for 16 rows of 64, of which sorting is 100 and six choices are 70, are half of its
 // time, launch and first rows much of the rest: 8 workers' 32768 rows of 64, bf16, 16.1 us, where the 48 MB are moved in 7.  Long ones are bound by the ALU: 262144 x 256,
-// bf16, 41.8 us, 3.8 TB/s.  Four to eight elements a lane and no sorting took 27 us of the first.
+// bf16, 41.8 us, 3.8 TB/s.  Four to eight elements a lane and no sorting took 27 us of the first, two
+// tiles a wave, the second asked for before the first is gone through, 18.2.
 template <int TYPE, int VEC, int L, int NV>
 __global__ void __launch_bounds__(kWave * kRouteWaves)
 k_route_16(Lists<kRouteLists> ls, RouteArgs a, uint32_t tiles)
